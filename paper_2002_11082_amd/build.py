@@ -1,8 +1,8 @@
-"""Builds libogq.so (HIP kernels + C ABI) for gfx950 with hipcc, and _marshal.so (the extension module that hands torch
-tensors to it) with g++.  Run: python -m paper_2002_11082_amd.build
+"""Builds libogq.so and libogq_groups.so (HIP kernels + C ABI) for gfx950 with hipcc, and _marshal.so (the extension module
+that hands torch tensors to them) with g++.  Run: python -m paper_2002_11082_amd.build
 
-The library is compiled as several object files in parallel (the random-rounding kernels once per bucket
-capacity) and linked into one shared library.
+The libraries are compiled as several object files in parallel (the random-rounding kernels once per bucket
+capacity) and each linked into one shared library.
 """
 from __future__ import annotations
 
@@ -18,6 +18,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libogq.so")
+GROUPS_LIB = os.path.join(PKG, "libogq_groups.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 
 HIPCC_FLAGS = [
@@ -36,6 +37,7 @@ UNITS = [("rounding_part.hip", [f"-DOGQ_PART={part}"], f"rounding_{part}.o") for
     ("decode.hip", [], "decode.o"),
     ("api.hip", [], "api.o"),
 ]
+GROUPS_UNITS = [(f"groups_{part}.hip", [], f"groups_{part}.o") for part in ("gradient", "elementwise", "matvec", "api")]
 
 
 def _run(cmd, verbose):
@@ -59,20 +61,22 @@ def _marshal_command():
 
 def build(verbose: bool = False, jobs: int = 0) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    jobs = jobs or max(1, min(len(UNITS), os.cpu_count() or 1, int(os.environ.get("MAX_JOBS", "16"))))
+    units = UNITS + GROUPS_UNITS
+    jobs = jobs or max(1, min(len(units), os.cpu_count() or 1, int(os.environ.get("MAX_JOBS", "16"))))
     shutil.rmtree(OBJ, ignore_errors=True)
     os.makedirs(OBJ)
-    objects = []
+    objects = {LIB: [], GROUPS_LIB: []}
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as pool:
         futures = []
-        for src, extra, obj in UNITS:
+        for src, extra, obj in units:
             out = os.path.join(OBJ, obj)
-            objects.append(out)
+            objects[GROUPS_LIB if src.startswith("groups_") else LIB].append(out)
             futures.append(pool.submit(_run, [hipcc, *HIPCC_FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", out], verbose))
         futures.append(pool.submit(_run, _marshal_command(), verbose))
         for f in futures:
             f.result()
-    _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB], verbose)
+    for library, parts in objects.items():
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *parts, "-o", library], verbose)
     shutil.rmtree(OBJ, ignore_errors=True)
     return LIB
 

@@ -1,0 +1,194 @@
+// Internal header of libogq_groups: the format of ogq_groups.h in device code, and the launchers that groups_api.hip calls.
+#ifndef OGQ_GROUPS_COMMON_H
+#define OGQ_GROUPS_COMMON_H
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "device_common.h"
+#include "launch.h"
+#include "ogq_groups.h"
+
+namespace ogq {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// The types of ogq_dtype_t.
+template <uint32_t DTYPE>
+struct ValueOf;
+template <>
+struct ValueOf<OGQ_FP32> { using type = float; };
+template <>
+struct ValueOf<OGQ_BF16> { using type = __bf16; };
+template <>
+struct ValueOf<OGQ_FP16> { using type = _Float16; };
+
+// The limits of a group's exponent: every q * 2^e is a value of T.
+template <class T, int BITS>
+struct ExponentLimits {
+    static constexpr bool kHalf = sizeof(T) == 2 && !__is_same(T, __bf16);
+    static constexpr int kLow = BITS == 8 ? (kHalf ? -24 : -126) : (kHalf ? -23 : -125);
+    static constexpr int kHigh = BITS == 8 ? (kHalf ? 9 : 121) : (kHalf ? 13 : 125);
+};
+
+// Eight consecutive values in 32 bits; only the first `valid` are read, the others are 0.  No alignment but the type's: the
+// hardware takes wide loads from any address.
+template <class T>
+__device__ __forceinline__ void load8(const T* from, int valid, float (&v)[8])
+{
+    T raw[8];
+    if (valid >= 8) {
+        memcpy(raw, from, sizeof raw);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[i] = i < valid ? from[i] : (T)0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)raw[i];
+}
+
+template <class T>
+__device__ __forceinline__ void store8(T* to, int valid, const float (&v)[8])
+{
+    T raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = (T)v[i];
+    if (valid >= 8) {
+        memcpy(to, raw, sizeof raw);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) to[i] = raw[i];
+    }
+}
+
+// The exponent byte of the group whose eight values per lane are v; 1 << lanes_log2 neighbouring lanes hold the group, and all lanes of
+// the wavefront are active.  The largest magnitude as an integer: infinities and NaN are the largest of all.
+template <class T, int BITS>
+__device__ __forceinline__ uint32_t exponent_byte(const float (&v)[8], uint32_t lanes_log2)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    most = max(most, dpp_u32<kDppXor1>(most));
+    most = max(most, dpp_u32<kDppXor2>(most));
+    if (lanes_log2 > 2) most = max(most, dpp_u32<kDppHalfMirror>(most));
+    if (lanes_log2 > 3) most = max(most, dpp_u32<kDppMirror>(most));
+    // 127 = 1.984375 * 2^6, 6 = 1.5 * 2^2
+    int byte = (int)(most >> 23) - (BITS == 8 ? 6 : 2) + ((most & 0x7FFFFFu) > (BITS == 8 ? 0x7E0000u : 0x400000u) ? 1 : 0);
+    byte = min(max(byte, ExponentLimits<T, BITS>::kLow + 127), ExponentLimits<T, BITS>::kHigh + 127);
+    return most >= 0x7F800000u ? 255u : (uint32_t)byte;
+}
+
+// 2^-e for an exponent byte (1 <= byte <= 252).
+__device__ __forceinline__ float inverse_power(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// 2^e for an exponent byte; infinite for 255, and a code of 0 times that is NaN.
+__device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight values as 8-bit codes.  x * 2^-e + 1.5 * 2^23 has the rounded number in its low bits, ties to even.
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], uint32_t byte)
+{
+    constexpr float kShift = 12582912.0f;
+    const float inverse = inverse_power(byte);
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        r[i] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(v[i], inverse, kShift), kShift - 127.0f, kShift + 127.0f));
+    uint2 w;
+    w.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(r[3], r[2], 0x0C0C0400u), __builtin_amdgcn_perm(r[1], r[0], 0x0C0C0400u), 0x05040100u);
+    w.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(r[7], r[6], 0x0C0C0400u), __builtin_amdgcn_perm(r[5], r[4], 0x0C0C0400u), 0x05040100u);
+    const bool finite = byte != 255u;
+    w.x = finite ? w.x : 0u;
+    w.y = finite ? w.y : 0u;
+    return w;
+}
+
+// Eight values as 4-bit codes: the conversion of the hardware rounds to the nearest of the eight numbers, ties to even, and takes
+// larger ones to 6.
+__device__ __forceinline__ uint32_t encode4(const float (&v)[8], uint32_t byte)
+{
+    const float unit = power(byte);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], unit, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], unit, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], unit, 3);
+    return byte != 255u ? w : 0u;
+}
+
+// What eight codes stand for.
+__device__ __forceinline__ void decode8(uint2 w, uint32_t byte, float (&v)[8])
+{
+    const float unit = power(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int q = (int)((i < 4 ? w.x : w.y) << (24 - 8 * (i & 3))) >> 24;
+        v[i] = (float)q * unit;
+    }
+}
+
+__device__ __forceinline__ float2 decode4_pair(bf16x2 p)
+{
+    uint32_t u;
+    memcpy(&u, &p, 4);
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t byte, float (&v)[8])
+{
+    const float unit = power(byte);
+    const float2 a = decode4_pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0)),
+                 b = decode4_pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1)),
+                 c = decode4_pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2)),
+                 d = decode4_pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3));
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+// The three pieces of a value in bf16, 8 bits of its fraction each; their sum is the value.  An infinity is its first piece alone.
+__device__ __forceinline__ void split3(float x, uint32_t& high, uint32_t& middle, uint32_t& low)
+{
+    const uint32_t u = __float_as_uint(x);
+    high = u & 0xFFFF0000u;
+    float rest = x - __uint_as_float(high);
+    rest = (u & 0x7FFFFFFFu) == 0x7F800000u ? 0.0f : rest;
+    middle = __float_as_uint(rest) & 0xFFFF0000u;
+    low = __float_as_uint(rest - __uint_as_float(middle));
+}
+
+// Launchers (groups_elementwise.hip, groups_gradient.hip, groups_matvec.hip).  Arguments already checked.
+struct Values {
+    const void* data;
+    size_t stride;
+};
+struct Result {
+    void* data;
+    size_t stride;
+};
+struct Groups {
+    void* codes;
+    uint8_t* exponents;
+};
+void launch_group_quantize(const Values& x, size_t rows, size_t cols, uint32_t dtype, const ogq_group_params_t* p,
+                           const Groups& to, hipStream_t st);
+void launch_group_dequantize(const Groups& from, size_t rows, size_t cols, const ogq_group_params_t* p, const Result& out,
+                             uint32_t dtype, hipStream_t st);
+void launch_activation_forward(const Values& x, const Values& up, size_t rows, size_t cols, uint32_t dtype, uint32_t act,
+                               const ogq_group_params_t* p, const Result& y, const Groups& x_to, const Groups& up_to, hipStream_t st);
+void launch_activation_backward(const Values& dy, const Groups& x, const Groups& up, size_t rows, size_t cols, uint32_t dtype,
+                                uint32_t act, const ogq_group_params_t* p, const Result& dx, const Result& dup, hipStream_t st);
+size_t weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t dtype);
+void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, size_t rows, size_t outs, size_t cols,
+                            const ogq_group_params_t* p, bool accumulate, float* dw, size_t dw_stride, void* workspace, hipStream_t st);
+size_t group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype);
+void launch_group_matvec(const Groups& w, size_t outs, size_t cols, const ogq_group_params_t* p, const Values& x, size_t tokens,
+                         uint32_t dtype, const Result& y, void* workspace, hipStream_t st);
+
+}  // namespace ogq
+#endif  // OGQ_GROUPS_COMMON_H

@@ -1,7 +1,8 @@
 // Argument marshalling between torch tensors and libogq's C ABI, as a CPython extension module: what binding.py's
 // ogq_quantize and ogq_dequantize_average do for every call, without the interpreter.  It checks the tensors (the kernels
 // trust their sizes), allocates the outputs the caller left out, and calls the library through the addresses that
-// binding.py hands to bind(); nothing of the path runs here and nothing links against libogq.
+// binding.py hands to bind(); nothing of the path runs here and nothing links against libogq.  The calls of ogq_groups.h are
+// in torch_marshal_groups.h.
 //
 // Why native: a call is one kernel launch (2.3 us on the host), and for gradients below about a million elements the
 // kernels take less than what the same checks cost in Python with ctypes (n = 1728, host time per call: quantize
@@ -11,14 +12,18 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdio>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 
 #include "ogq.h"
+#include "ogq_groups.h"
 
 namespace {
 
@@ -287,6 +292,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     Py_RETURN_NONE;
 }
 
+#include "torch_marshal_groups.h"
+
 template <class F>
 PyCFunction as_method(F f)
 {
@@ -297,6 +304,13 @@ PyMethodDef methods[] = {
     {"bind", as_method(bind), METH_FASTCALL, "the library's entry points and the two callables"},
     {"quantize", as_method(quantize), METH_FASTCALL, "ogq_quantize on tensors; after bind()"},
     {"dequantize_average", as_method(dequantize_average), METH_FASTCALL, "ogq_dequantize_average on tensors; after bind()"},
+    {"bind_groups", as_method(bind_groups), METH_FASTCALL, "the entry points of ogq_groups.h, their check and parameters"},
+    {"group_quantize", as_method(group_quantize), METH_FASTCALL, "ogq_group_quantize on tensors; after bind_groups()"},
+    {"group_dequantize", as_method(group_dequantize), METH_FASTCALL, "ogq_group_dequantize on tensors; after bind_groups()"},
+    {"activation_forward", as_method(activation_forward), METH_FASTCALL, "ogq_activation_forward on tensors; after bind_groups()"},
+    {"activation_backward", as_method(activation_backward), METH_FASTCALL, "ogq_activation_backward on tensors; after bind_groups()"},
+    {"weight_gradient", as_method(weight_gradient), METH_FASTCALL, "ogq_weight_gradient on tensors; after bind_groups()"},
+    {"group_matvec", as_method(group_matvec), METH_FASTCALL, "ogq_group_matvec on tensors; after bind_groups()"},
     {nullptr, nullptr, 0, nullptr},
 };
 
