@@ -17,6 +17,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // The types of ogq_dtype_t.
@@ -128,10 +129,7 @@ __device__ __forceinline__ void decode8(uint2 w, uint32_t byte, float (&v)[8])
 {
     const float unit = power(byte);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int q = (int)((i < 4 ? w.x : w.y) << (24 - 8 * (i & 3))) >> 24;
-        v[i] = (float)q * unit;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * unit;  // (a signed byte becomes a float in one instruction)
 }
 
 __device__ __forceinline__ float2 decode4_pair(bf16x2 p)

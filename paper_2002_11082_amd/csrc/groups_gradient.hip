@@ -1,7 +1,7 @@
 // libogq_groups: the gradient of a linear layer's weights from the gradient of its outputs and its 8-bit inputs,
 //   dw[o][i] = sum over t of dy[t][o] * x^[t][i].
 //
-// A workgroup holds a tile of 128 x 128 sums in registers and goes along t in steps of 32 rows.  In memory both factors have the summed index
+// A workgroup holds a tile of sums in registers and goes along t in steps of 32 rows.  In memory both factors have the summed index
 // outside; the matrix instruction wants eight of it per lane.  The rows go to LDS as they are and come back transposed (ds_read_b64_tr_b16: 16
 // lanes read four rows of 16 values and receive four values of one column each).  The codes become 16-bit values on the way to LDS, exactly.
 #include "groups_common.h"
@@ -10,13 +10,13 @@ namespace ogq {
 
 namespace {
 
-constexpr int kTile = 128;   // inputs and outputs of a workgroup's sums
 constexpr int kDepth = 32;   // rows of a step
-constexpr int kRowBytes = kTile * 2;
+constexpr int kSmall = 128;  // inputs and outputs of a workgroup's sums: weight_gradient_kernel
+constexpr int kLarge = 256;  // large_weight_gradient_kernel
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// A row of a tile in LDS is eight chunks of 32 bytes (16 values); chunk c of row k lies at c ^ twist(k): the eight rows that half a wavefront reads
+// A row of a tile in LDS is 8 or 16 chunks of 32 bytes (16 values); chunk c of row k lies at c ^ twist(k): the eight rows that half a wavefront reads
 // at once lie in different banks.
 __device__ __forceinline__ uint32_t twist(uint32_t k) { return (k & 3u) | ((k >> 1) & 4u); }
 
@@ -24,35 +24,33 @@ __device__ __forceinline__ uint32_t twist(uint32_t k) { return (k & 3u) | ((k >>
 template <class T>
 struct Rows16 {
     static constexpr int kPieces = 1;
-    uint4 raw[2];
+    uint32_t raw[8];
+    __device__ __forceinline__ void load(const T* from) { memcpy(raw, from, 32); }
     __device__ __forceinline__ void load(const T* from, int valid)
     {
         if (valid >= 16) {
-            memcpy(raw, from, 32);
-        } else {
-            uint16_t v[16];
+            load(from);
+            return;
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] = 0;
-                if (i < valid) memcpy(&v[i], from + i, 2);
-            }
-            memcpy(raw, v, 32);
+        for (int i = 0; i < 8; ++i) {
+            uint16_t low = 0, high = 0;
+            if (2 * i < valid) memcpy(&low, from + 2 * i, 2);
+            if (2 * i + 1 < valid) memcpy(&high, from + 2 * i + 1, 2);
+            raw[i] = low | (uint32_t)high << 16;
         }
     }
-    __device__ __forceinline__ void store(char* to, int) const
-    {
-        reinterpret_cast<uint4*>(to)[0] = raw[0];
-        reinterpret_cast<uint4*>(to)[1] = raw[1];
-    }
+    __device__ __forceinline__ void store(char* to, int) const { memcpy(to, raw, 32); }
 };
 template <>
 struct Rows16<float> {
     static constexpr int kPieces = 3;
     float raw[16];
+    __device__ __forceinline__ void load(const float* from) { memcpy(raw, from, 64); }
     __device__ __forceinline__ void load(const float* from, int valid)
     {
         if (valid >= 16) {
-            memcpy(raw, from, 64);
+            load(from);
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) raw[i] = i < valid ? from[i] : 0.0f;
@@ -86,8 +84,8 @@ __device__ __forceinline__ void store_codes(const uint4& codes, uint32_t byte, c
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (__is_same(T, _Float16)) {
-                const _Float16 a[2] = {(_Float16)v[2 * i], (_Float16)v[2 * i + 1]};
-                memcpy(&w[4 * h + i], a, 4);
+                const auto a = __builtin_amdgcn_cvt_pkrtz(v[2 * i], v[2 * i + 1]);
+                memcpy(&w[4 * h + i], &a, 4);
             } else {  // the upper halves, exactly
                 w[4 * h + i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
             }
@@ -96,10 +94,11 @@ __device__ __forceinline__ void store_codes(const uint4& codes, uint32_t byte, c
     memcpy(to, w, 32);
 }
 
+template <int ROW_BYTES>
 __device__ __forceinline__ s16x8 read_transposed(const char* at)
 {
     typedef __attribute__((address_space(3))) s16x4* Lds;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * kRowBytes));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * ROW_BYTES));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -110,6 +109,13 @@ __device__ __forceinline__ f32x4 multiply_add(s16x8 a, s16x8 b, f32x4 c)
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+template <class T>
+__device__ __forceinline__ f32x16 multiply_add32(s16x8 a, s16x8 b, f32x16 c)
+{
+    if constexpr (__is_same(T, _Float16)) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
 struct GradientShape {
     uint32_t rows, outs, cols, groups, group_log2;
     uint32_t tiles_in, tiles_out;  // tiles along the inputs and the outputs
@@ -117,59 +123,157 @@ struct GradientShape {
     uint64_t dy_stride, out_stride, out_part;
 };
 
-// `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the next).
+// Four neighbouring sums into a row of dw, or added to it.
+__device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t cols, bool wide, bool accumulate, f32x4 v)
+{
+    float* p = row + at;
+    if (wide && at + 4 <= cols) {
+        if (accumulate) v += *reinterpret_cast<f32x4*>(p);
+        *reinterpret_cast<f32x4*>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (at + r < cols) p[r] = accumulate ? p[r] + v[r] : v[r];
+}
+
+// What a workgroup's 256 threads bring of both factors to LDS, a step (kDepth rows) at a time: sixteen values of kUnits rows of either to a thread, on their
+// way in SETS sets of registers.
+template <class T, int TILE, int SETS>
+struct Feeder {
+    static constexpr int kUnits = TILE / 128, kUnitRows = kDepth / kUnits, kRowBytes = TILE * 2, kPlane = kDepth * kRowBytes;
+    static constexpr int kStage = (1 + Rows16<T>::kPieces) * kPlane;  // of LDS: the codes as values, then the pieces of dy
+    const T* dy;
+    const uint8_t *codes, *exponents;
+    uint64_t dy_stride, pitch;
+    uint32_t groups, group_log2, first, last, row, i_mine, o_mine;
+    uint32_t at_codes, at_byte, at_dy;
+    uint32_t whole;  // steps that are there in all rows, and can be read without asking
+    bool has_codes;
+    int valid;
+    char* to;
+    Rows16<T> g[SETS][kUnits];
+    uint4 q[SETS][kUnits];
+    uint32_t byte[SETS][kUnits];
+
+    __device__ __forceinline__ Feeder(const T* dy_, const uint8_t* codes_, const uint8_t* exponents_, const GradientShape& s, uint32_t i0, uint32_t o0, uint32_t first_,
+                                      uint32_t last_, char* lds)
+        : dy(dy_), codes(codes_), exponents(exponents_), dy_stride(s.dy_stride), pitch((uint64_t)s.groups << s.group_log2), groups(s.groups),
+          group_log2(s.group_log2), first(first_), last(last_)
+    {
+        const uint32_t chunk = threadIdx.x % (TILE / 16);
+        row = threadIdx.x / (TILE / 16);
+        i_mine = i0 + chunk * 16, o_mine = o0 + chunk * 16;
+        has_codes = i_mine < pitch;
+        valid = o_mine >= s.outs ? 0 : (int)min(16u, s.outs - o_mine);
+        to = lds + row * kRowBytes + ((chunk ^ twist(row)) * 32);  // (kUnitRows is a multiple of 16, which twist does not see)
+        // What lies behind the last input or output is any value that is there: its sums are not stored.  A thread whose sixteen outputs reach beyond the
+        // last reads on into the next row; the tensor's last rows are then left to the steps that ask.
+        const bool partial = o0 + TILE > s.outs && s.outs % 16 != 0;
+        whole = first < last ? (last - first) / kDepth : 0;
+        if (partial && whole != 0 && first + whole * kDepth == s.rows) --whole;
+        // (a thread's place in a unit's rows is held in 32 bits; reading on needs a next row)
+        if ((dy_stride | pitch) >= (1u << 24) || (partial && dy_stride < 16)) whole = 0;
+        const uint32_t i = has_codes ? i_mine : i0, o = valid != 0 ? o_mine : o0;
+        at_codes = row * (uint32_t)pitch + i;
+        at_byte = row * groups + (i >> group_log2);
+        at_dy = row * (uint32_t)dy_stride + o;
+    }
+    // Of step n, of the whole ones.  (One behind the last of them is the last one again, and not used.)
+    __device__ __forceinline__ void fetch_codes(uint32_t n, int set, int u)
+    {
+        const uint32_t t = first + min(n, whole - 1) * kDepth + kUnitRows * u;
+        q[set][u] = *reinterpret_cast<const uint4*>(codes + t * pitch + at_codes);
+        byte[set][u] = (exponents + (uint64_t)t * groups)[at_byte];
+    }
+    __device__ __forceinline__ void fetch_dy(uint32_t n, int set, int u)
+    {
+        const uint32_t t = first + min(n, whole - 1) * kDepth + kUnitRows * u;
+        g[set][u].load(dy + t * dy_stride + at_dy);
+    }
+    __device__ __forceinline__ void bring_codes(uint32_t stage, int set, int u) { store_codes<T>(q[set][u], byte[set][u], to + stage * kStage + u * kUnitRows * kRowBytes); }
+    __device__ __forceinline__ void bring_dy(uint32_t stage, int set, int u) { g[set][u].store(to + stage * kStage + kPlane + u * kUnitRows * kRowBytes, kPlane); }
+    // Rows t ... of any step, what is not there as 0, to the first stage.
+    __device__ __forceinline__ void bring_asking(uint32_t t)
+    {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const uint32_t mine = t + row + kUnitRows * u;
+            q[0][u] = make_uint4(0, 0, 0, 0);
+            byte[0][u] = 127;
+            if (mine < last && has_codes) {
+                q[0][u] = *reinterpret_cast<const uint4*>(codes + mine * pitch + i_mine);
+                byte[0][u] = exponents[(uint64_t)mine * groups + (i_mine >> group_log2)];
+            }
+            g[0][u].load(dy + mine * dy_stride + o_mine, mine < last ? valid : 0);
+            bring_dy(0, 0, u);
+            bring_codes(0, 0, u);
+        }
+    }
+};
+
+// Tiles of 128 x 128 sums, 64 x 64 in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
+// next).
 template <class T>
-__global__ __launch_bounds__(256) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
+__global__ __launch_bounds__(256, 3) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
                                                               float* out)
 {
-    constexpr int kPieces = Rows16<T>::kPieces, kPlane = kDepth * kRowBytes;
-    __shared__ __align__(16) char lds[(1 + kPieces) * kPlane];
+    constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 ? 2 : 1;
+    using Feed = Feeder<T, kSmall, kSets>;
+    __shared__ __align__(16) char lds[kSets * Feed::kStage];
     const uint32_t tile = blockIdx.x % (s.tiles_in * s.tiles_out), part = blockIdx.x / (s.tiles_in * s.tiles_out);
-    const uint32_t i0 = tile % s.tiles_in * kTile, o0 = tile / s.tiles_in * kTile;
+    const uint32_t i0 = tile % s.tiles_in * kSmall, o0 = tile / s.tiles_in * kSmall;
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // what this thread brings to LDS: sixteen values of one row of either factor
-    const uint32_t row = threadIdx.x >> 3, chunk = threadIdx.x & 7;
-    const uint32_t i_mine = i0 + chunk * 16, o_mine = o0 + chunk * 16;
-    const uint64_t pitch = (uint64_t)s.groups << s.group_log2;
-    const bool has_codes = i_mine < pitch;
-    const int valid = o_mine >= s.outs ? 0 : (int)min(16u, s.outs - o_mine);
-    char* to = lds + row * kRowBytes + ((chunk ^ twist(row)) * 32);
-    Rows16<T> g;
-    uint4 q;
-    uint32_t byte;
-    const auto fetch = [&](uint32_t t) {
-        t += row;
-        q = make_uint4(0, 0, 0, 0);
-        byte = 127;
-        if (t < last && has_codes) {
-            q = *reinterpret_cast<const uint4*>(codes + t * pitch + i_mine);
-            byte = exponents[(uint64_t)t * s.groups + (i_mine >> s.group_log2)];
-        }
-        g.load(dy + t * s.dy_stride + o_mine, t < last ? valid : 0);
-    };
+    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
     f32x4 sum[4][4] = {};
     const uint32_t k = (lane >> 4) * 8 + ((lane >> 2) & 3), f = twist(k);
-    const char* from = lds + k * kRowBytes + (lane & 3) * 8;
+    const char* from = lds + k * Feed::kRowBytes + (lane & 3) * 8;
     const uint32_t ci = (wave & 1) * 4, co = (wave >> 1) * 4;  // first chunk of the wavefront's sums
-    if (first < last) fetch(first);
-    for (uint32_t t = first; t < last; t += kDepth) {
-        __syncthreads();
-        store_codes<T>(q, byte, to);
-        g.store(to + kPlane, kPlane);
-        __syncthreads();
-        if (t + kDepth < last) fetch(t + kDepth);
+    const auto products = [&](uint32_t stage) __attribute__((always_inline)) {
+        const char* at = from + stage * Feed::kStage;
         s16x8 a[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = read_transposed(from + ((ci + i) ^ f) * 32);
+        for (int i = 0; i < 4; ++i) a[i] = read_transposed<Feed::kRowBytes>(at + ((ci + i) ^ f) * 32);
 #pragma unroll
         for (int p = kPieces - 1; p >= 0; --p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const s16x8 b = read_transposed(from + (1 + p) * kPlane + ((co + j) ^ f) * 32);
+                const s16x8 b = read_transposed<Feed::kRowBytes>(at + (1 + p) * Feed::kPlane + ((co + j) ^ f) * 32);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i][j] = multiply_add<T>(a[i], b, sum[i][j]);
             }
+    };
+    // 16-bit types: two steps are on their way while one is multiplied, in two stages of LDS with one barrier a step.  fp32: one of each, which leaves room for
+    // a third workgroup on a CU (4096 x 25088 sums of 256 rows: 209 us, 270 with two).
+    const auto step = [&](uint32_t n, int set) __attribute__((always_inline)) {
+        if (kSets == 1) __syncthreads();
+        feed.bring_dy(set, set, 0);
+        feed.bring_codes(set, set, 0);
+        if (kSets == 1) __syncthreads();
+        feed.fetch_dy(n + kSets, set, 0);
+        feed.fetch_codes(n + kSets, set, 0);
+        if (kSets == 2) __syncthreads();
+        products(set);
+    };
+    if (feed.whole != 0) {
+#pragma unroll
+        for (int n = 0; n < kSets; ++n) {
+            feed.fetch_dy(n, n, 0);
+            feed.fetch_codes(n, n, 0);
+        }
+        uint32_t n = 0;
+        for (; n + kSets <= feed.whole; n += kSets) {
+            step(n, 0);
+            if constexpr (kSets == 2) step(n + 1, 1);
+        }
+        if (n < feed.whole) step(n, 0);
+    }
+    for (uint32_t t = first + feed.whole * kDepth; t < last; t += kDepth) {
+        __syncthreads();
+        feed.bring_asking(t);
+        __syncthreads();
+        products(0);
     }
     out += part * s.out_part;
     const bool wide = ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 15) == 0;
@@ -180,55 +284,218 @@ __global__ __launch_bounds__(256) void weight_gradient_kernel(const T* dy, const
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t at = i0 + (ci + i) * 16 + (lane >> 4) * 4;
-            if (at >= s.cols) continue;
-            float* p = out + o * s.out_stride + at;
-            f32x4 v = sum[i][j];
-            if (wide && at + 4 <= s.cols) {
-                if (accumulate) v += *reinterpret_cast<f32x4*>(p);
-                *reinterpret_cast<f32x4*>(p) = v;
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (at + r < s.cols) p[r] = accumulate ? p[r] + v[r] : v[r];
-            }
+            store_sums(out + o * s.out_stride, at, s.cols, wide, accumulate, sum[i][j]);
         }
     }
 }
 
-// The parts of the sum, added in their order.
-__global__ __launch_bounds__(kBlock) void add_parts_kernel(const float* parts, uint32_t number, uint64_t part, uint64_t pitch, uint32_t cols, bool accumulate,
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
+// time.
+__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_in, uint32_t tiles_out)
+{
+    constexpr uint32_t kXcds = 8, kWide = 4;
+    const uint32_t tiles = tiles_in * tiles_out, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
+    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
+    const uint32_t panel = n / (kWide * tiles_out), rest = n % (kWide * tiles_out), width = min(kWide, tiles_in - panel * kWide);
+    return make_uint2(panel * kWide + rest % width, rest / width);
+}
+
+// The order of instructions around eight products, which the matrix core takes 32 cycles for each: behind each of them, reads of operands, a few vector
+// instructions, and behind some a write to LDS and a load.
+template <int READS, int VECTOR, int WRITES>
+__device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                          // matrix
+        if (READS >= 8) __builtin_amdgcn_sched_group_barrier(0x100, READS / 8, 0);  // LDS read
+        if (i < READS % 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (VECTOR != 0) __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);  // vector
+        if (WRITES == 4 ? i % 2 == 1 : WRITES == 2 ? i >= 6 : false) {
+            __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS write
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // memory read
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles of 256 x 256 sums, 128 x 128 in each of four wavefronts, one to a SIMD, which has all of its registers: 256 hold the sums.  While a wavefront
+// multiplies what it holds of a step, it reads its share of the next one from LDS and brings the one after that there; the step behind that is on its
+// way from memory.  One barrier a step, behind which all that the matrix cores need is in registers.
+template <class T>
+__global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
+                                                                       bool accumulate, float* out)
+{
+    static_assert(Rows16<T>::kPieces == 1);
+    using Feed = Feeder<T, kLarge, 2>;
+    constexpr int kRowBytes = Feed::kRowBytes, kPlane = Feed::kPlane, kStage = Feed::kStage;
+    __shared__ __align__(16) char lds[2 * kStage];
+    const uint32_t tiles = s.tiles_in * s.tiles_out, part = blockIdx.x / tiles;
+    const uint2 tile = tile_of(blockIdx.x % tiles, s.tiles_in, s.tiles_out);
+    const uint32_t i0 = tile.x * kLarge, o0 = tile.y * kLarge;
+    const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
+    // operands of v_mfma_f32_32x32x16: lane l holds k = l / 32 * 8 ... of column l % 32
+    const uint32_t k = (lane >> 5) * 8 + ((lane >> 2) & 3), f = twist(k), side = (lane >> 4) & 1;
+    const uint32_t ci = (wave & 1) * 8, co = (wave >> 1) * 8;  // first chunk of the wavefront's sums
+    const char *from_in[4], *from_out[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        from_in[n] = lds + k * kRowBytes + (lane & 3) * 8 + (((ci + 2 * n + side) ^ f) * 32);
+        from_out[n] = lds + k * kRowBytes + (lane & 3) * 8 + (((co + 2 * n + side) ^ f) * 32);
+    }
+    using Operands = s16x8[4][2];
+    // Operand n of a factor, and all of one.
+    const auto read = [&](Operands& r, const char* const (&at)[4], uint32_t stage, int plane, int n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) r[n][h] = read_transposed<kRowBytes>(at[n] + stage * kStage + plane * kPlane + h * 16 * kRowBytes);
+    };
+    f32x16 sum[4][4] = {};
+    // An eighth of a step's products.
+    const auto products = [&](const Operands& in, const Operands& o, int eighth) __attribute__((always_inline)) {
+        const int h = eighth / 4, i = eighth % 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[i][j] = multiply_add32<T>(in[i][h], o[j][h], sum[i][j]);
+    };
+    // One step: what it multiplies is held in `in` and `o`, the next one's goes to the others.  Step n + 1 is in LDS, step n + 2 goes where step n was, and
+    // step n + 4 sets off.
+    const auto step = [&](uint32_t n, uint32_t here, Operands& in, Operands& o, Operands& next_in, Operands& next_o) __attribute__((always_inline)) {
+        const uint32_t next = here ^ 1;
+        read(next_in, from_in, next, 0, 0), read(next_o, from_out, next, 1, 0), read(next_o, from_out, next, 1, 1);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            feed.bring_dy(here, here, u);
+            feed.fetch_dy(n + 4, here, u);
+        }
+        products(in, o, 0), products(in, o, 1);
+        interleave<12, 2, 4>();
+        read(next_o, from_out, next, 1, 2), read(next_o, from_out, next, 1, 3), read(next_in, from_in, next, 0, 1);
+        feed.bring_codes(here, here, 0);
+        feed.fetch_codes(n + 4, here, 0);
+        products(in, o, 2), products(in, o, 3);
+        interleave<12, 6, 2>();
+        read(next_in, from_in, next, 0, 2), read(next_in, from_in, next, 0, 3);
+        feed.bring_codes(here, here, 1);
+        feed.fetch_codes(n + 4, here, 1);
+        products(in, o, 4), products(in, o, 5);
+        interleave<8, 6, 2>();
+        // the barrier between the last products: those before it give the writes time, those behind it the other wavefronts
+        products(in, o, 6);
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        products(in, o, 7);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Operands a, b, na, nb;
+    if (feed.whole != 0) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                feed.fetch_dy(n, n, u);
+                feed.fetch_codes(n, n, u);
+            }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                feed.bring_dy(n, n, u);
+                feed.fetch_dy(n + 2, n, u);
+                feed.bring_codes(n, n, u);
+                feed.fetch_codes(n + 2, n, u);
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) read(a, from_in, 0, 0, k), read(b, from_out, 0, 1, k);
+        __syncthreads();
+        uint32_t n = 0;
+        for (; n + 2 <= feed.whole; n += 2) {
+            step(n, 0, a, b, na, nb);
+            step(n + 1, 1, na, nb, a, b);
+        }
+        if (n < feed.whole) step(n, 0, a, b, na, nb);
+    }
+    for (uint32_t t = first + feed.whole * kDepth; t < last; t += kDepth) {
+        feed.bring_asking(t);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) read(a, from_in, 0, 0, k), read(b, from_out, 0, 1, k);
+#pragma unroll
+        for (int eighth = 0; eighth < 8; ++eighth) products(a, b, eighth);
+        __syncthreads();
+    }
+    out += part * s.out_part;
+    const bool wide = ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 15) == 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t o = o0 + (co + 2 * j) * 16 + (lane & 31);
+        if (o >= s.outs) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const f32x4 v = {sum[i][j][4 * m], sum[i][j][4 * m + 1], sum[i][j][4 * m + 2], sum[i][j][4 * m + 3]};
+                store_sums(out + o * s.out_stride, i0 + (ci + 2 * i) * 16 + 8 * m + (lane >> 5) * 4, s.cols, wide, accumulate, v);
+            }
+    }
+}
+
+// The parts of the sums, added in an order that their number alone decides.  Four sums to a thread, and four threads to them: each adds every fourth part.
+__global__ __launch_bounds__(kBlock) void add_parts_kernel(const f32x4* parts, uint32_t number, uint32_t quads, uint32_t row_quads, uint32_t cols, bool accumulate,
                                                            float* dw, uint64_t dw_stride)
 {
-    const uint32_t i = (blockIdx.x * kBlock + threadIdx.x) * 4;
-    if (i >= cols) return;
-    const float* from = parts + blockIdx.y * pitch + i;
-    float* to = dw + blockIdx.y * dw_stride + i;
-    const int valid = min(4u, cols - i);
-    f32x4 v = *reinterpret_cast<const f32x4*>(from);
-    for (uint32_t n = 1; n < number; ++n) v += *reinterpret_cast<const f32x4*>(from + n * part);
+    __shared__ f32x4 shared[3][64];
+    const uint32_t lane = threadIdx.x & 63, fourth = threadIdx.x >> 6, quad = blockIdx.x * 64 + lane;
+    f32x4 v = {};
+    if (quad < quads) {
+        const f32x4* from = parts + quad;
+#pragma unroll 8
+        for (uint32_t n = fourth; n < number; n += 4) v += from[(uint64_t)n * quads];
+    }
+    if (fourth != 0) shared[fourth - 1][lane] = v;
+    __syncthreads();
+    if (fourth != 0 || quad >= quads) return;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (r < valid) to[r] = accumulate ? to[r] + v[r] : v[r];
+    for (int n = 0; n < 3; ++n) v += shared[n][lane];
+    const uint32_t o = quad / row_quads, at = quad % row_quads * 4;
+    float* row = dw + o * dw_stride;
+    store_sums(row, at, cols, (reinterpret_cast<uintptr_t>(row) & 15) == 0, accumulate, v);
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-// Into how many parts a sum is cut: where the tiles alone do not fill the chip, as many as make 512 workgroups, of 256 rows at least.
-uint32_t parts_of(size_t rows, size_t outs, size_t cols)
+// Which kernel, and into how many parts a sum is cut.
+// The larger tiles where they fill most of the chip and a tile's own costs (its first steps, 256 KB of sums to store) are spread over 384 rows: 4096 x 4096 sums of 256
+// rows 26.2 us and 25.7 with the smaller ones, of 512 33.0 and 38.6, of 2048 76 and 113; not for fp32, whose three pieces want 128 KB of LDS (4096 rows: 757 us and 456).
+// Parts up to 512 workgroups in all, of 512 rows at least (the sums of a part are written and read once more): 200 x 333 sums of 16385 rows in 16 parts 23.2 us, 32
+// 18.6, 65 19.4; 1024 x 1024 of 8192 rows in 4 parts 39.7, 8 38.1, 16 47.2; of 2048 rows in 2 parts 22.8, 4 18.7, 8 22.0; 2048 x 2048 of 8192 rows in one part 113, 2
+// 102, 4 103.
+struct Plan {
+    uint32_t tile, tiles_in, tiles_out, parts, part;
+};
+
+Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
 {
-    const uint64_t tiles = (uint64_t)ceil_div(outs, kTile) * ceil_div(cols, kTile);
-    const uint64_t wanted = tiles >= 256 ? 1 : (512 + tiles - 1) / tiles, most = (rows + 255) / 256;
-    const uint64_t n = wanted < most ? wanted : most;
-    return n < 1 ? 1 : (uint32_t)n;
+    Plan p;
+    p.tile = (uint64_t)ceil_div(outs, kLarge) * ceil_div(cols, kLarge) >= 192 && dtype != OGQ_FP32 && rows >= 384 ? kLarge : kSmall;
+    p.tiles_in = ceil_div(cols, p.tile), p.tiles_out = ceil_div(outs, p.tile);
+    const uint64_t tiles = (uint64_t)p.tiles_in * p.tiles_out;
+    const uint64_t wanted = p.tile == kLarge ? 1 : 512 / tiles, most = rows / 512;
+    p.parts = (uint32_t)(wanted < most ? wanted : most);
+    if (p.parts < 1) p.parts = 1;
+    p.part = ceil_div(ceil_div(rows, p.parts), kDepth) * kDepth;
+    return p;
 }
 
 uint64_t pitch_of(size_t cols) { return (cols + 3) / 4 * 4; }
 
 }  // namespace
 
-size_t weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t)
+size_t weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t dtype)
 {
-    const uint32_t parts = parts_of(rows, outs, cols);
+    const uint32_t parts = plan_of(rows, outs, cols, dtype).parts;
     return parts > 1 ? parts * outs * pitch_of(cols) * sizeof(float) : 0;
 }
 
@@ -239,10 +506,9 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     s.rows = (uint32_t)rows, s.outs = (uint32_t)outs, s.cols = (uint32_t)cols;
     s.groups = ceil_div(cols, p->group_size);
     s.group_log2 = p->group_size == 32 ? 5 : p->group_size == 64 ? 6 : 7;
-    s.tiles_in = ceil_div(cols, kTile), s.tiles_out = ceil_div(outs, kTile);
-    const uint32_t wanted = parts_of(rows, outs, cols);
-    s.part = ceil_div(ceil_div(rows, wanted), kDepth) * kDepth;
-    const uint32_t parts = wanted;  // (the last ones may be empty: their sums are 0)
+    const Plan plan = plan_of(rows, outs, cols, dtype);
+    const uint32_t parts = plan.parts;  // (the last ones may be empty: their sums are 0)
+    s.tiles_in = plan.tiles_in, s.tiles_out = plan.tiles_out, s.part = plan.part;
     s.dy_stride = dy.stride;
     s.out_stride = parts > 1 ? pitch_of(cols) : dw_stride;
     s.out_part = parts > 1 ? outs * s.out_stride : 0;
@@ -250,12 +516,19 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     const bool add = accumulate && parts == 1;
     const dim3 grid(s.tiles_in * s.tiles_out * parts), block(256);
     const auto codes = static_cast<const uint8_t*>(x.codes);
-    if (dtype == OGQ_FP32) launch_kernel(weight_gradient_kernel<float>, grid, block, st, static_cast<const float*>(dy.data), codes, x.exponents, s, add, out);
-    else if (dtype == OGQ_BF16) launch_kernel(weight_gradient_kernel<__bf16>, grid, block, st, static_cast<const __bf16*>(dy.data), codes, x.exponents, s, add, out);
-    else launch_kernel(weight_gradient_kernel<_Float16>, grid, block, st, static_cast<const _Float16*>(dy.data), codes, x.exponents, s, add, out);
+    const auto go = [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        void (*kernel)(const T*, const uint8_t*, const uint8_t*, GradientShape, bool, float*) = weight_gradient_kernel<T>;
+        if constexpr (sizeof(T) == 2)
+            if (plan.tile == kLarge) kernel = large_weight_gradient_kernel<T>;
+        launch_kernel(kernel, grid, block, st, static_cast<const T*>(dy.data), codes, x.exponents, s, add, out);
+    };
+    if (dtype == OGQ_FP32) go((float*)nullptr);
+    else if (dtype == OGQ_BF16) go((__bf16*)nullptr);
+    else go((_Float16*)nullptr);
     if (parts > 1)
-        launch_kernel(add_parts_kernel, dim3(ceil_div(cols, 4 * kBlock), (uint32_t)outs), dim3(kBlock), st, out, parts, s.out_part, s.out_stride, s.cols,
-                      accumulate, dw, (uint64_t)dw_stride);
+        launch_kernel(add_parts_kernel, dim3(ceil_div(s.out_part / 4, 64)), dim3(kBlock), st, reinterpret_cast<const f32x4*>(out), parts, (uint32_t)(s.out_part / 4),
+                      (uint32_t)(s.out_stride / 4), s.cols, accumulate, dw, (uint64_t)dw_stride);
 }
 
 }  // namespace ogq

@@ -1,47 +1,230 @@
 // libogq_groups: tokens times the transpose of weights held in 4 bits,
 //   y[t][o] = sum over i of x[t][i] * w^[o][i].
 //
-// The weights are read once, 16 bytes per lane, and become 8 values of bf16 per dword in four conversions that take the group's power along;
-// they are the left operand of a matrix instruction whose 16 columns are tokens.  The order of the summed index within an instruction does
-// not matter as long as both operands have it: lane l holds 32 consecutive weights of row l % 16, and the tokens' values follow them.
+// group_matvec_kernel (one token) on the vector unit, group_matmul_kernel (more) on the matrix cores.  Both read 32 weights (16 bytes) per lane and
+// turn eight of them into bf16 with four conversions, which take the group's power along.
 #include "groups_common.h"
 
 namespace ogq {
 
 namespace {
 
-constexpr int kRows = 16;     // rows of weights of a workgroup
-constexpr int kStep = 128;    // columns of a wavefront's step: 32 weights in each of four lanes
-constexpr int kSplit = 8;     // wavefronts of a workgroup, which share the columns
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+constexpr int kLaneCols = 32;  // weights of a lane's load: within one group
+
+struct MatvecShape {
+    uint32_t tokens, outs, cols, groups, group_log2, row_blocks, token_blocks;
+    uint32_t steps;  // of a wavefront: chunks of columns, or of a part of the sum
+    uint64_t x_stride, y_stride, y_part;
+};
+
+__device__ __forceinline__ uint32_t word_of(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
+
+// Pair n (0 .. 15) of a lane's 32 weights; the conversion's byte is a constant of the instruction.
+#define OGQ_PAIR(cvt, w, n, unit) \
+    ((n) % 4 == 0 ? cvt(word_of(w, (n) / 4), unit, 0) : (n) % 4 == 1 ? cvt(word_of(w, (n) / 4), unit, 1) : (n) % 4 == 2 ? cvt(word_of(w, (n) / 4), unit, 2) : cvt(word_of(w, (n) / 4), unit, 3))
+
+// Two values summed over the two halves of the wavefront (of each pair of rows of 16 lanes): the lower one keeps the first's sum.
+__device__ __forceinline__ float halves_sum(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float rows_sum(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// One step of a sum of N values over the wavefront: while there are several, lanes and their partners at distance D share them, half each.
+template <int D, int N>
+__device__ __forceinline__ void sum_step(float* v, uint32_t lane, uint32_t& index)
+{
+    if constexpr (N > 1) {
+        constexpr int H = N / 2;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            if constexpr (D == 32) {
+                v[i] = halves_sum(v[i], v[i + H]);
+            } else if constexpr (D == 16) {
+                v[i] = rows_sum(v[i], v[i + H]);
+            } else {
+                const bool upper = (lane & D) != 0;
+                const float keep = upper ? v[i + H] : v[i], send = upper ? v[i] : v[i + H];
+                v[i] = keep + __uint_as_float(lane_xor<D>(__float_as_uint(send), lane));
+            }
+        }
+        index += (lane & D) ? H : 0;
+    } else {
+        v[0] += __uint_as_float(lane_xor<D>(__float_as_uint(v[0]), lane));
+    }
+}
+
+// Sums N values (a power of two) over the wavefront.  A lane ends with the sums `index`, ... (as many as N / 64, at least one).
+template <int N>
+__device__ __forceinline__ uint32_t sum_over_lanes(float* v, uint32_t lane)
+{
+    uint32_t index = 0;
+    sum_step<32, N>(v, lane, index);
+    sum_step<16, (N > 2 ? N / 2 : 1)>(v, lane, index);
+    sum_step<8, (N > 4 ? N / 4 : 1)>(v, lane, index);
+    sum_step<4, (N > 8 ? N / 8 : 1)>(v, lane, index);
+    sum_step<2, (N > 16 ? N / 16 : 1)>(v, lane, index);
+    sum_step<1, (N > 32 ? N / 32 : 1)>(v, lane, index);
+    return index;
+}
+
+// A lane's 32 values of a token, as they are in memory; `whole`: all lanes have 32, a branch of the scalar unit.
+template <class T>
+constexpr int kLaneWords = kLaneCols * sizeof(T) / 4;
+
+template <class T>
+__device__ __forceinline__ void load_lane(const T* from, int valid, bool whole, uint32_t (&to)[kLaneWords<T>])
+{
+    if (whole) {
+        memcpy(to, from, sizeof to);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLaneWords<T>; ++i) {
+        to[i] = 0;
+        if constexpr (sizeof(T) == 4) {
+            if (i < valid) memcpy(&to[i], from + i, 4);
+        } else {
+            uint16_t low = 0, high = 0;
+            if (2 * i < valid) memcpy(&low, from + 2 * i, 2);
+            if (2 * i + 1 < valid) memcpy(&high, from + 2 * i + 1, 2);
+            to[i] = low | ((uint32_t)high << 16);
+        }
+    }
+}
+
+// The same of 64 lanes' values that are all there: in the order of memory, 1 KB at once, and through LDS to the lane that wants them (a lane's own
+// 32 values lie 64 or 128 bytes from its neighbour's, four times as many trips to the cache).  Sixteen bytes p of lane l lie at p ^ (l / 2 or l).
+template <class T>
+__device__ __forceinline__ void load_turned(const T* from, uint32_t lane, uint4* turn, uint32_t (&to)[kLaneWords<T>])
+{
+    constexpr uint32_t kQuads = kLaneWords<T> / 4, kShift = kQuads == 4 ? 1 : 0;
+    uint4 q[kQuads];
+#pragma unroll
+    for (uint32_t i = 0; i < kQuads; ++i) memcpy(&q[i], from + (i * 64 + lane) * (16 / sizeof(T)), 16);
+#pragma unroll
+    for (uint32_t i = 0; i < kQuads; ++i) {
+        const uint32_t n = i * 64 + lane, of = n / kQuads;
+        turn[of * kQuads + ((n ^ (of >> kShift)) & (kQuads - 1))] = q[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (uint32_t p = 0; p < kQuads; ++p) {
+        const uint4 w = turn[lane * kQuads + ((p ^ (lane >> kShift)) & (kQuads - 1))];
+        memcpy(&to[4 * p], &w, 16);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Their products with 32 weights, added to a sum.
+template <class T>
+__device__ __forceinline__ float times(const uint32_t (&x)[kLaneWords<T>], const uint4& w, float unit, float sum)
+{
+    if constexpr (__is_same(T, __bf16)) {
+#pragma unroll
+        for (int n = 0; n < 16; ++n)
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x[n]), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w, n, unit), sum, false);
+        return sum;
+    } else if constexpr (__is_same(T, _Float16)) {
+        // (a weight times its group's power may be outside of fp16: the power comes in behind the sum)
+        float part = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 16; ++n)
+            part = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x[n]), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4, w, n, 1.0f), part, false);
+        return __builtin_fmaf(part, unit, sum);
+    } else {
+#pragma unroll
+        for (int n = 0; n < 16; ++n) {
+            const f32x2 q = OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4, w, n, unit);
+            sum = __builtin_fmaf(q[1], __uint_as_float(x[2 * n + 1]), __builtin_fmaf(q[0], __uint_as_float(x[2 * n]), sum));
+        }
+        return sum;
+    }
+}
+
+constexpr int kFew = 4;  // rows of weights of a wavefront, and most wavefronts of a workgroup
+
+// One token: a lane keeps 32 of its values and multiplies them with the same columns of four rows of weights, whose loads are all under way at
+// once, 1 KB of a row in a piece.  The wavefronts of a workgroup share the columns.  Bound by memory behind 3 us of latency: 4096 x 25088 weights
+// 13.8 us.  (Eight rows 14.1, sixteen 16.2, two 18.1; eight wavefronts 16.7; with the next piece's loads ahead of the products 14.3.)
+template <class T>
+__global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, T* y)
+{
+    // fp32: through LDS (15.6 -> 15.0 us); 16-bit types straight (15.5 through LDS)
+    constexpr bool kTurned = sizeof(T) == 4;
+    __shared__ float parts[kFew][kFew];
+    __shared__ uint4 turn[kTurned ? kFew : 1][kTurned ? 64 * kLaneWords<T> / 4 : 1];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t o0 = blockIdx.x * kFew;
+    const uint32_t pitch = s.groups << s.group_log2;
+    float sum[kFew] = {};
+    for (uint32_t chunk = wave; chunk < s.steps; chunk += waves) {
+        const uint32_t first = chunk * (64 * kLaneCols), col = first + lane * kLaneCols;
+        const bool whole = first + 64 * kLaneCols <= s.cols;
+        uint4 w[kFew];
+        uint32_t byte[kFew], v[kLaneWords<T>];
+#pragma unroll
+        for (int r = 0; r < kFew; ++r) w[r] = make_uint4(0, 0, 0, 0), byte[r] = 127;
+        if (col < pitch) {
+#pragma unroll
+            for (int r = 0; r < kFew; ++r) {
+                const uint64_t row = min(o0 + r, s.outs - 1);  // (what is not there repeats the last)
+                w[r] = *reinterpret_cast<const uint4*>(codes + row * (pitch / 2) + col / 2);
+                byte[r] = exponents[row * s.groups + (col >> s.group_log2)];
+            }
+        }
+        if constexpr (kTurned) {
+            if (whole) load_turned(x + first, lane, turn[wave], v);
+            else load_lane(x + col, (int)(s.cols - col), false, v);
+        } else {
+            load_lane(x + col, (int)(s.cols - col), whole, v);
+        }
+#pragma unroll
+        for (int r = 0; r < kFew; ++r) sum[r] = times<T>(v, w[r], power(byte[r]), sum[r]);
+    }
+    const uint32_t index = sum_over_lanes<kFew>(sum, lane);
+    parts[wave][index] = sum[0];  // (several lanes write the same)
+    __syncthreads();
+    if (threadIdx.x < kFew && o0 + threadIdx.x < s.outs) {
+        float all = parts[0][threadIdx.x];
+        for (uint32_t k = 1; k < waves; ++k) all += parts[k][threadIdx.x];
+        y[o0 + threadIdx.x] = (T)all;
+    }
+}
+
+// ----------------------------------------------------------------------------------------------------------------------
+// More tokens
+// ----------------------------------------------------------------------------------------------------------------------
 template <class T>
 constexpr int kPiecesOf = __is_same(T, __bf16) ? 1 : __is_same(T, _Float16) ? 2 : 3;
 
-// Eight values of a token in pieces of bf16 whose sum they are.
+// Eight values of a token as they are in memory, in pieces of bf16 whose sum they are.
 template <class T>
-__device__ __forceinline__ void pieces_of(const T* x, int valid, bf16x8 (&out)[kPiecesOf<T>])
+__device__ __forceinline__ void pieces_of(const uint32_t* raw, bf16x8 (&out)[kPiecesOf<T>])
 {
     if constexpr (__is_same(T, __bf16)) {
-        uint16_t v[8];
-        if (valid >= 8) {
-            memcpy(v, x, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = 0;
-                if (i < valid) memcpy(&v[i], x + i, 2);
-            }
-        }
-        memcpy(&out[0], v, 16);
+        memcpy(&out[0], raw, 16);
     } else {
-        float v[8];
-        load8(x, valid, v);
+        T v[8];
+        memcpy(v, raw, sizeof v);
         uint32_t w[3][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t a[3], b[3];
-            split3(v[2 * i], a[0], a[1], a[2]);
-            split3(v[2 * i + 1], b[0], b[1], b[2]);
+            split3((float)v[2 * i], a[0], a[1], a[2]);
+            split3((float)v[2 * i + 1], b[0], b[1], b[2]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) w[p][i] = __builtin_amdgcn_perm(b[p], a[p], 0x07060302u);
         }
@@ -50,76 +233,198 @@ __device__ __forceinline__ void pieces_of(const T* x, int valid, bf16x8 (&out)[k
     }
 }
 
-struct MatvecShape {
-    uint32_t tokens, outs, cols, groups, group_log2, row_blocks;
-    uint64_t x_stride, y_stride;
-};
+constexpr int kStep = 4 * kLaneCols;  // columns of a wavefront's step
+constexpr int kWaves = 8;             // wavefronts of a workgroup, which share the columns
 
-template <class T>
-__global__ __launch_bounds__(64 * kSplit) void group_matvec_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, T* y)
+// A wavefront's sums: 16 * RB rows of weights and 16 * NT tokens.  The order of the summed index within a matrix instruction does not matter as long
+// as both operands have it: lane l holds 32 consecutive weights of row l % 16, and the tokens' values follow them.  OUT: T, or float where the
+// columns are cut into parts that a second launch adds (y_part values from one to the next).
+template <class T, class OUT, int NT, int RB>
+__global__ __launch_bounds__(64 * kWaves) void group_matmul_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, OUT* y)
 {
-    constexpr int kPieces = kPiecesOf<T>;
-    __shared__ f32x4 parts[kSplit][64];
+    constexpr int kPieces = kPiecesOf<T>, kTiles = NT * RB;
+    __shared__ f32x4 parts[kWaves / 2][kTiles][64];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t o0 = blockIdx.x % s.row_blocks * kRows, t0 = blockIdx.x / s.row_blocks * 16;
-    const uint32_t row = min(o0 + (lane & 15), s.outs - 1), token = min(t0 + (lane & 15), s.tokens - 1);  // (what is not there repeats the last)
-    const uint64_t pitch = (uint64_t)s.groups << s.group_log2;
-    const uint8_t* w_row = codes + row * (pitch / 2);
-    const uint8_t* e_row = exponents + (uint64_t)row * s.groups;
-    const T* x_row = x + token * s.x_stride;
-    f32x4 sum = {};
-    for (uint32_t i = wave * kStep + (lane >> 4) * 32; i - (lane >> 4) * 32 < pitch; i += kSplit * kStep) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        uint32_t byte = 127;
-        if (i < pitch) {
-            w = *reinterpret_cast<const uint4*>(w_row + i / 2);
-            byte = e_row[i >> s.group_log2];
+    uint32_t block = blockIdx.x;
+    const uint32_t o0 = block % s.row_blocks * (16 * RB);
+    block /= s.row_blocks;
+    const uint32_t t0 = block % s.token_blocks * (16 * NT), part = block / s.token_blocks;
+    const uint32_t pitch = s.groups << s.group_log2;
+    const uint32_t mine = (lane >> 4) * kLaneCols;  // this lane's columns of a step
+    const uint32_t end = min((part + 1) * s.steps * kStep, pitch);
+    const uint8_t* w_row[RB];
+    const uint8_t* e_row[RB];
+    const T* x_row[NT];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const uint64_t row = min(o0 + 16 * r + (lane & 15), s.outs - 1);  // (what is not there repeats the last)
+        w_row[r] = codes + row * (pitch / 2);
+        e_row[r] = exponents + row * s.groups;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x_row[n] = x + min(t0 + 16 * n + (lane & 15), s.tokens - 1) * s.x_stride;
+    f32x4 sum[RB][NT] = {};
+    for (uint32_t first = (part * s.steps + wave) * kStep; first < end; first += kWaves * kStep) {
+        const uint32_t col = first + mine;
+        uint4 w[RB];
+        uint32_t byte[RB];
+        uint32_t v[NT][kLaneWords<T>];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) w[r] = make_uint4(0, 0, 0, 0), byte[r] = 127;
+        if (col < end) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                w[r] = *reinterpret_cast<const uint4*>(w_row[r] + col / 2);
+                byte[r] = e_row[r][col >> s.group_log2];
+            }
         }
-        const float unit = power(byte);
-        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) load_lane(x_row[n] + col, (int)(s.cols - col), first + kStep <= s.cols, v[n]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[j], unit, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[j], unit, 1),
-                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[j], unit, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[j], unit, 3)};
-            bf16x8 a;
-            memcpy(&a, p, 16);
-            bf16x8 b[kPieces];
-            const int left = (int)s.cols - (int)(i + 8 * j);
-            pieces_of<T>(x_row + i + 8 * j, left, b);
+            bf16x8 a[RB];
 #pragma unroll
-            for (int q = kPieces - 1; q >= 0; --q) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[q], sum, 0, 0, 0);
+            for (int r = 0; r < RB; ++r) {
+                const float unit = power(byte[r]);
+                const bf16x2 p[4] = {OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j, unit), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 1, unit),
+                                     OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 2, unit), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 3, unit)};
+                memcpy(&a[r], p, 16);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                bf16x8 b[kPieces];
+                pieces_of<T>(v[n] + j * (kLaneWords<T> / 4), b);
+#pragma unroll
+                for (int q = kPieces - 1; q >= 0; --q)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) sum[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r], b[q], sum[r][n], 0, 0, 0);
+            }
         }
     }
-    parts[wave][lane] = sum;
-    __syncthreads();
+    // the wavefronts' sums, in halves
+#pragma unroll
+    for (uint32_t half = kWaves / 2; half >= 1; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int k = 0; k < kTiles; ++k) parts[wave - half][k][lane] = sum[k / NT][k % NT];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int k = 0; k < kTiles; ++k) sum[k / NT][k % NT] += parts[wave][k][lane];
+        __syncthreads();
+    }
     if (wave != 0) return;
+    y += part * s.y_part;
 #pragma unroll
-    for (int n = 1; n < kSplit; ++n) sum += parts[n][lane];
-    const uint32_t t = t0 + (lane & 15), o = o0 + (lane >> 4) * 4;
-    if (t >= s.tokens) return;
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t t = t0 + 16 * n + (lane & 15);
+        if (t >= s.tokens) continue;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (o + r < s.outs) y[t * s.y_stride + o + r] = (T)sum[r];
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t o = o0 + 16 * r + (lane >> 4) * 4 + i;
+                if (o < s.outs) y[t * s.y_stride + o] = (OUT)sum[r][n][i];
+            }
+    }
+}
+
+// The parts of the sums, added in their order.
+template <class T>
+__global__ __launch_bounds__(kBlock) void add_token_parts_kernel(const float* parts, uint32_t number, uint64_t part, uint32_t outs, uint32_t blocks, T* y,
+                                                                 uint64_t y_stride)
+{
+    const uint32_t o = blockIdx.x % blocks * kBlock + threadIdx.x;
+    const uint64_t t = blockIdx.x / blocks;
+    if (o >= outs) return;
+    const float* from = parts + t * outs + o;
+    float v = *from;
+    for (uint32_t n = 1; n < number; ++n) v += from[n * part];
+    y[t * y_stride + o] = (T)v;
+}
+
+uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+
+struct Plan {
+    uint32_t token_tiles, row_tiles, row_blocks, token_blocks, parts, steps;
+};
+
+// How group_matmul_kernel is launched.
+Plan plan_of(size_t tokens, size_t outs, size_t cols)
+{
+    Plan p;
+    p.token_tiles = tokens <= 16 ? 1 : tokens <= 32 ? 2 : 4;
+    p.row_tiles = outs >= 2048 ? 4 : 1;
+    p.row_blocks = ceil_div(outs, 16 * p.row_tiles);
+    p.token_blocks = ceil_div(tokens, 16 * p.token_tiles);
+    const uint32_t steps = ceil_div(cols, kStep);
+    const uint64_t blocks = (uint64_t)p.row_blocks * p.token_blocks;
+    const uint32_t wanted = blocks >= 256 ? 1 : (uint32_t)(256 / blocks), most = ceil_div(steps, kWaves);
+    p.parts = wanted < most ? wanted : most;
+    if (p.parts < 1) p.parts = 1;
+    p.steps = ceil_div(steps, p.parts);
+    return p;
+}
+
+template <class T, class OUT>
+void launch_matmul(const Plan& p, const uint8_t* codes, const uint8_t* exponents, const T* x, const MatvecShape& s, OUT* y, hipStream_t st)
+{
+    const dim3 grid(p.row_blocks * p.token_blocks * p.parts), block(64 * kWaves);
+    const auto kernel = p.row_tiles == 4 ? (p.token_tiles == 1   ? group_matmul_kernel<T, OUT, 1, 4>
+                                            : p.token_tiles == 2 ? group_matmul_kernel<T, OUT, 2, 4>
+                                                                 : group_matmul_kernel<T, OUT, 4, 4>)
+                                         : (p.token_tiles == 1   ? group_matmul_kernel<T, OUT, 1, 1>
+                                            : p.token_tiles == 2 ? group_matmul_kernel<T, OUT, 2, 1>
+                                                                 : group_matmul_kernel<T, OUT, 4, 1>);
+    launch_kernel(kernel, grid, block, st, codes, exponents, x, s, y);
+}
+
+template <class T>
+void launch_of(const Groups& w, MatvecShape s, const T* x, T* y, void* workspace, hipStream_t st)
+{
+    const auto codes = static_cast<const uint8_t*>(w.codes);
+    if (s.tokens == 1) {
+        s.steps = ceil_div((uint64_t)s.groups << s.group_log2, 64 * kLaneCols);
+        const uint32_t rounds = ceil_div(s.steps, kFew), waves = rounds ? ceil_div(s.steps, rounds) : 1;
+        launch_kernel(group_matvec_kernel<T>, dim3(ceil_div(s.outs, kFew)), dim3(64 * waves), st, codes, w.exponents, x, s, y);
+        return;
+    }
+    const Plan p = plan_of(s.tokens, s.outs, s.cols);
+    s.row_blocks = p.row_blocks, s.token_blocks = p.token_blocks, s.steps = p.steps, s.y_part = 0;
+    if (p.parts == 1) {
+        launch_matmul<T, T>(p, codes, w.exponents, x, s, y, st);
+        return;
+    }
+    const uint64_t y_stride = s.y_stride;
+    float* parts = static_cast<float*>(workspace);
+    s.y_stride = s.outs;
+    s.y_part = (uint64_t)s.tokens * s.outs;
+    launch_matmul<T, float>(p, codes, w.exponents, x, s, parts, st);
+    const uint32_t blocks = ceil_div(s.outs, kBlock);
+    launch_kernel(add_token_parts_kernel<T>, dim3(blocks * s.tokens), dim3(kBlock), st, parts, p.parts, s.y_part, s.outs, blocks, y, y_stride);
 }
 
 }  // namespace
 
-size_t group_matvec_workspace(size_t, size_t, size_t, uint32_t) { return 0; }
+size_t group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t)
+{
+    if (tokens == 1) return 0;
+    const Plan p = plan_of(tokens, outs, cols);
+    return p.parts > 1 ? p.parts * tokens * outs * sizeof(float) : 0;
+}
 
 void launch_group_matvec(const Groups& w, size_t outs, size_t cols, const ogq_group_params_t* p, const Values& x, size_t tokens, uint32_t dtype,
-                         const Result& y, void*, hipStream_t st)
+                         const Result& y, void* workspace, hipStream_t st)
 {
-    MatvecShape s;
+    MatvecShape s = {};
     s.tokens = (uint32_t)tokens, s.outs = (uint32_t)outs, s.cols = (uint32_t)cols;
-    s.groups = (uint32_t)((cols + p->group_size - 1) / p->group_size);
+    s.groups = ceil_div(cols, p->group_size);
     s.group_log2 = p->group_size == 32 ? 5 : p->group_size == 64 ? 6 : 7;
     s.x_stride = x.stride, s.y_stride = y.stride;
-    s.row_blocks = (uint32_t)((outs + kRows - 1) / kRows);
-    const dim3 grid(s.row_blocks * (uint32_t)((tokens + 15) / 16)), block(64 * kSplit);
-    const auto codes = static_cast<const uint8_t*>(w.codes);
-    if (dtype == OGQ_FP32) launch_kernel(group_matvec_kernel<float>, grid, block, st, codes, w.exponents, static_cast<const float*>(x.data), s, static_cast<float*>(y.data));
-    else if (dtype == OGQ_BF16) launch_kernel(group_matvec_kernel<__bf16>, grid, block, st, codes, w.exponents, static_cast<const __bf16*>(x.data), s, static_cast<__bf16*>(y.data));
-    else launch_kernel(group_matvec_kernel<_Float16>, grid, block, st, codes, w.exponents, static_cast<const _Float16*>(x.data), s, static_cast<_Float16*>(y.data));
+    if (dtype == OGQ_FP32) launch_of(w, s, static_cast<const float*>(x.data), static_cast<float*>(y.data), workspace, st);
+    else if (dtype == OGQ_BF16) launch_of(w, s, static_cast<const __bf16*>(x.data), static_cast<__bf16*>(y.data), workspace, st);
+    else launch_of(w, s, static_cast<const _Float16*>(x.data), static_cast<_Float16*>(y.data), workspace, st);
 }
 
 }  // namespace ogq
