@@ -123,13 +123,18 @@ struct GradientShape {
     uint64_t dy_stride, out_stride, out_part;
 };
 
-// Four neighbouring sums into a row of dw, or added to it.
-__device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t cols, bool wide, bool accumulate, f32x4 v)
+// Four neighbouring sums into a row of dw, or added to it, at once where the row has all four (the hardware takes 16 bytes at any value's address: rows of 2589 sums
+// 20.7 us and 12.8).
+__device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t cols, bool accumulate, f32x4 v)
 {
     float* p = row + at;
-    if (wide && at + 4 <= cols) {
-        if (accumulate) v += *reinterpret_cast<f32x4*>(p);
-        *reinterpret_cast<f32x4*>(p) = v;
+    if (at + 4 <= cols) {
+        if (accumulate) {
+            f32x4 held;
+            memcpy(&held, p, sizeof held);
+            v += held;
+        }
+        memcpy(p, &v, sizeof v);
         return;
     }
 #pragma unroll
@@ -276,7 +281,6 @@ __global__ __launch_bounds__(256, 3) void weight_gradient_kernel(const T* dy, co
         products(0);
     }
     out += part * s.out_part;
-    const bool wide = ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 15) == 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t o = o0 + (co + j) * 16 + (lane & 15);
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(256, 3) void weight_gradient_kernel(const T* dy, co
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t at = i0 + (ci + i) * 16 + (lane >> 4) * 4;
-            store_sums(out + o * s.out_stride, at, s.cols, wide, accumulate, sum[i][j]);
+            store_sums(out + o * s.out_stride, at, s.cols, accumulate, sum[i][j]);
         }
     }
 }
@@ -427,7 +431,6 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
         __syncthreads();
     }
     out += part * s.out_part;
-    const bool wide = ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 15) == 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t o = o0 + (co + 2 * j) * 16 + (lane & 31);
@@ -437,7 +440,7 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 const f32x4 v = {sum[i][j][4 * m], sum[i][j][4 * m + 1], sum[i][j][4 * m + 2], sum[i][j][4 * m + 3]};
-                store_sums(out + o * s.out_stride, i0 + (ci + 2 * i) * 16 + 8 * m + (lane >> 5) * 4, s.cols, wide, accumulate, v);
+                store_sums(out + o * s.out_stride, i0 + (ci + 2 * i) * 16 + 8 * m + (lane >> 5) * 4, s.cols, accumulate, v);
             }
     }
 }
@@ -460,8 +463,7 @@ __global__ __launch_bounds__(kBlock) void add_parts_kernel(const f32x4* parts, u
 #pragma unroll
     for (int n = 0; n < 3; ++n) v += shared[n][lane];
     const uint32_t o = quad / row_quads, at = quad % row_quads * 4;
-    float* row = dw + o * dw_stride;
-    store_sums(row, at, cols, (reinterpret_cast<uintptr_t>(row) & 15) == 0, accumulate, v);
+    store_sums(dw + o * dw_stride, at, cols, accumulate, v);
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
@@ -469,9 +471,10 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // Which kernel, and into how many parts a sum is cut.
 // The larger tiles where they fill most of the chip and a tile's own costs (its first steps, 256 KB of sums to store) are spread over 384 rows: 4096 x 4096 sums of 256
 // rows 26.2 us and 25.7 with the smaller ones, of 512 33.0 and 38.6, of 2048 76 and 113; not for fp32, whose three pieces want 128 KB of LDS (4096 rows: 757 us and 456).
-// Parts up to 512 workgroups in all, of 512 rows at least (the sums of a part are written and read once more): 200 x 333 sums of 16385 rows in 16 parts 23.2 us, 32
-// 18.6, 65 19.4; 1024 x 1024 of 8192 rows in 4 parts 39.7, 8 38.1, 16 47.2; of 2048 rows in 2 parts 22.8, 4 18.7, 8 22.0; 2048 x 2048 of 8192 rows in one part 113, 2
-// 102, 4 103.
+// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a step of 32 rows takes about 1 us in fp32 and 0.45 in 16 bits.  As many parts as make the two
+// equal, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us: 200 x 333 sums of 16385 rows in fp16 (35 parts by this) in 16 parts
+// 23.2 us, 32 18.6, 65 19.4, 128 23.6; 1024 x 1024 in bf16 (6) of 8192 rows in 4 parts 39.7, 8 38.1, 16 47.2; of 2048 rows (3) in 2 parts 22.8, 4 18.7, 8 22.0; 2048 x
+// 2048 of 8192 rows (2) in one part 113, 2 102, 4 103; 512 x 512 of 512 rows in one part 10.2, 2 10.4.
 struct Plan {
     uint32_t tile, tiles_in, tiles_out, parts, part;
 };
@@ -482,9 +485,12 @@ Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
     p.tile = (uint64_t)ceil_div(outs, kLarge) * ceil_div(cols, kLarge) >= 192 && dtype != OGQ_FP32 && rows >= 384 ? kLarge : kSmall;
     p.tiles_in = ceil_div(cols, p.tile), p.tiles_out = ceil_div(outs, p.tile);
     const uint64_t tiles = (uint64_t)p.tiles_in * p.tiles_out;
-    const uint64_t wanted = p.tile == kLarge ? 1 : 512 / tiles, most = rows / 512;
-    p.parts = (uint32_t)(wanted < most ? wanted : most);
-    if (p.parts < 1) p.parts = 1;
+    p.parts = 1;
+    if (p.tile == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 192 : 512)) {
+        const uint64_t squared = (uint64_t)rows * (dtype == OGQ_FP32 ? 12000 : 5000) / (outs * cols);
+        const uint64_t most = rows / 64 < 512 / tiles ? rows / 64 : 512 / tiles;
+        while (p.parts < most && (uint64_t)(p.parts + 1) * (p.parts + 1) <= squared) ++p.parts;
+    }
     p.part = ceil_div(ceil_div(rows, p.parts), kDepth) * kDepth;
     return p;
 }
