@@ -80,15 +80,15 @@ __device__ __forceinline__ uint32_t sum_over_lanes(float* v, uint32_t lane)
 template <class T>
 constexpr int kLaneWords = kLaneCols * sizeof(T) / 4;
 
-template <class T>
-__device__ __forceinline__ void load_lane(const T* from, int valid, bool whole, uint32_t (&to)[kLaneWords<T>])
+template <class T, int WORDS>
+__device__ __forceinline__ void load_words(const T* from, int valid, bool whole, uint32_t (&to)[WORDS])
 {
     if (whole) {
         memcpy(to, from, sizeof to);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < kLaneWords<T>; ++i) {
+    for (int i = 0; i < WORDS; ++i) {
         to[i] = 0;
         if constexpr (sizeof(T) == 4) {
             if (i < valid) memcpy(&to[i], from + i, 4);
@@ -187,9 +187,9 @@ __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* 
         }
         if constexpr (kTurned) {
             if (whole) load_turned(x + first, lane, turn[wave], v);
-            else load_lane(x + col, (int)(s.cols - col), false, v);
+            else load_words<T, kLaneWords<T>>(x + col, (int)(s.cols - col), false, v);
         } else {
-            load_lane(x + col, (int)(s.cols - col), whole, v);
+            load_words<T, kLaneWords<T>>(x + col, (int)(s.cols - col), whole, v);
         }
 #pragma unroll
         for (int r = 0; r < kFew; ++r) sum[r] = times<T>(v, w[r], power(byte[r]), sum[r]);
@@ -233,155 +233,232 @@ __device__ __forceinline__ void pieces_of(const uint32_t* raw, bf16x8 (&out)[kPi
     }
 }
 
-constexpr int kStep = 4 * kLaneCols;  // columns of a wavefront's step
-constexpr int kWaves = 8;             // wavefronts of a workgroup, which share the columns
-
-// A wavefront's sums: 16 * RB rows of weights and 16 * NT tokens.  The order of the summed index within a matrix instruction does not matter as long
-// as both operands have it: lane l holds 32 consecutive weights of row l % 16, and the tokens' values follow them.  OUT: T, or float where the
-// columns are cut into parts that a second launch adds (y_part values from one to the next).
-template <class T, class OUT, int NT, int RB>
-__global__ __launch_bounds__(64 * kWaves) void group_matmul_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, OUT* y)
+// Eight weights of a lane's 32.
+__device__ __forceinline__ bf16x8 weights_of(const uint4& w, int q, float unit)
 {
-    constexpr int kPieces = kPiecesOf<T>, kTiles = NT * RB;
-    __shared__ f32x4 parts[kWaves / 2][kTiles][64];
+    const uint32_t word = word_of(w, q);
+    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 1),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 3)};
+    bf16x8 a;
+    memcpy(&a, p, 16);
+    return a;
+}
+
+// Four neighbouring results of a token.
+template <class OUT>
+__device__ __forceinline__ void store_outs(OUT* row, uint32_t o, uint32_t outs, f32x4 v)
+{
+    OUT r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (OUT)v[i];
+    if (o + 4 <= outs) {
+        memcpy(row + o, r, sizeof r);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (o + i < outs) row[o + i] = r[i];
+}
+
+constexpr int kStep = 4 * kLaneCols;  // columns of a wavefront's step
+
+// Columns of a workgroup's stage, and how many stages it has in LDS: what leaves room for several workgroups on a CU.
+constexpr uint32_t stage_cols(uint32_t value_bytes, uint32_t token_tiles) { return value_bytes == 4 || token_tiles == 4 ? 128 : 256; }
+template <class T>
+constexpr int stage_buffers(int token_tiles) { return stage_cols(sizeof(T), token_tiles) * 16 * token_tiles * kPiecesOf<T> * 2 <= 20480 ? 2 : 1; }
+
+
+// Many weights: the wavefronts of a workgroup hold 16 * RB rows each and share the tokens' values, which come to LDS a stage of columns at a time, in pieces and in the order
+// of the matrix instruction's operands, while the weights and the values of the next stage are on their way.  Lane l has the columns l / 16 * STAGE / 4 ... of a stage.
+template <class T, class OUT, int NT>
+__global__ __launch_bounds__(256) void group_matmul_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, OUT* y)
+{
+    constexpr int kPieces = kPiecesOf<T>, kRb = 2, kStageCols = stage_cols(sizeof(T), NT), kLoads = kStageCols / kStep, kBuffers = stage_buffers<T>(NT);
+    constexpr int kOctets = kStageCols / 8, kMine = 16 * NT * kOctets / 256, kFragments = 4 * kLoads * NT * kPieces;
+    __shared__ uint4 operands[kBuffers][kFragments][64];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t block = blockIdx.x;
-    const uint32_t o0 = block % s.row_blocks * (16 * RB);
+    const uint32_t o0 = block % s.row_blocks * (64 * kRb) + wave * (16 * kRb);
     block /= s.row_blocks;
     const uint32_t t0 = block % s.token_blocks * (16 * NT), part = block / s.token_blocks;
     const uint32_t pitch = s.groups << s.group_log2;
-    const uint32_t mine = (lane >> 4) * kLaneCols;  // this lane's columns of a step
-    const uint32_t end = min((part + 1) * s.steps * kStep, pitch);
-    const uint8_t* w_row[RB];
-    const uint8_t* e_row[RB];
-    const T* x_row[NT];
+    const uint32_t first = part * s.steps * kStageCols, end = min(first + s.steps * kStageCols, pitch);
+    const uint32_t mine = (lane >> 4) * (kStageCols / 4);
+    const uint8_t* w_row[kRb];
+    const uint8_t* e_row[kRb];
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
+    for (int r = 0; r < kRb; ++r) {
         const uint64_t row = min(o0 + 16 * r + (lane & 15), s.outs - 1);  // (what is not there repeats the last)
         w_row[r] = codes + row * (pitch / 2);
         e_row[r] = exponents + row * s.groups;
     }
+    uint4 w[kRb][kLoads], next_w[kRb][kLoads];
+    uint32_t bytes[kRb], next_bytes[kRb];
+    const auto fetch_weights = [&](uint32_t at, uint4 (&to)[kRb][kLoads], uint32_t (&to_bytes)[kRb]) __attribute__((always_inline)) {
+        const uint32_t col = at + mine;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x_row[n] = x + min(t0 + 16 * n + (lane & 15), s.tokens - 1) * s.x_stride;
-    f32x4 sum[RB][NT] = {};
-    for (uint32_t first = (part * s.steps + wave) * kStep; first < end; first += kWaves * kStep) {
-        const uint32_t col = first + mine;
-        uint4 w[RB];
-        uint32_t byte[RB];
-        uint32_t v[NT][kLaneWords<T>];
+        for (int r = 0; r < kRb; ++r) {
+            to_bytes[r] = 0x7F7F;
 #pragma unroll
-        for (int r = 0; r < RB; ++r) w[r] = make_uint4(0, 0, 0, 0), byte[r] = 127;
-        if (col < end) {
+            for (int j = 0; j < kLoads; ++j) to[r][j] = make_uint4(0, 0, 0, 0);
+        }
+        if (col + kLoads * kLaneCols <= pitch) {
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                w[r] = *reinterpret_cast<const uint4*>(w_row[r] + col / 2);
-                byte[r] = e_row[r][col >> s.group_log2];
+            for (int r = 0; r < kRb; ++r) {
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j) to[r][j] = *reinterpret_cast<const uint4*>(w_row[r] + col / 2 + 16 * j);
+                const uint8_t* e = e_row[r] + (col >> s.group_log2);
+                if (kLoads == 2 && s.group_log2 == 5) {
+                    uint16_t both;
+                    memcpy(&both, e, 2);
+                    to_bytes[r] = both;
+                } else {
+                    to_bytes[r] = *e * 0x0101u;
+                }
+            }
+        } else if (col < pitch) {  // (the first 32 columns alone)
+#pragma unroll
+            for (int r = 0; r < kRb; ++r) {
+                to[r][0] = *reinterpret_cast<const uint4*>(w_row[r] + col / 2);
+                to_bytes[r] = e_row[r][col >> s.group_log2] | 0x7F00u;
             }
         }
+    };
+    // eight values of a token to a thread and pass
+    uint32_t v[kMine][kLaneWords<T> / 4];
+    const auto fetch_values = [&](uint32_t at) __attribute__((always_inline)) {
+        const bool whole = at + kStageCols <= s.cols;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) load_lane(x_row[n] + col, (int)(s.cols - col), first + kStep <= s.cols, v[n]);
+        for (int i = 0; i < kMine; ++i) {
+            const uint32_t n = i * 256 + threadIdx.x, token = min(t0 + n / kOctets, s.tokens - 1), col = at + n % kOctets * 8;
+            load_words<T, kLaneWords<T> / 4>(x + token * s.x_stride + col, (int)(s.cols - col), whole, v[i]);
+        }
+    };
+    // (a fragment's 64 pieces of 16 bytes lie at lane ^ its number: neighbouring octets, which go to the same lane of eight fragments, in different banks)
+    const auto bring_values = [&](uint32_t buffer) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            bf16x8 a[RB];
+        for (int i = 0; i < kMine; ++i) {
+            const uint32_t n = i * 256 + threadIdx.x, token = n / kOctets, octet = n % kOctets;
+            const uint32_t of = octet / (kOctets / 4) * 16 + token % 16, fragment = octet % (kOctets / 4);
+            bf16x8 b[kPieces];
+            pieces_of<T>(v[i], b);
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float unit = power(byte[r]);
-                const bf16x2 p[4] = {OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j, unit), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 1, unit),
-                                     OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 2, unit), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w[r], 4 * j + 3, unit)};
-                memcpy(&a[r], p, 16);
+            for (int p = 0; p < kPieces; ++p)
+                operands[buffer][(fragment * NT + token / 16) * kPieces + p][of ^ (fragment & 7)] = __builtin_bit_cast(uint4, b[p]);
+        }
+    };
+    f32x4 sum[kRb][NT] = {};
+    if (first < end) {
+        fetch_weights(first, w, bytes);
+        fetch_values(first);
+    }
+    uint32_t buffer = 0;
+    for (uint32_t at = first; at < end; at += kStageCols, buffer ^= kBuffers - 1) {
+        if (kBuffers == 1) __syncthreads();
+        bring_values(buffer);
+        if (at + kStageCols < end) {
+            fetch_weights(at + kStageCols, next_w, next_bytes);
+            fetch_values(at + kStageCols);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                bf16x8 a[kRb];
+#pragma unroll
+                for (int r = 0; r < kRb; ++r) a[r] = weights_of(w[r][j], q, power(bytes[r] >> (8 * j) & 0xFFu));
+                const int fragment = 4 * j + q;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int p = kPieces - 1; p >= 0; --p) {
+                        const bf16x8 b = __builtin_bit_cast(bf16x8, operands[buffer][(fragment * NT + n) * kPieces + p][lane ^ (fragment & 7)]);
+#pragma unroll
+                        for (int r = 0; r < kRb; ++r) sum[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r], b, sum[r][n], 0, 0, 0);
+                    }
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                bf16x8 b[kPieces];
-                pieces_of<T>(v[n] + j * (kLaneWords<T> / 4), b);
+        for (int r = 0; r < kRb; ++r) {
+            bytes[r] = next_bytes[r];
 #pragma unroll
-                for (int q = kPieces - 1; q >= 0; --q)
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) sum[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r], b[q], sum[r][n], 0, 0, 0);
-            }
+            for (int j = 0; j < kLoads; ++j) w[r][j] = next_w[r][j];
         }
     }
-    // the wavefronts' sums, in halves
-#pragma unroll
-    for (uint32_t half = kWaves / 2; half >= 1; half /= 2) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int k = 0; k < kTiles; ++k) parts[wave - half][k][lane] = sum[k / NT][k % NT];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int k = 0; k < kTiles; ++k) sum[k / NT][k % NT] += parts[wave][k][lane];
-        __syncthreads();
-    }
-    if (wave != 0) return;
     y += part * s.y_part;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t t = t0 + 16 * n + (lane & 15);
         if (t >= s.tokens) continue;
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t o = o0 + 16 * r + (lane >> 4) * 4 + i;
-                if (o < s.outs) y[t * s.y_stride + o] = (OUT)sum[r][n][i];
-            }
+        for (int r = 0; r < kRb; ++r) store_outs(y + t * s.y_stride, o0 + 16 * r + (lane >> 4) * 4, s.outs, sum[r][n]);
     }
 }
 
-// The parts of the sums, added in their order.
+// The parts of the sums, added in an order that their number alone decides: four sums to a thread, and four threads to them, which add every fourth part.
 template <class T>
-__global__ __launch_bounds__(kBlock) void add_token_parts_kernel(const float* parts, uint32_t number, uint64_t part, uint32_t outs, uint32_t blocks, T* y,
-                                                                 uint64_t y_stride)
+__global__ __launch_bounds__(kBlock) void add_token_parts_kernel(const float* parts, uint32_t number, uint32_t tokens, uint32_t outs, T* y, uint64_t y_stride)
 {
-    const uint32_t o = blockIdx.x % blocks * kBlock + threadIdx.x;
-    const uint64_t t = blockIdx.x / blocks;
-    if (o >= outs) return;
-    const float* from = parts + t * outs + o;
-    float v = *from;
-    for (uint32_t n = 1; n < number; ++n) v += from[n * part];
-    y[t * y_stride + o] = (T)v;
+    __shared__ f32x4 shared[3][64];
+    const uint32_t lane = threadIdx.x & 63, fourth = threadIdx.x >> 6, row_quads = (outs + 3) / 4, quad = blockIdx.x * 64 + lane;
+    const uint32_t t = quad / row_quads, o = quad % row_quads * 4;
+    f32x4 v = {};
+    if (t < tokens) {
+        const float* from = parts + (uint64_t)t * row_quads * 4 + o;
+        const uint64_t part = (uint64_t)tokens * row_quads * 4;
+#pragma unroll 4
+        for (uint32_t n = fourth; n < number; n += 4) v += *reinterpret_cast<const f32x4*>(from + n * part);
+    }
+    if (fourth != 0) shared[fourth - 1][lane] = v;
+    __syncthreads();
+    if (fourth != 0 || t >= tokens) return;
+#pragma unroll
+    for (int n = 0; n < 3; ++n) v += shared[n][lane];
+    store_outs(y + t * y_stride, o, outs, v);
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
 
+// How group_matmul_kernel is launched.
 struct Plan {
-    uint32_t token_tiles, row_tiles, row_blocks, token_blocks, parts, steps;
+    uint32_t token_tiles, row_blocks, token_blocks, parts, steps;
 };
 
-// How group_matmul_kernel is launched.
-Plan plan_of(size_t tokens, size_t outs, size_t cols)
+Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
 {
     Plan p;
     p.token_tiles = tokens <= 16 ? 1 : tokens <= 32 ? 2 : 4;
-    p.row_tiles = outs >= 2048 ? 4 : 1;
-    p.row_blocks = ceil_div(outs, 16 * p.row_tiles);
+    p.row_blocks = ceil_div(outs, 128);
     p.token_blocks = ceil_div(tokens, 16 * p.token_tiles);
-    const uint32_t steps = ceil_div(cols, kStep);
     const uint64_t blocks = (uint64_t)p.row_blocks * p.token_blocks;
-    const uint32_t wanted = blocks >= 256 ? 1 : (uint32_t)(256 / blocks), most = ceil_div(steps, kWaves);
-    p.parts = wanted < most ? wanted : most;
+    const uint32_t steps = ceil_div(cols, stage_cols(dtype == OGQ_FP32 ? 4 : 2, p.token_tiles));
+    // Parts of the sums (bf16 unless said): 1024 workgroups, four to a CU, where a part's sums, written and read once more, are few beside its weights.  61 tokens against
+    // 7708 x 5992: 3 parts 43.0 us, 6 30.0, 12 25.6; 64 against 4096 x 25088: 12 parts 50.3, 16 42.5, 24 38.4, 32 38.0; fp32, 64 against 4096 x 16384: 8 parts 54.9, 16
+    // 42.2, 32 44.2; 16 against 4096 x 25088: 8 parts 25.5, 16 19.2, 32 19.2; 5 in fp16 against 1000 x 4096: 12 parts 8.9, 16 6.9.
+    uint64_t most = cols / ((dtype == OGQ_FP32 ? 16 : 8) * tokens);
+    const uint64_t little = 262144 / (tokens * outs);  // (1 MB of parts costs nothing)
+    if (most < little) most = little;
+    if (most > steps) most = steps;
+    if (steps <= 4) most = 1;  // (a second launch costs more than four stages)
+    const uint64_t wanted = 1024 / blocks;
+    p.parts = (uint32_t)(wanted < most ? wanted : most);
     if (p.parts < 1) p.parts = 1;
     p.steps = ceil_div(steps, p.parts);
     return p;
 }
 
+uint64_t pitch_of(size_t outs) { return (outs + 3) / 4 * 4; }
+
 template <class T, class OUT>
 void launch_matmul(const Plan& p, const uint8_t* codes, const uint8_t* exponents, const T* x, const MatvecShape& s, OUT* y, hipStream_t st)
 {
-    const dim3 grid(p.row_blocks * p.token_blocks * p.parts), block(64 * kWaves);
-    const auto kernel = p.row_tiles == 4 ? (p.token_tiles == 1   ? group_matmul_kernel<T, OUT, 1, 4>
-                                            : p.token_tiles == 2 ? group_matmul_kernel<T, OUT, 2, 4>
-                                                                 : group_matmul_kernel<T, OUT, 4, 4>)
-                                         : (p.token_tiles == 1   ? group_matmul_kernel<T, OUT, 1, 1>
-                                            : p.token_tiles == 2 ? group_matmul_kernel<T, OUT, 2, 1>
-                                                                 : group_matmul_kernel<T, OUT, 4, 1>);
-    launch_kernel(kernel, grid, block, st, codes, exponents, x, s, y);
+    const auto kernel = p.token_tiles == 1 ? group_matmul_kernel<T, OUT, 1> : p.token_tiles == 2 ? group_matmul_kernel<T, OUT, 2> : group_matmul_kernel<T, OUT, 4>;
+    launch_kernel(kernel, dim3(p.row_blocks * p.token_blocks * p.parts), dim3(256), st, codes, exponents, x, s, y);
 }
 
 template <class T>
-void launch_of(const Groups& w, MatvecShape s, const T* x, T* y, void* workspace, hipStream_t st)
+void launch_of(const Groups& w, MatvecShape s, const T* x, uint32_t dtype, T* y, void* workspace, hipStream_t st)
 {
     const auto codes = static_cast<const uint8_t*>(w.codes);
     if (s.tokens == 1) {
@@ -390,7 +467,7 @@ void launch_of(const Groups& w, MatvecShape s, const T* x, T* y, void* workspace
         launch_kernel(group_matvec_kernel<T>, dim3(ceil_div(s.outs, kFew)), dim3(64 * waves), st, codes, w.exponents, x, s, y);
         return;
     }
-    const Plan p = plan_of(s.tokens, s.outs, s.cols);
+    const Plan p = plan_of(s.tokens, s.outs, s.cols, dtype);
     s.row_blocks = p.row_blocks, s.token_blocks = p.token_blocks, s.steps = p.steps, s.y_part = 0;
     if (p.parts == 1) {
         launch_matmul<T, T>(p, codes, w.exponents, x, s, y, st);
@@ -398,20 +475,19 @@ void launch_of(const Groups& w, MatvecShape s, const T* x, T* y, void* workspace
     }
     const uint64_t y_stride = s.y_stride;
     float* parts = static_cast<float*>(workspace);
-    s.y_stride = s.outs;
-    s.y_part = (uint64_t)s.tokens * s.outs;
+    s.y_stride = pitch_of(s.outs);
+    s.y_part = s.tokens * s.y_stride;
     launch_matmul<T, float>(p, codes, w.exponents, x, s, parts, st);
-    const uint32_t blocks = ceil_div(s.outs, kBlock);
-    launch_kernel(add_token_parts_kernel<T>, dim3(blocks * s.tokens), dim3(kBlock), st, parts, p.parts, s.y_part, s.outs, blocks, y, y_stride);
+    launch_kernel(add_token_parts_kernel<T>, dim3(ceil_div(s.y_part / 4, 64)), dim3(kBlock), st, parts, p.parts, s.tokens, s.outs, y, y_stride);
 }
 
 }  // namespace
 
-size_t group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t)
+size_t group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
 {
     if (tokens == 1) return 0;
-    const Plan p = plan_of(tokens, outs, cols);
-    return p.parts > 1 ? p.parts * tokens * outs * sizeof(float) : 0;
+    const Plan p = plan_of(tokens, outs, cols, dtype);
+    return p.parts > 1 ? p.parts * tokens * pitch_of(outs) * sizeof(float) : 0;
 }
 
 void launch_group_matvec(const Groups& w, size_t outs, size_t cols, const ogq_group_params_t* p, const Values& x, size_t tokens, uint32_t dtype,
@@ -422,9 +498,9 @@ void launch_group_matvec(const Groups& w, size_t outs, size_t cols, const ogq_gr
     s.groups = ceil_div(cols, p->group_size);
     s.group_log2 = p->group_size == 32 ? 5 : p->group_size == 64 ? 6 : 7;
     s.x_stride = x.stride, s.y_stride = y.stride;
-    if (dtype == OGQ_FP32) launch_of(w, s, static_cast<const float*>(x.data), static_cast<float*>(y.data), workspace, st);
-    else if (dtype == OGQ_BF16) launch_of(w, s, static_cast<const __bf16*>(x.data), static_cast<__bf16*>(y.data), workspace, st);
-    else launch_of(w, s, static_cast<const _Float16*>(x.data), static_cast<_Float16*>(y.data), workspace, st);
+    if (dtype == OGQ_FP32) launch_of(w, s, static_cast<const float*>(x.data), dtype, static_cast<float*>(y.data), workspace, st);
+    else if (dtype == OGQ_BF16) launch_of(w, s, static_cast<const __bf16*>(x.data), dtype, static_cast<__bf16*>(y.data), workspace, st);
+    else launch_of(w, s, static_cast<const _Float16*>(x.data), dtype, static_cast<_Float16*>(y.data), workspace, st);
 }
 
 }  // namespace ogq

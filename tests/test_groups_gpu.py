@@ -332,7 +332,10 @@ def test_weight_gradient_of_what_is_not_finite(dtype):
 
 MATVECS = [  # tokens, outs, cols, group, pad
     (1, 1, 1, 32, 0), (1, 16, 32, 32, 0), (1, 33, 1000, 64, 0), (2, 100, 4096, 128, 0), (5, 1000, 333, 32, 1), (16, 64, 130, 64, 8), (17, 250, 520, 32, 3),
-    (64, 40, 2048, 128, 0), (100, 130, 260, 64, 0), (1, 4096, 1024, 32, 0), (3, 17, 25088, 32, 0), (130, 48, 96, 32, 5), (33, 512, 4128, 32, 0)]
+    (64, 40, 2048, 128, 0), (100, 130, 260, 64, 0), (1, 4096, 1024, 32, 0), (3, 17, 25088, 32, 0), (130, 48, 96, 32, 5), (33, 512, 4128, 32, 0),
+    # many weights: stages of columns, parts of a sum, rows and columns that end inside of them
+    (2, 1100, 4128, 32, 0), (16, 4100, 1025, 64, 1), (17, 2050, 2080, 32, 3), (40, 1025, 4100, 128, 0), (64, 1024, 8192, 64, 8), (150, 3000, 1440, 32, 0),
+    (5, 129, 40000, 32, 2)]
 
 
 @pytest.mark.parametrize("tokens,outs,cols,group,pad", MATVECS)
