@@ -76,18 +76,18 @@ struct Rows16<float> {
 template <class T>
 __device__ __forceinline__ void store_codes(const uint4& codes, uint32_t byte, char* to)
 {
-    float v[8];
     uint32_t w[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        decode8(h ? make_uint2(codes.z, codes.w) : make_uint2(codes.x, codes.y), byte, v);
+    for (int h = 0; h < 4; ++h) {
+        float v[4];
+        decode8(h == 0 ? codes.x : h == 1 ? codes.y : h == 2 ? codes.z : codes.w, byte, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
             if constexpr (__is_same(T, _Float16)) {
                 const auto a = __builtin_amdgcn_cvt_pkrtz(v[2 * i], v[2 * i + 1]);
-                memcpy(&w[4 * h + i], &a, 4);
+                memcpy(&w[2 * h + i], &a, 4);
             } else {  // the upper halves, exactly
-                w[4 * h + i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
+                w[2 * h + i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
             }
         }
     }
