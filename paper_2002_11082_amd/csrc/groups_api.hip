@@ -1,10 +1,10 @@
-// libogq_groups: the C ABI declared in ogq_groups.h.  This file checks the arguments and calls the launchers (groups_common.h).
+// libogq_groups: the C ABI declared in ogq_groups.h.  This file checks the arguments and calls the launchers (groups_launch.h).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <initializer_list>
 
-#include "groups_common.h"
+#include "groups_launch.h"
 #include "ogq_groups.h"
 
 namespace ogq {

@@ -475,3 +475,12 @@ def test_captured_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(out, eager):
             assert torch.equal(a, b)
+
+
+def test_the_example_learns_and_serves():
+    from paper_2002_11082_amd import checkpointed_block
+    losses, block = checkpointed_block.train(128, 256, 128, 2, 40, tell=lambda text: say(text))
+    assert losses[-1] < 0.2 * losses[0], (losses[0], losses[-1])
+    x = torch.randn(5, 128, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    exact = block.plain(x)
+    assert float((checkpointed_block.Served(block)(x).float() - exact).norm()) < 0.4 * float(exact.norm())
