@@ -11,14 +11,13 @@ namespace ogq {
 namespace {
 
 constexpr int kDepth = 32;   // rows of a step
-constexpr int kSmall = 128;  // inputs and outputs of a workgroup's sums: weight_gradient_kernel
-constexpr int kLarge = 256;  // large_weight_gradient_kernel
+constexpr int kSmall = 128, kLarge = 256;  // inputs and outputs of a workgroup's sums
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// A row of a tile in LDS is 8 or 16 chunks of 32 bytes (16 values); chunk c of row k lies at c ^ twist(k): the eight rows that half a wavefront reads
-// at once lie in different banks.
-__device__ __forceinline__ uint32_t twist(uint32_t k) { return (k & 3u) | ((k >> 1) & 4u); }
+// A row of a tile in LDS is 8 or 16 chunks of 32 bytes (16 values); chunk c of row k lies at c ^ twist(k): what half a wavefront reads at once, two neighbouring chunks of
+// four rows, lies in different banks.
+__device__ __forceinline__ uint32_t twist(uint32_t k) { return (k & 3u) * 2u; }
 
 // Sixteen values of a row of dy in the pieces that the matrix cores take: one for 16-bit types, three for fp32.
 template <class T>
@@ -103,13 +102,6 @@ __device__ __forceinline__ s16x8 read_transposed(const char* at)
 }
 
 template <class T>
-__device__ __forceinline__ f32x4 multiply_add(s16x8 a, s16x8 b, f32x4 c)
-{
-    if constexpr (__is_same(T, _Float16)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-template <class T>
 __device__ __forceinline__ f32x16 multiply_add32(s16x8 a, s16x8 b, f32x16 c)
 {
     if constexpr (__is_same(T, _Float16)) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -120,12 +112,13 @@ struct GradientShape {
     uint32_t rows, outs, cols, groups, group_log2;
     uint32_t tiles_in, tiles_out;  // tiles along the inputs and the outputs
     uint32_t part;                 // rows of a part of the sum, a multiple of kDepth
+    bool stream;                   // whether the caches need not keep the sums
     uint64_t dy_stride, out_stride, out_part;
 };
 
 // Four neighbouring sums into a row of dw, or added to it, at once where the row has all four (the hardware takes 16 bytes at any value's address: rows of 2589 sums
 // 20.7 us and 12.8).
-__device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t cols, bool accumulate, f32x4 v)
+__device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t cols, bool accumulate, bool stream, f32x4 v)
 {
     float* p = row + at;
     if (at + 4 <= cols) {
@@ -134,7 +127,8 @@ __device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t col
             memcpy(&held, p, sizeof held);
             v += held;
         }
-        memcpy(p, &v, sizeof v);
+        if (stream) __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words*>(p));
+        else memcpy(p, &v, sizeof v);
         return;
     }
 #pragma unroll
@@ -142,131 +136,209 @@ __device__ __forceinline__ void store_sums(float* row, uint32_t at, uint32_t col
         if (at + r < cols) p[r] = accumulate ? p[r] + v[r] : v[r];
 }
 
-// What a workgroup's 256 threads bring of both factors to LDS, a step (kDepth rows) at a time: sixteen values of kUnits rows of either to a thread, on their
-// way in SETS sets of registers.
-template <class T, int TILE, int SETS>
+// What a workgroup's 256 threads bring of both factors to LDS, a step (kDepth rows) at a time: sixteen values of a row to a thread and unit, on their way in SETS sets
+// of registers.  Tiles of IN inputs and OUT outputs.
+template <class T, int IN, int OUT, int SETS>
 struct Feeder {
-    static constexpr int kUnits = TILE / 128, kUnitRows = kDepth / kUnits, kRowBytes = TILE * 2, kPlane = kDepth * kRowBytes;
-    static constexpr int kStage = (1 + Rows16<T>::kPieces) * kPlane;  // of LDS: the codes as values, then the pieces of dy
+    static constexpr int kInUnits = IN / 128, kOutUnits = OUT / 128;
+    static constexpr int kInRows = kDepth / kInUnits, kOutRows = kDepth / kOutUnits;  // of a unit
+    static constexpr int kInBytes = IN * 2, kOutBytes = OUT * 2;                      // of a row in LDS
+    static constexpr int kInPlane = kDepth * kInBytes, kOutPlane = kDepth * kOutBytes;
+    static constexpr int kStage = kInPlane + Rows16<T>::kPieces * kOutPlane;  // of LDS: the codes as values, then the pieces of dy
     const T* dy;
     const uint8_t *codes, *exponents;
     uint64_t dy_stride, pitch;
-    uint32_t groups, group_log2, first, last, row, i_mine, o_mine;
+    uint32_t groups, group_log2, first, last, in_row, out_row, i_mine, o_mine;
     uint32_t at_codes, at_byte, at_dy;
     uint32_t whole;  // steps that are there in all rows, and can be read without asking
     bool has_codes;
     int valid;
-    char* to;
-    Rows16<T> g[SETS][kUnits];
-    uint4 q[SETS][kUnits];
-    uint32_t byte[SETS][kUnits];
+    char *in_to, *out_to;
+    Rows16<T> g[SETS][kOutUnits];
+    uint4 q[SETS][kInUnits];
+    uint32_t byte[SETS][kInUnits];
 
     __device__ __forceinline__ Feeder(const T* dy_, const uint8_t* codes_, const uint8_t* exponents_, const GradientShape& s, uint32_t i0, uint32_t o0, uint32_t first_,
                                       uint32_t last_, char* lds)
         : dy(dy_), codes(codes_), exponents(exponents_), dy_stride(s.dy_stride), pitch((uint64_t)s.groups << s.group_log2), groups(s.groups),
           group_log2(s.group_log2), first(first_), last(last_)
     {
-        const uint32_t chunk = threadIdx.x % (TILE / 16);
-        row = threadIdx.x / (TILE / 16);
-        i_mine = i0 + chunk * 16, o_mine = o0 + chunk * 16;
+        const uint32_t in_chunk = threadIdx.x % (IN / 16), out_chunk = threadIdx.x % (OUT / 16);
+        in_row = threadIdx.x / (IN / 16), out_row = threadIdx.x / (OUT / 16);
+        i_mine = i0 + in_chunk * 16, o_mine = o0 + out_chunk * 16;
         has_codes = i_mine < pitch;
         valid = o_mine >= s.outs ? 0 : (int)min(16u, s.outs - o_mine);
-        to = lds + row * kRowBytes + ((chunk ^ twist(row)) * 32);  // (kUnitRows is a multiple of 16, which twist does not see)
+        // (a unit's rows are a multiple of 16, which twist does not see)
+        in_to = lds + in_row * kInBytes + ((in_chunk ^ twist(in_row)) * 32);
+        out_to = lds + kInPlane + out_row * kOutBytes + ((out_chunk ^ twist(out_row)) * 32);
         // What lies behind the last input or output is any value that is there: its sums are not stored.  A thread whose sixteen outputs reach beyond the
         // last reads on into the next row; the tensor's last rows are then left to the steps that ask.
-        const bool partial = o0 + TILE > s.outs && s.outs % 16 != 0;
+        const bool partial = o0 + OUT > s.outs && s.outs % 16 != 0;
         whole = first < last ? (last - first) / kDepth : 0;
         if (partial && whole != 0 && first + whole * kDepth == s.rows) --whole;
         // (a thread's place in a unit's rows is held in 32 bits; reading on needs a next row)
         if ((dy_stride | pitch) >= (1u << 24) || (partial && dy_stride < 16)) whole = 0;
         const uint32_t i = has_codes ? i_mine : i0, o = valid != 0 ? o_mine : o0;
-        at_codes = row * (uint32_t)pitch + i;
-        at_byte = row * groups + (i >> group_log2);
-        at_dy = row * (uint32_t)dy_stride + o;
+        at_codes = in_row * (uint32_t)pitch + i;
+        at_byte = in_row * groups + (i >> group_log2);
+        at_dy = out_row * (uint32_t)dy_stride + o;
     }
     // Of step n, of the whole ones.  (One behind the last of them is the last one again, and not used.)
     __device__ __forceinline__ void fetch_codes(uint32_t n, int set, int u)
     {
-        const uint32_t t = first + min(n, whole - 1) * kDepth + kUnitRows * u;
+        const uint32_t t = first + min(n, whole - 1) * kDepth + kInRows * u;
         q[set][u] = *reinterpret_cast<const uint4*>(codes + t * pitch + at_codes);
         byte[set][u] = (exponents + (uint64_t)t * groups)[at_byte];
     }
     __device__ __forceinline__ void fetch_dy(uint32_t n, int set, int u)
     {
-        const uint32_t t = first + min(n, whole - 1) * kDepth + kUnitRows * u;
+        const uint32_t t = first + min(n, whole - 1) * kDepth + kOutRows * u;
         g[set][u].load(dy + t * dy_stride + at_dy);
     }
-    __device__ __forceinline__ void bring_codes(uint32_t stage, int set, int u) { store_codes<T>(q[set][u], byte[set][u], to + stage * kStage + u * kUnitRows * kRowBytes); }
-    __device__ __forceinline__ void bring_dy(uint32_t stage, int set, int u) { g[set][u].store(to + stage * kStage + kPlane + u * kUnitRows * kRowBytes, kPlane); }
+    __device__ __forceinline__ void bring_codes(uint32_t stage, int set, int u) { store_codes<T>(q[set][u], byte[set][u], in_to + stage * kStage + u * kInRows * kInBytes); }
+    __device__ __forceinline__ void bring_dy(uint32_t stage, int set, int u) { g[set][u].store(out_to + stage * kStage + u * kOutRows * kOutBytes, kOutPlane); }
+    __device__ __forceinline__ void fetch(uint32_t n, int set)
+    {
+#pragma unroll
+        for (int u = 0; u < kOutUnits; ++u) fetch_dy(n, set, u);
+#pragma unroll
+        for (int u = 0; u < kInUnits; ++u) fetch_codes(n, set, u);
+    }
+    __device__ __forceinline__ void bring(uint32_t stage, int set)
+    {
+#pragma unroll
+        for (int u = 0; u < kOutUnits; ++u) bring_dy(stage, set, u);
+#pragma unroll
+        for (int u = 0; u < kInUnits; ++u) bring_codes(stage, set, u);
+    }
     // Rows t ... of any step, what is not there as 0, to the first stage.
     __device__ __forceinline__ void bring_asking(uint32_t t)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const uint32_t mine = t + row + kUnitRows * u;
+        for (int u = 0; u < kInUnits; ++u) {
+            const uint32_t mine = t + in_row + kInRows * u;
             q[0][u] = make_uint4(0, 0, 0, 0);
             byte[0][u] = 127;
             if (mine < last && has_codes) {
                 q[0][u] = *reinterpret_cast<const uint4*>(codes + mine * pitch + i_mine);
                 byte[0][u] = exponents[(uint64_t)mine * groups + (i_mine >> group_log2)];
             }
-            g[0][u].load(dy + mine * dy_stride + o_mine, mine < last ? valid : 0);
-            bring_dy(0, 0, u);
-            bring_codes(0, 0, u);
         }
+#pragma unroll
+        for (int u = 0; u < kOutUnits; ++u) {
+            const uint32_t mine = t + out_row + kOutRows * u;
+            g[0][u].load(dy + mine * dy_stride + o_mine, mine < last ? valid : 0);
+        }
+        bring(0, 0);
     }
 };
 
-// Tiles of 128 x 128 sums, 64 x 64 in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
-// next).
-template <class T>
-__global__ __launch_bounds__(256, 3) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
-                                                              float* out)
+// Where a lane finds its part of the operands of v_mfma_f32_32x32x16: lane l holds k = l / 32 * 8 ... of column l % 32.  Operand n begins at chunk first + 2 n of a row.
+template <int N, int ROW_BYTES>
+struct OperandPlaces {
+    const char* at[N];
+    __device__ __forceinline__ OperandPlaces(const char* plane, uint32_t lane, uint32_t first)
+    {
+        const uint32_t k = (lane >> 5) * 8 + ((lane >> 2) & 3), f = twist(k), side = (lane >> 4) & 1;
+#pragma unroll
+        for (int n = 0; n < N; ++n) at[n] = plane + k * ROW_BYTES + (lane & 3) * 8 + (((first + 2 * n + side) ^ f) * 32);
+    }
+    // Operand n of the upper or lower 16 rows of a step, `bytes` behind the plane that the places are in.
+    __device__ __forceinline__ s16x8 read(int n, int half, uint32_t bytes) const { return read_transposed<ROW_BYTES>(at[n] + bytes + half * 16 * ROW_BYTES); }
+};
+
+// The sums of a wavefront, 32 * NI inputs from i and 32 * NO outputs from o, to dw or the workspace.  A lane holds pieces of 16 bytes of one row; through LDS (`space`, 4608
+// bytes of the wavefront's own) eight lanes get the 128 bytes of one, so that lines are written whole.
+constexpr int kTurnRow = 144, kTurnBytes = 32 * kTurnRow;  // (16 bytes between rows: eight rows' pieces in different banks)
+
+__device__ __forceinline__ void wavefront_sync()
 {
-    constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 ? 2 : 1;
-    using Feed = Feeder<T, kSmall, kSets>;
-    __shared__ __align__(16) char lds[kSets * Feed::kStage];
-    const uint32_t tile = blockIdx.x % (s.tiles_in * s.tiles_out), part = blockIdx.x / (s.tiles_in * s.tiles_out);
-    const uint32_t i0 = tile % s.tiles_in * kSmall, o0 = tile / s.tiles_in * kSmall;
-    const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
-    f32x4 sum[4][4] = {};
-    const uint32_t k = (lane >> 4) * 8 + ((lane >> 2) & 3), f = twist(k);
-    const char* from = lds + k * Feed::kRowBytes + (lane & 3) * 8;
-    const uint32_t ci = (wave & 1) * 4, co = (wave >> 1) * 4;  // first chunk of the wavefront's sums
-    const auto products = [&](uint32_t stage) __attribute__((always_inline)) {
-        const char* at = from + stage * Feed::kStage;
-        s16x8 a[4];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int NI, int NO>
+__device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t i, uint32_t o, uint32_t lane, const GradientShape& s, bool accumulate, float* out, char* space)
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = read_transposed<Feed::kRowBytes>(at + ((ci + i) ^ f) * 32);
+    for (int b = 0; b < NO; ++b)
 #pragma unroll
-        for (int p = kPieces - 1; p >= 0; --p)
+        for (int a = 0; a < NI; ++a) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const s16x8 b = read_transposed<Feed::kRowBytes>(at + (1 + p) * Feed::kPlane + ((co + j) ^ f) * 32);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i][j] = multiply_add<T>(a[i], b, sum[i][j]);
+            for (int m = 0; m < 4; ++m) {
+                const f32x4 v = {sum[a][b][4 * m], sum[a][b][4 * m + 1], sum[a][b][4 * m + 2], sum[a][b][4 * m + 3]};
+                *reinterpret_cast<f32x4*>(space + (lane & 31) * kTurnRow + 32 * m + (lane >> 5) * 16) = v;
             }
+            wavefront_sync();
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const uint32_t row = 8 * m + (lane >> 3);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(space + row * kTurnRow + (lane & 7) * 16);
+                if (o + 32 * b + row < s.outs) store_sums(out + (o + 32 * b + row) * s.out_stride, i + 32 * a + (lane & 7) * 4, s.cols, accumulate, s.stream, v);
+            }
+            wavefront_sync();
+        }
+}
+
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
+// time.
+__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_in, uint32_t tiles_out)
+{
+    constexpr uint32_t kXcds = 8, kWide = 4;
+    const uint32_t tiles = tiles_in * tiles_out, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
+    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
+    const uint32_t panel = n / (kWide * tiles_out), rest = n % (kWide * tiles_out), width = min(kWide, tiles_in - panel * kWide);
+    return make_uint2(panel * kWide + rest % width, rest / width);
+}
+
+// Tiles of IN x OUT sums, a quarter in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
+// next).
+template <class T, int IN, int OUT, int GROUPS>
+__global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
+                                                                      float* out)
+{
+    constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
+    using Feed = Feeder<T, IN, OUT, kSets>;
+    __shared__ __align__(16) char lds[kSets * Feed::kStage];
+    const uint32_t tiles = s.tiles_in * s.tiles_out, part = blockIdx.x / tiles;
+    const uint2 tile = tile_of(blockIdx.x % tiles, s.tiles_in, s.tiles_out);
+    const uint32_t i0 = tile.x * IN, o0 = tile.y * OUT;
+    const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
+    const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * (IN / 2), o_wave = (threadIdx.x >> 7) * (OUT / 2);
+    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
+    const OperandPlaces<kIn, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
+    const OperandPlaces<kOut, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
+    f32x16 sum[kIn][kOut] = {};
+    const auto products = [&](uint32_t stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s16x8 a[kIn];
+#pragma unroll
+            for (int i = 0; i < kIn; ++i) a[i] = from_in.read(i, h, stage * Feed::kStage);
+#pragma unroll
+            for (int p = kPieces - 1; p >= 0; --p)
+#pragma unroll
+                for (int j = 0; j < kOut; ++j) {
+                    const s16x8 b = from_out.read(j, h, stage * Feed::kStage + p * Feed::kOutPlane);
+#pragma unroll
+                    for (int i = 0; i < kIn; ++i) sum[i][j] = multiply_add32<T>(a[i], b, sum[i][j]);
+                }
+        }
     };
     // 16-bit types: two steps are on their way while one is multiplied, in two stages of LDS with one barrier a step.  fp32: one of each, which leaves room for
-    // a third workgroup on a CU (4096 x 25088 sums of 256 rows: 209 us, 270 with two).
+    // more workgroups on a CU (4096 x 25088 sums of 256 rows in tiles of 128 x 128: 209 us, 270 with two).
     const auto step = [&](uint32_t n, int set) __attribute__((always_inline)) {
         if (kSets == 1) __syncthreads();
-        feed.bring_dy(set, set, 0);
-        feed.bring_codes(set, set, 0);
+        feed.bring(set, set);
         if (kSets == 1) __syncthreads();
-        feed.fetch_dy(n + kSets, set, 0);
-        feed.fetch_codes(n + kSets, set, 0);
+        feed.fetch(n + kSets, set);
         if (kSets == 2) __syncthreads();
         products(set);
     };
     if (feed.whole != 0) {
 #pragma unroll
-        for (int n = 0; n < kSets; ++n) {
-            feed.fetch_dy(n, n, 0);
-            feed.fetch_codes(n, n, 0);
-        }
+        for (int n = 0; n < kSets; ++n) feed.fetch(n, n);
         uint32_t n = 0;
         for (; n + kSets <= feed.whole; n += kSets) {
             step(n, 0);
@@ -280,28 +352,8 @@ __global__ __launch_bounds__(256, 3) void weight_gradient_kernel(const T* dy, co
         __syncthreads();
         products(0);
     }
-    out += part * s.out_part;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t o = o0 + (co + j) * 16 + (lane & 15);
-        if (o >= s.outs) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t at = i0 + (ci + i) * 16 + (lane >> 4) * 4;
-            store_sums(out + o * s.out_stride, at, s.cols, accumulate, sum[i][j]);
-        }
-    }
-}
-
-// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
-// time.
-__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_in, uint32_t tiles_out)
-{
-    constexpr uint32_t kXcds = 8, kWide = 4;
-    const uint32_t tiles = tiles_in * tiles_out, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
-    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
-    const uint32_t panel = n / (kWide * tiles_out), rest = n % (kWide * tiles_out), width = min(kWide, tiles_in - panel * kWide);
-    return make_uint2(panel * kWide + rest % width, rest / width);
+    __syncthreads();
+    store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, lds + (threadIdx.x >> 6) * kTurnBytes);
 }
 
 // The order of instructions around eight products, which the matrix core takes 32 cycles for each: behind each of them, reads of operands, a few vector
@@ -331,29 +383,21 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
                                                                        bool accumulate, float* out)
 {
     static_assert(Rows16<T>::kPieces == 1);
-    using Feed = Feeder<T, kLarge, 2>;
-    constexpr int kRowBytes = Feed::kRowBytes, kPlane = Feed::kPlane, kStage = Feed::kStage;
-    __shared__ __align__(16) char lds[2 * kStage];
+    using Feed = Feeder<T, kLarge, kLarge, 2>;
+    __shared__ __align__(16) char lds[2 * Feed::kStage];
     const uint32_t tiles = s.tiles_in * s.tiles_out, part = blockIdx.x / tiles;
     const uint2 tile = tile_of(blockIdx.x % tiles, s.tiles_in, s.tiles_out);
     const uint32_t i0 = tile.x * kLarge, o0 = tile.y * kLarge;
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * 128, o_wave = (threadIdx.x >> 7) * 128;
     Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
-    // operands of v_mfma_f32_32x32x16: lane l holds k = l / 32 * 8 ... of column l % 32
-    const uint32_t k = (lane >> 5) * 8 + ((lane >> 2) & 3), f = twist(k), side = (lane >> 4) & 1;
-    const uint32_t ci = (wave & 1) * 8, co = (wave >> 1) * 8;  // first chunk of the wavefront's sums
-    const char *from_in[4], *from_out[4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        from_in[n] = lds + k * kRowBytes + (lane & 3) * 8 + (((ci + 2 * n + side) ^ f) * 32);
-        from_out[n] = lds + k * kRowBytes + (lane & 3) * 8 + (((co + 2 * n + side) ^ f) * 32);
-    }
+    const OperandPlaces<4, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
+    const OperandPlaces<4, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
     using Operands = s16x8[4][2];
-    // Operand n of a factor, and all of one.
-    const auto read = [&](Operands& r, const char* const (&at)[4], uint32_t stage, int plane, int n) __attribute__((always_inline)) {
+    // Operand n of a factor.
+    const auto read = [&](Operands& r, const auto& from, uint32_t stage, int n) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) r[n][h] = read_transposed<kRowBytes>(at[n] + stage * kStage + plane * kPlane + h * 16 * kRowBytes);
+        for (int h = 0; h < 2; ++h) r[n][h] = from.read(n, h, stage * Feed::kStage);
     };
     f32x16 sum[4][4] = {};
     // An eighth of a step's products.
@@ -366,7 +410,7 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
     // step n + 4 sets off.
     const auto step = [&](uint32_t n, uint32_t here, Operands& in, Operands& o, Operands& next_in, Operands& next_o) __attribute__((always_inline)) {
         const uint32_t next = here ^ 1;
-        read(next_in, from_in, next, 0, 0), read(next_o, from_out, next, 1, 0), read(next_o, from_out, next, 1, 1);
+        read(next_in, from_in, next, 0), read(next_o, from_out, next, 0), read(next_o, from_out, next, 1);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             feed.bring_dy(here, here, u);
@@ -374,12 +418,12 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
         }
         products(in, o, 0), products(in, o, 1);
         interleave<12, 2, 4>();
-        read(next_o, from_out, next, 1, 2), read(next_o, from_out, next, 1, 3), read(next_in, from_in, next, 0, 1);
+        read(next_o, from_out, next, 2), read(next_o, from_out, next, 3), read(next_in, from_in, next, 1);
         feed.bring_codes(here, here, 0);
         feed.fetch_codes(n + 4, here, 0);
         products(in, o, 2), products(in, o, 3);
         interleave<12, 6, 2>();
-        read(next_in, from_in, next, 0, 2), read(next_in, from_in, next, 0, 3);
+        read(next_in, from_in, next, 2), read(next_in, from_in, next, 3);
         feed.bring_codes(here, here, 1);
         feed.fetch_codes(n + 4, here, 1);
         products(in, o, 4), products(in, o, 5);
@@ -412,7 +456,7 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
             }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) read(a, from_in, 0, 0, k), read(b, from_out, 0, 1, k);
+        for (int k = 0; k < 4; ++k) read(a, from_in, 0, k), read(b, from_out, 0, k);
         __syncthreads();
         uint32_t n = 0;
         for (; n + 2 <= feed.whole; n += 2) {
@@ -425,24 +469,13 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
         feed.bring_asking(t);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) read(a, from_in, 0, 0, k), read(b, from_out, 0, 1, k);
+        for (int k = 0; k < 4; ++k) read(a, from_in, 0, k), read(b, from_out, 0, k);
 #pragma unroll
         for (int eighth = 0; eighth < 8; ++eighth) products(a, b, eighth);
         __syncthreads();
     }
-    out += part * s.out_part;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t o = o0 + (co + 2 * j) * 16 + (lane & 31);
-        if (o >= s.outs) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const f32x4 v = {sum[i][j][4 * m], sum[i][j][4 * m + 1], sum[i][j][4 * m + 2], sum[i][j][4 * m + 3]};
-                store_sums(out + o * s.out_stride, i0 + (ci + 2 * i) * 16 + 8 * m + (lane >> 5) * 4, s.cols, accumulate, v);
-            }
-    }
+    __syncthreads();
+    store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, lds + (threadIdx.x >> 6) * kTurnBytes);
 }
 
 // The parts of the sums, added in an order that their number alone decides.  Four sums to a thread, and four threads to them: each adds every fourth part.
@@ -463,30 +496,40 @@ __global__ __launch_bounds__(kBlock) void add_parts_kernel(const f32x4* parts, u
 #pragma unroll
     for (int n = 0; n < 3; ++n) v += shared[n][lane];
     const uint32_t o = quad / row_quads, at = quad % row_quads * 4;
-    store_sums(dw + o * dw_stride, at, cols, accumulate, v);
+    store_sums(dw + o * dw_stride, at, cols, accumulate, false, v);
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-// Which kernel, and into how many parts a sum is cut.
-// The larger tiles where they fill most of the chip and a tile's own costs (its first steps, 256 KB of sums to store) are spread over 384 rows: 4096 x 4096 sums of 256
-// rows 26.2 us and 25.7 with the smaller ones, of 512 33.0 and 38.6, of 2048 76 and 113; not for fp32, whose three pieces want 128 KB of LDS (4096 rows: 757 us and 456).
+// Which tiles, and into how many parts a sum is cut.
+// 16-bit types: 256 x 256 where such tiles fill most of the chip and a tile's own costs (its first steps, 256 KB of sums to store, with one workgroup on a CU) are
+// spread over 640 rows: 4096 x 4096 sums of 512 rows 27.9 us and 28.6 with 128 x 128, of 768 34.6 and 38.3, of 2048 68 and 86; 8192 x 8192 of 512 rows 114 and 99, of
+// 1024 167 and 195; 2560 x 4096 (160 tiles) of 4096 rows 100 and 115, 2048 x 4096 (128) of 2048 rows 58 and 47.  256 x 128: not better than 128 x 128 anywhere.
+// fp32: 256 x 128 where such tiles fill the chip, because LDS holds three pieces of dy beside one of the inputs: 4096 x 4096 of 2048 rows 176 us and 256 with 128 x
+// 128, 4096 x 25088 of 256 rows 194 and 225; 1024 x 1024 (32 tiles) of 8192 rows in the best parts 68 and 79, 1000 x 4096 (128) of 1000 rows 47 and 49, 512 x 512 of
+// 1024 rows 20 and 19.
 // A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a step of 32 rows takes about 1 us in fp32 and 0.45 in 16 bits.  As many parts as make the two
 // equal, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us: 200 x 333 sums of 16385 rows in fp16 (35 parts by this) in 16 parts
 // 23.2 us, 32 18.6, 65 19.4, 128 23.6; 1024 x 1024 in bf16 (6) of 8192 rows in 4 parts 39.7, 8 38.1, 16 47.2; of 2048 rows (3) in 2 parts 22.8, 4 18.7, 8 22.0; 2048 x
 // 2048 of 8192 rows (2) in one part 113, 2 102, 4 103; 512 x 512 of 512 rows in one part 10.2, 2 10.4.
 struct Plan {
-    uint32_t tile, tiles_in, tiles_out, parts, part;
+    uint32_t tile_in, tile_out, tiles_in, tiles_out, parts, part;
 };
 
 Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
 {
+    const auto tiles_of = [&](uint32_t in, uint32_t out) { return (uint64_t)ceil_div(cols, in) * ceil_div(outs, out); };
     Plan p;
-    p.tile = (uint64_t)ceil_div(outs, kLarge) * ceil_div(cols, kLarge) >= 192 && dtype != OGQ_FP32 && rows >= 384 ? kLarge : kSmall;
-    p.tiles_in = ceil_div(cols, p.tile), p.tiles_out = ceil_div(outs, p.tile);
-    const uint64_t tiles = (uint64_t)p.tiles_in * p.tiles_out;
+    p.tile_in = p.tile_out = kSmall;
+    if (dtype == OGQ_FP32) {
+        if (tiles_of(kLarge, kSmall) >= 256) p.tile_in = kLarge;
+    } else if (tiles_of(kLarge, kLarge) >= 160 && rows >= 640) {
+        p.tile_in = p.tile_out = kLarge;
+    }
+    p.tiles_in = ceil_div(cols, p.tile_in), p.tiles_out = ceil_div(outs, p.tile_out);
+    const uint64_t tiles = tiles_of(p.tile_in, p.tile_out);
     p.parts = 1;
-    if (p.tile == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 192 : 512)) {
+    if (p.tile_in == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 192 : 512)) {
         const uint64_t squared = (uint64_t)rows * (dtype == OGQ_FP32 ? 12000 : 5000) / (outs * cols);
         const uint64_t most = rows / 64 < 512 / tiles ? rows / 64 : 512 / tiles;
         while (p.parts < most && (uint64_t)(p.parts + 1) * (p.parts + 1) <= squared) ++p.parts;
@@ -519,14 +562,18 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     s.out_stride = parts > 1 ? pitch_of(cols) : dw_stride;
     s.out_part = parts > 1 ? outs * s.out_stride : 0;
     float* out = parts > 1 ? static_cast<float*>(workspace) : dw;
+    // (32 MB of sums, more than the caches of the eight XCDs: 4096 x 25088 of 256 rows in bf16 136 us and 92 past them, in fp32 202 and 194)
+    s.stream = parts == 1 && outs * cols >= ((size_t)8 << 20);
     const bool add = accumulate && parts == 1;
     const dim3 grid(s.tiles_in * s.tiles_out * parts), block(256);
     const auto codes = static_cast<const uint8_t*>(x.codes);
     const auto go = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        void (*kernel)(const T*, const uint8_t*, const uint8_t*, GradientShape, bool, float*) = weight_gradient_kernel<T>;
-        if constexpr (sizeof(T) == 2)
-            if (plan.tile == kLarge) kernel = large_weight_gradient_kernel<T>;
+        auto kernel = weight_gradient_kernel<T, kSmall, kSmall, 3>;
+        if (plan.tile_in == kLarge) {
+            if constexpr (sizeof(T) == 4) kernel = weight_gradient_kernel<T, kLarge, kSmall, 2>;
+            else kernel = large_weight_gradient_kernel<T>;
+        }
         launch_kernel(kernel, grid, block, st, static_cast<const T*>(dy.data), codes, x.exponents, s, add, out);
     };
     if (dtype == OGQ_FP32) go((float*)nullptr);
