@@ -281,17 +281,6 @@ __device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t
         }
 }
 
-// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
-// time.
-__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_in, uint32_t tiles_out)
-{
-    constexpr uint32_t kXcds = 8, kWide = 4;
-    const uint32_t tiles = tiles_in * tiles_out, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
-    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
-    const uint32_t panel = n / (kWide * tiles_out), rest = n % (kWide * tiles_out), width = min(kWide, tiles_in - panel * kWide);
-    return make_uint2(panel * kWide + rest % width, rest / width);
-}
-
 // Tiles of IN x OUT sums, a quarter in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
 // next).
 template <class T, int IN, int OUT, int GROUPS>
@@ -301,9 +290,8 @@ __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* d
     constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
     using Feed = Feeder<T, IN, OUT, kSets>;
     __shared__ __align__(16) char lds[kSets * Feed::kStage];
-    const uint32_t tiles = s.tiles_in * s.tiles_out, part = blockIdx.x / tiles;
-    const uint2 tile = tile_of(blockIdx.x % tiles, s.tiles_in, s.tiles_out);
-    const uint32_t i0 = tile.x * IN, o0 = tile.y * OUT;
+    const uint32_t tiles = s.tiles_in * s.tiles_out, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
+    const uint32_t i0 = tile % s.tiles_in * IN, o0 = tile / s.tiles_in * OUT;  // (neighbours along a row of sums: 8192 x 16384 of 32 rows 97 us, 131 in tile_of's order)
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
     const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * (IN / 2), o_wave = (threadIdx.x >> 7) * (OUT / 2);
     Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
@@ -354,6 +342,17 @@ __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* d
     }
     __syncthreads();
     store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, lds + (threadIdx.x >> 6) * kTurnBytes);
+}
+
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
+// time.
+__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_in, uint32_t tiles_out)
+{
+    constexpr uint32_t kXcds = 8, kWide = 4;
+    const uint32_t tiles = tiles_in * tiles_out, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
+    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
+    const uint32_t panel = n / (kWide * tiles_out), rest = n % (kWide * tiles_out), width = min(kWide, tiles_in - panel * kWide);
+    return make_uint2(panel * kWide + rest % width, rest / width);
 }
 
 // The order of instructions around eight products, which the matrix core takes 32 cycles for each: behind each of them, reads of operands, a few vector
@@ -562,8 +561,9 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     s.out_stride = parts > 1 ? pitch_of(cols) : dw_stride;
     s.out_part = parts > 1 ? outs * s.out_stride : 0;
     float* out = parts > 1 ? static_cast<float*>(workspace) : dw;
-    // (32 MB of sums, more than the caches of the eight XCDs: 4096 x 25088 of 256 rows in bf16 136 us and 92 past them, in fp32 202 and 194)
-    s.stream = parts == 1 && outs * cols >= ((size_t)8 << 20);
+    // Past the caches: 32 MB of sums, more than those of the eight XCDs hold, in rows of whole lines (4096 x 25088 of 256 rows in bf16 136 us and 92 past them, in fp32
+    // 202 and 194; but 2700 x 6890, whose lines two rows share, of 9 rows 48.4 and 18.9 through them).
+    s.stream = parts == 1 && outs * cols >= ((size_t)8 << 20) && ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 63) == 0;
     const bool add = accumulate && parts == 1;
     const dim3 grid(s.tiles_in * s.tiles_out * parts), block(256);
     const auto codes = static_cast<const uint8_t*>(x.codes);
