@@ -37,6 +37,28 @@ struct ExponentLimits {
     static constexpr int kHigh = BITS == 8 ? (kHalf ? 9 : 121) : (kHalf ? 13 : 125);
 };
 
+// N consecutive values as they are in memory, N * sizeof(T) / 4 words, of which only the first `valid` are there: the others are 0.  Every load is one of a value that
+// is there, so that none waits for another's turn.
+template <class T, int N>
+__device__ __forceinline__ void load_some(const T* from, int valid, uint32_t (&to)[N * sizeof(T) / 4])
+{
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 4); ++i) to[i] = 0;
+    if (valid <= 0) return;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) memcpy(&to[i], from + min(i, valid - 1), 4);
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = i < valid ? to[i] : 0u;
+    } else {
+        uint16_t v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) memcpy(&v[i], from + min(i, valid - 1), 2);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) to[i] = (2 * i < valid ? v[2 * i] : 0u) | (2 * i + 1 < valid ? (uint32_t)v[2 * i + 1] << 16 : 0u);
+    }
+}
+
 // A lane's piece of a row: 16 bytes of values, so that a wavefront reads and writes 1 KB without a gap.
 template <class T>
 constexpr int kPiece = 16 / sizeof(T);
@@ -54,8 +76,9 @@ __device__ __forceinline__ void load_piece(const T* from, int valid, float (&v)[
         const uint4 w = __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load(words) : *words);
         memcpy(raw, &w, 16);
     } else {
-#pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) raw[i] = i < valid ? from[i] : (T)0.0f;
+        uint32_t words[4];
+        load_some<T, kPiece<T>>(from, valid, words);
+        memcpy(raw, words, 16);
     }
 #pragma unroll
     for (int i = 0; i < kPiece<T>; ++i) v[i] = (float)raw[i];

@@ -27,33 +27,20 @@ struct Rows16 {
     __device__ __forceinline__ void load(const T* from) { memcpy(raw, from, 32); }
     __device__ __forceinline__ void load(const T* from, int valid)
     {
-        if (valid >= 16) {
-            load(from);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint16_t low = 0, high = 0;
-            if (2 * i < valid) memcpy(&low, from + 2 * i, 2);
-            if (2 * i + 1 < valid) memcpy(&high, from + 2 * i + 1, 2);
-            raw[i] = low | (uint32_t)high << 16;
-        }
+        if (valid >= 16) load(from);
+        else load_some<T, 16>(from, valid, raw);
     }
     __device__ __forceinline__ void store(char* to, int) const { memcpy(to, raw, 32); }
 };
 template <>
 struct Rows16<float> {
     static constexpr int kPieces = 3;
-    float raw[16];
+    uint32_t raw[16];
     __device__ __forceinline__ void load(const float* from) { memcpy(raw, from, 64); }
     __device__ __forceinline__ void load(const float* from, int valid)
     {
-        if (valid >= 16) {
-            load(from);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) raw[i] = i < valid ? from[i] : 0.0f;
-        }
+        if (valid >= 16) load(from);
+        else load_some<float, 16>(from, valid, raw);
     }
     __device__ __forceinline__ void store(char* to, int plane) const
     {
@@ -61,8 +48,8 @@ struct Rows16<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t a[3], b[3];
-            split3(raw[2 * i], a[0], a[1], a[2]);
-            split3(raw[2 * i + 1], b[0], b[1], b[2]);
+            split3(__uint_as_float(raw[2 * i]), a[0], a[1], a[2]);
+            split3(__uint_as_float(raw[2 * i + 1]), b[0], b[1], b[2]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) w[p][i] = __builtin_amdgcn_perm(b[p], a[p], 0x07060302u);
         }

@@ -80,25 +80,11 @@ __device__ __forceinline__ uint32_t sum_over_lanes(float* v, uint32_t lane)
 template <class T>
 constexpr int kLaneWords = kLaneCols * sizeof(T) / 4;
 
-template <class T, int WORDS>
-__device__ __forceinline__ void load_words(const T* from, int valid, bool whole, uint32_t (&to)[WORDS])
+template <class T, int N>
+__device__ __forceinline__ void load_values(const T* from, int valid, bool whole, uint32_t (&to)[N * sizeof(T) / 4])
 {
-    if (whole) {
-        memcpy(to, from, sizeof to);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-        to[i] = 0;
-        if constexpr (sizeof(T) == 4) {
-            if (i < valid) memcpy(&to[i], from + i, 4);
-        } else {
-            uint16_t low = 0, high = 0;
-            if (2 * i < valid) memcpy(&low, from + 2 * i, 2);
-            if (2 * i + 1 < valid) memcpy(&high, from + 2 * i + 1, 2);
-            to[i] = low | ((uint32_t)high << 16);
-        }
-    }
+    if (whole || valid >= N) memcpy(to, from, sizeof to);
+    else load_some<T, N>(from, valid, to);
 }
 
 // The same of 64 lanes' values that are all there: in the order of memory, 1 KB at once, and through LDS to the lane that wants them (a lane's own
@@ -187,9 +173,9 @@ __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* 
         }
         if constexpr (kTurned) {
             if (whole) load_turned(x + first, lane, turn[wave], v);
-            else load_words<T, kLaneWords<T>>(x + col, (int)(s.cols - col), false, v);
+            else load_values<T, kLaneCols>(x + col, (int)(s.cols - col), false, v);
         } else {
-            load_words<T, kLaneWords<T>>(x + col, (int)(s.cols - col), whole, v);
+            load_values<T, kLaneCols>(x + col, (int)(s.cols - col), whole, v);
         }
 #pragma unroll
         for (int r = 0; r < kFew; ++r) sum[r] = times<T>(v, w[r], power(byte[r]), sum[r]);
@@ -331,7 +317,7 @@ __global__ __launch_bounds__(256) void group_matmul_kernel(const uint8_t* codes,
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const uint32_t n = i * 256 + threadIdx.x, token = min(t0 + n / kOctets, s.tokens - 1), col = at + n % kOctets * 8;
-            load_words<T, kLaneWords<T> / 4>(x + token * s.x_stride + col, (int)(s.cols - col), whole, v[i]);
+            load_values<T, 8>(x + token * s.x_stride + col, (int)(s.cols - col), whole, v[i]);
         }
     };
     // (a fragment's 64 pieces of 16 bytes lie at lane ^ its number: neighbouring octets, which go to the same lane of eight fragments, in different banks)
