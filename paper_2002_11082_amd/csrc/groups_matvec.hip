@@ -1,7 +1,7 @@
 // libogq_groups: tokens times the transpose of weights held in 4 bits,
 //   y[t][o] = sum over i of x[t][i] * w^[o][i].
 //
-// group_matvec_kernel (one token) on the vector unit, group_matmul_kernel (more) on the matrix cores.  Both read 32 weights (16 bytes) per lane and
+// group_matvec_kernel (a few tokens) on the vector unit, group_matmul_kernel (more) on the matrix cores.  Both read 32 weights (16 bytes) per lane and
 // turn eight of them into bf16 with four conversions, which take the group's power along.
 #include "groups_common.h"
 
@@ -17,6 +17,7 @@ constexpr int kLaneCols = 32;  // weights of a lane's load: within one group
 struct MatvecShape {
     uint32_t tokens, outs, cols, groups, group_log2, row_blocks, token_blocks;
     uint32_t steps;  // of a wavefront: chunks of columns, or of a part of the sum
+    uint32_t team;   // wavefronts that share the columns of a row
     uint64_t x_stride, y_stride, y_part;
 };
 
@@ -87,19 +88,23 @@ __device__ __forceinline__ void load_values(const T* from, int valid, bool whole
     else load_some<T, N>(from, valid, to);
 }
 
-// The same of 64 lanes' values that are all there: in the order of memory, 1 KB at once, and through LDS to the lane that wants them (a lane's own
-// 32 values lie 64 or 128 bytes from its neighbour's, four times as many trips to the cache).  Sixteen bytes p of lane l lie at p ^ (l / 2 or l).
+// The same of 64 lanes' values: in the order of memory, 1 KB at once, and through LDS to the lane that wants them (a lane's own 32 values lie 64 or
+// 128 bytes from its neighbour's, four times as many trips to the cache).  Sixteen bytes p of lane l lie at p ^ (l / 2 or l).
 template <class T>
-__device__ __forceinline__ void load_turned(const T* from, uint32_t lane, uint4* turn, uint32_t (&to)[kLaneWords<T>])
+__device__ __forceinline__ void load_turned(const T* from, int valid, bool whole, uint32_t lane, uint4* turn, uint32_t (&to)[kLaneWords<T>])
 {
     constexpr uint32_t kQuads = kLaneWords<T> / 4, kShift = kQuads == 4 ? 1 : 0;
-    uint4 q[kQuads];
+    constexpr int kQuad = 16 / sizeof(T);
+    uint32_t q[kQuads][4];
 #pragma unroll
-    for (uint32_t i = 0; i < kQuads; ++i) memcpy(&q[i], from + (i * 64 + lane) * (16 / sizeof(T)), 16);
+    for (uint32_t i = 0; i < kQuads; ++i) {
+        const int at = (int)(i * 64 + lane) * kQuad;
+        load_values<T, kQuad>(from + at, valid - at, whole, q[i]);
+    }
 #pragma unroll
     for (uint32_t i = 0; i < kQuads; ++i) {
         const uint32_t n = i * 64 + lane, of = n / kQuads;
-        turn[of * kQuads + ((n ^ (of >> kShift)) & (kQuads - 1))] = q[i];
+        turn[of * kQuads + ((n ^ (of >> kShift)) & (kQuads - 1))] = make_uint4(q[i][0], q[i][1], q[i][2], q[i][3]);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -114,53 +119,61 @@ __device__ __forceinline__ void load_turned(const T* from, uint32_t lane, uint4*
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Their products with 32 weights, added to a sum.
-template <class T>
-__device__ __forceinline__ float times(const uint32_t (&x)[kLaneWords<T>], const uint4& w, float unit, float sum)
+// The products of 32 weights with every token's values, added to the tokens' sums.
+template <class T, int NT>
+__device__ __forceinline__ void add_products(const uint32_t (&x)[NT][kLaneWords<T>], const uint4& w, float unit, float* sum)
 {
     if constexpr (__is_same(T, __bf16)) {
 #pragma unroll
-        for (int n = 0; n < 16; ++n)
-            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x[n]), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w, n, unit), sum, false);
-        return sum;
+        for (int n = 0; n < 16; ++n) {
+            const bf16x2 q = OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4, w, n, unit);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sum[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x[t][n]), q, sum[t], false);
+        }
     } else if constexpr (__is_same(T, _Float16)) {
         // (a weight times its group's power may be outside of fp16: the power comes in behind the sum)
-        float part = 0.0f;
+        float part[NT] = {};
 #pragma unroll
-        for (int n = 0; n < 16; ++n)
-            part = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x[n]), OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4, w, n, 1.0f), part, false);
-        return __builtin_fmaf(part, unit, sum);
+        for (int n = 0; n < 16; ++n) {
+            const f16x2 q = OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4, w, n, 1.0f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) part[t] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x[t][n]), q, part[t], false);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[t] = __builtin_fmaf(part[t], unit, sum[t]);
     } else {
 #pragma unroll
         for (int n = 0; n < 16; ++n) {
             const f32x2 q = OGQ_PAIR(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4, w, n, unit);
-            sum = __builtin_fmaf(q[1], __uint_as_float(x[2 * n + 1]), __builtin_fmaf(q[0], __uint_as_float(x[2 * n]), sum));
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                sum[t] = __builtin_fmaf(q[1], __uint_as_float(x[t][2 * n + 1]), __builtin_fmaf(q[0], __uint_as_float(x[t][2 * n]), sum[t]));
         }
-        return sum;
     }
 }
 
 constexpr int kFew = 4;  // rows of weights of a wavefront, and most wavefronts of a workgroup
 
-// One token: a lane keeps 32 of its values and multiplies them with the same columns of four rows of weights, whose loads are all under way at
-// once, 1 KB of a row in a piece.  The wavefronts of a workgroup share the columns.  Bound by memory behind 3 us of latency: 4096 x 25088 weights
-// 13.8 us.  (Eight rows 14.1, sixteen 16.2, two 18.1; eight wavefronts 16.7; with the next piece's loads ahead of the products 14.3.)
-template <class T>
+// A few tokens: a lane keeps 32 of the values of each and multiplies them with the same columns of four rows of weights, whose loads are all under way at
+// once, 1 KB of a row in a piece.  The wavefronts of a team share the columns of its rows; a workgroup has up to four wavefronts, in one team or several.
+// Bound by memory behind 3 us of latency: one token in bf16 against 4096 x 25088 weights 11.0 us, 5.0 TB/s.  (Eight rows 14.1, sixteen 16.2, two 18.1 where four
+// took 13.8; eight wavefronts 16.7; with the next piece's loads ahead of the products 14.3.)
+// Values straight from memory or through LDS: one token in bf16 11.0 and 11.3 us, two 23.5 and 15.3, four against 4096 x 4096 8.8 and 5.6; one in fp32 15.6 and 15.0.
+template <class T, int NT>
 __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* codes, const uint8_t* exponents, const T* x, MatvecShape s, T* y)
 {
-    // fp32: through LDS (15.6 -> 15.0 us); 16-bit types straight (15.5 through LDS)
-    constexpr bool kTurned = sizeof(T) == 4;
-    __shared__ float parts[kFew][kFew];
+    constexpr bool kTurned = sizeof(T) == 4 || NT > 1;
+    __shared__ float parts[kFew][kFew * NT];
     __shared__ uint4 turn[kTurned ? kFew : 1][kTurned ? 64 * kLaneWords<T> / 4 : 1];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const uint32_t o0 = blockIdx.x * kFew;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), teams = blockDim.x / (64 * s.team);
+    const uint32_t o0 = (blockIdx.x * teams + wave / s.team) * kFew;
     const uint32_t pitch = s.groups << s.group_log2;
-    float sum[kFew] = {};
-    for (uint32_t chunk = wave; chunk < s.steps; chunk += waves) {
+    float sum[kFew * NT] = {};
+    for (uint32_t chunk = wave % s.team; chunk < s.steps; chunk += s.team) {
         const uint32_t first = chunk * (64 * kLaneCols), col = first + lane * kLaneCols;
         const bool whole = first + 64 * kLaneCols <= s.cols;
         uint4 w[kFew];
-        uint32_t byte[kFew], v[kLaneWords<T>];
+        uint32_t byte[kFew], v[NT][kLaneWords<T>];
 #pragma unroll
         for (int r = 0; r < kFew; ++r) w[r] = make_uint4(0, 0, 0, 0), byte[r] = 127;
         if (col < pitch) {
@@ -171,22 +184,30 @@ __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* 
                 byte[r] = exponents[row * s.groups + (col >> s.group_log2)];
             }
         }
-        if constexpr (kTurned) {
-            if (whole) load_turned(x + first, lane, turn[wave], v);
-            else load_values<T, kLaneCols>(x + col, (int)(s.cols - col), false, v);
-        } else {
-            load_values<T, kLaneCols>(x + col, (int)(s.cols - col), whole, v);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const T* of = x + min((uint32_t)t, s.tokens - 1) * s.x_stride;
+            if constexpr (kTurned) {
+                // (fp32: a check per piece costs registers, two tokens against 4096 x 25088 30.8 us for 24.5)
+                if (sizeof(T) == 2) load_turned(of + first, (int)(s.cols - first), whole, lane, turn[wave], v[t]);
+                else if (whole) load_turned(of + first, 0, true, lane, turn[wave], v[t]);
+                else load_values<T, kLaneCols>(of + col, (int)(s.cols - col), false, v[t]);
+            } else {
+                load_values<T, kLaneCols>(of + col, (int)(s.cols - col), whole, v[t]);
+            }
         }
 #pragma unroll
-        for (int r = 0; r < kFew; ++r) sum[r] = times<T>(v, w[r], power(byte[r]), sum[r]);
+        for (int r = 0; r < kFew; ++r) add_products<T, NT>(v, w[r], power(byte[r]), sum + r * NT);
     }
-    const uint32_t index = sum_over_lanes<kFew>(sum, lane);
+    const uint32_t index = sum_over_lanes<kFew * NT>(sum, lane);
     parts[wave][index] = sum[0];  // (several lanes write the same)
     __syncthreads();
-    if (threadIdx.x < kFew && o0 + threadIdx.x < s.outs) {
-        float all = parts[0][threadIdx.x];
-        for (uint32_t k = 1; k < waves; ++k) all += parts[k][threadIdx.x];
-        y[o0 + threadIdx.x] = (T)all;
+    if (threadIdx.x < teams * kFew * NT) {
+        const uint32_t r = threadIdx.x / NT, t = threadIdx.x % NT, o = blockIdx.x * teams * kFew + r, first = r / kFew * s.team, at = threadIdx.x % (kFew * NT);
+        if (o >= s.outs || t >= s.tokens) return;
+        float all = parts[first][at];
+        for (uint32_t k = 1; k < s.team; ++k) all += parts[first + k][at];
+        y[t * s.y_stride + o] = (T)all;
     }
 }
 
@@ -406,6 +427,18 @@ __global__ __launch_bounds__(kBlock) void add_token_parts_kernel(const float* pa
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
 
+// Which calls group_matvec_kernel takes: one launch for two, while what it reads of the tokens, once for four rows of weights, does not yet cost more.  Its us and the two launches'
+// together.  Two tokens in bf16: 4096 x 25088 15.3 and 18.4, 4096 x 4096 4.4 and 7.4, 16384 x 1024 5.8 and 8.0, 2048 x 1024 4.0 and 7.3, 16384 x 500 6.4 and 5.2.  Four: 4096 x 4096 5.6
+// and 7.6, 8192 x 1024 5.5 and 7.5, 8192 x 2816 9.7 and 9.0, 16384 x 1024 8.6 and 8.0, 4096 x 25088 26.4 and 18.4.  Two in fp32: 4096 x 16384 16.1 and 19.5, 4096 x 4096 6.0 and 9.1,
+// 8192 x 1024 7.2 and 7.4, 4096 x 25088 24.5 and 23.6, 16384 x 1024 11.2 and 9.0; four: 4096 x 4096 8.6 and 9.4, 8192 x 1024 13.0 and 7.4.
+bool few_tokens(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
+{
+    if (tokens <= 1) return true;
+    if (dtype == OGQ_FP32) return tokens == 2 && outs <= 8192 && cols <= 16384;
+    if (tokens == 2) return outs <= 8192 || cols >= 1024;
+    return tokens <= 4 && outs <= 8192 && outs * cols <= (1u << 24);
+}
+
 // How group_matmul_kernel is launched.
 struct Plan {
     uint32_t token_tiles, row_blocks, token_blocks, parts, steps;
@@ -444,13 +477,25 @@ void launch_matmul(const Plan& p, const uint8_t* codes, const uint8_t* exponents
 }
 
 template <class T>
+void launch_few(dim3 grid, dim3 block, const uint8_t* codes, const uint8_t* exponents, const T* x, const MatvecShape& s, T* y, hipStream_t st)
+{
+    auto kernel = s.tokens == 1 ? group_matvec_kernel<T, 1> : group_matvec_kernel<T, 2>;
+    if constexpr (sizeof(T) == 2)
+        if (s.tokens > 2) kernel = group_matvec_kernel<T, 4>;
+    launch_kernel(kernel, grid, block, st, codes, exponents, x, s, y);
+}
+
+template <class T>
 void launch_of(const Groups& w, MatvecShape s, const T* x, uint32_t dtype, T* y, void* workspace, hipStream_t st)
 {
     const auto codes = static_cast<const uint8_t*>(w.codes);
-    if (s.tokens == 1) {
+    if (few_tokens(s.tokens, s.outs, s.cols, dtype)) {
         s.steps = ceil_div((uint64_t)s.groups << s.group_log2, 64 * kLaneCols);
-        const uint32_t rounds = ceil_div(s.steps, kFew), waves = rounds ? ceil_div(s.steps, rounds) : 1;
-        launch_kernel(group_matvec_kernel<T>, dim3(ceil_div(s.outs, kFew)), dim3(64 * waves), st, codes, w.exponents, x, s, y);
+        const uint32_t rounds = ceil_div(s.steps, kFew);
+        s.team = rounds ? ceil_div(s.steps, rounds) : 1;
+        // Several teams to a workgroup where 512 workgroups are left: one token in fp32, 1 and 4 teams: 16384 x 1024 8.0 and 5.7 us, 8192 x 1024 5.2 and 4.2, 2048 x 1024 3.2 and 3.8.
+        const uint32_t teams = min(kFew / s.team, max(1u, ceil_div(s.outs, kFew) / 512));
+        launch_few(dim3(ceil_div(s.outs, kFew * teams)), dim3(64 * s.team * teams), codes, w.exponents, x, s, y, st);
         return;
     }
     const Plan p = plan_of(s.tokens, s.outs, s.cols, dtype);
@@ -471,7 +516,7 @@ void launch_of(const Groups& w, MatvecShape s, const T* x, uint32_t dtype, T* y,
 
 size_t group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
 {
-    if (tokens == 1) return 0;
+    if (few_tokens(tokens, outs, cols, dtype)) return 0;
     const Plan p = plan_of(tokens, outs, cols, dtype);
     return p.parts > 1 ? p.parts * tokens * pitch_of(outs) * sizeof(float) : 0;
 }

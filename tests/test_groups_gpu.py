@@ -363,6 +363,17 @@ def test_matvec(dtype, tokens, outs, cols, group, pad):
     assert torch.equal(wide[:, 1:1 + outs], y) and (wide[:, 0] == 2.5).all() and (wide[:, 1 + outs:] == 2.5).all()
 
 
+# Two to four tokens, and rows so many that the wavefronts of a workgroup have different ones: one, two, three and four teams.
+FEW_TOKENS = [(2, 4099, 2100, 32, 1), (3, 8190, 500, 64, 0), (4, 6145, 999, 128, 8), (1, 8193, 2080, 32, 0), (1, 4097, 33, 32, 2), (2, 37, 6200, 64, 0),
+    (4, 1, 1, 32, 0), (3, 2050, 8160, 32, 0), (2, 8200, 1000, 32, 0)]
+
+
+@pytest.mark.parametrize("tokens,outs,cols,group,pad", FEW_TOKENS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_matvec_of_few_tokens(dtype, tokens, outs, cols, group, pad):
+    test_matvec(dtype, tokens, outs, cols, group, pad)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_matvec_of_what_is_not_finite(dtype):
     t = TYPES[dtype]
