@@ -45,7 +45,7 @@ def main():
                         need = lib.ogq_weight_gradient_workspace(rows, outs, cols, dtype, p8)
                         call(f"gradient {rows} {outs} {cols} {dtype}", 2 if need else 1, lib.ogq_weight_gradient, A, outs, dtype, A, A, rows, outs, cols, p8, 0, A, cols,
                              A, need, None)
-                for tokens in (1, 2, 5, 16, 17, 33, 64, 100, 1000):
+                for tokens in (1, 2, 3, 4, 5, 16, 17, 33, 64, 100, 1000):
                     for cols in (0,) + SIZES:
                         need = lib.ogq_group_matvec_workspace(tokens, rows, cols, dtype, p4)
                         call(f"matvec {tokens} {rows} {cols} {dtype}", 2 if need else 1, lib.ogq_group_matvec, A, A, rows, cols, p4, A, cols, tokens, dtype, A, rows, A, need,
