@@ -3,6 +3,8 @@
 //
 // group_matvec_kernel (a few tokens) on the vector unit, group_matmul_kernel (more) on the matrix cores.  Both read 32 weights (16 bytes) per lane and
 // turn eight of them into bf16 with four conversions, which take the group's power along.
+#include <cmath>
+
 #include "groups_common.h"
 
 namespace ogq {
@@ -452,17 +454,16 @@ Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
     p.token_blocks = ceil_div(tokens, 16 * p.token_tiles);
     const uint64_t blocks = (uint64_t)p.row_blocks * p.token_blocks;
     const uint32_t steps = ceil_div(cols, stage_cols(dtype == OGQ_FP32 ? 4 : 2, p.token_tiles));
-    // Parts of the sums (bf16 unless said): 1024 workgroups, four to a CU, where a part's sums, written and read once more, are few beside its weights.  61 tokens against
-    // 7708 x 5992: 3 parts 43.0 us, 6 30.0, 12 25.6; 64 against 4096 x 25088: 12 parts 50.3, 16 42.5, 24 38.4, 32 38.0; fp32, 64 against 4096 x 16384: 8 parts 54.9, 16
-    // 42.2, 32 44.2; 16 against 4096 x 25088: 8 parts 25.5, 16 19.2, 32 19.2; 5 in fp16 against 1000 x 4096: 12 parts 8.9, 16 6.9.
-    uint64_t most = cols / ((dtype == OGQ_FP32 ? 16 : 8) * tokens);
-    const uint64_t little = 262144 / (tokens * outs);  // (1 MB of parts costs nothing)
-    if (most < little) most = little;
-    if (most > steps) most = steps;
-    if (steps <= 4) most = 1;  // (a second launch costs more than four stages)
-    const uint64_t wanted = 1024 / blocks;
-    p.parts = (uint32_t)(wanted < most ? wanted : most);
-    if (p.parts < 1) p.parts = 1;
+    // Parts of the sums, where they save more than the second launch (3 us).  `alone`: us of a workgroup that has all steps, 1.2, 1.8 or 2.2 each, which more parts share out;
+    // `sums`: us for a part's sums on their way out and back.  Their sum is least at sqrt(alone / sums) parts.  Beyond one workgroup to a CU (`full`) only some two fifths of a
+    // step's time is still shared out, and whole rounds of 256 workgroups count.  us of both launches, by parts: 64 tokens in bf16, 1000 x 4096: 1 51, 4 19.6, 8 11.9, 16 10.9,
+    // 32 12.3; 2048 x 2048: 4 14.4, 8 10.6, 16 11.6; 4096 x 25088: 12 50.3, 16 42.5, 24 38.4, 32 38.0; in fp32, 4096 x 4096: 4 29.4, 8 22.0, 16 22.5, 32 28.2; 4096 x 16384: 8 54.9,
+    // 16 42.2, 32 44.2; 16 tokens in bf16, 4096 x 25088: 8 25.5, 16 19.2, 32 19.2; 16384 x 1024: 1 8.2, 2 8.6; 32 tokens: 1 13.0, 2 11.9; 512 tokens, 4096 x 4096: 1 73.5, 4 45.6.
+    const double alone = steps * (p.token_tiles == 1 ? 1.2 : p.token_tiles == 2 ? 1.8 : 2.2), sums = 1e-6 * (double)tokens * (double)outs;
+    const double full = 256.0 / blocks;
+    double parts = sqrt(alone / sums);
+    if (parts > full) parts = full * fmax(1.0, floor(0.63 * parts / full + 0.25));
+    p.parts = alone > 6.0 ? (uint32_t)fmax(1.0, fmin(parts, fmin(1024.0 / blocks, steps))) : 1;
     p.steps = ceil_div(steps, p.parts);
     return p;
 }
