@@ -494,10 +494,12 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // fp32: 256 x 128 where such tiles fill the chip, because LDS holds three pieces of dy beside one of the inputs: 4096 x 4096 of 2048 rows 176 us and 256 with 128 x
 // 128, 4096 x 25088 of 256 rows 194 and 225; 1024 x 1024 (32 tiles) of 8192 rows in the best parts 68 and 79, 1000 x 4096 (128) of 1000 rows 47 and 49, 512 x 512 of
 // 1024 rows 20 and 19.
-// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a step of 32 rows takes about 1 us in fp32 and 0.45 in 16 bits.  As many parts as make the two
-// equal, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us: 200 x 333 sums of 16385 rows in fp16 (35 parts by this) in 16 parts
-// 23.2 us, 32 18.6, 65 19.4, 128 23.6; 1024 x 1024 in bf16 (6) of 8192 rows in 4 parts 39.7, 8 38.1, 16 47.2; of 2048 rows (3) in 2 parts 22.8, 4 18.7, 8 22.0; 2048 x
-// 2048 of 8192 rows (2) in one part 113, 2 102, 4 103; 512 x 512 of 512 rows in one part 10.2, 2 10.4.
+// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.45 us in fp32 and 0.4 in 16 bits where it has the CU alone.  As
+// many parts as make the two together little, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us.  us of both launches, by parts, at
+// outputs x inputs of rows; 16 bits: 512 x 512 of 8192: 8 23.8, 12 20.5 (12 by this), 16 18.7, 32 21.3; 1024 x 1024 of 4096: 2 37.6, 4 27.6 (4), 6 28.1, 8 27.3, 12 31.1; 221 x 7969 of
+// 2280: 1 39.2, 2 30.7 (2), 4 28.8, 6 32.4; 2048 x 2048 of 2048: 1 35.3 (1), 2 37.8; 1733 x 1216 of 1249: 1 25.0 (1), 2 26.5, 3 23.9; 200 x 333 of 16385: 16 23.2, 32 18.6 (35), 65 19.4.
+// fp32: 512 x 512 of 8192: 8 59.3, 16 37.8, 24 33.7, 32 31.6 (27); 1024 x 1024 of 4096: 4 65.3, 6 55.5, 8 48.7 (8), 12 48.7; 1733 x 1216 of 1249: 1 68.8, 2 50.6, 3 40.8 (3), 4 41.2; 237 x
+// 5423 of 416: 1 25.4, 2 24.5 (2), 4 22.7; 1024 x 1024 of 256: 1 15.4 (1), 2 18.6.
 struct Plan {
     uint32_t tile_in, tile_out, tiles_in, tiles_out, parts, part;
 };
@@ -515,8 +517,8 @@ Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
     p.tiles_in = ceil_div(cols, p.tile_in), p.tiles_out = ceil_div(outs, p.tile_out);
     const uint64_t tiles = tiles_of(p.tile_in, p.tile_out);
     p.parts = 1;
-    if (p.tile_in == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 192 : 512)) {
-        const uint64_t squared = (uint64_t)rows * (dtype == OGQ_FP32 ? 12000 : 5000) / (outs * cols);
+    if (p.tile_in == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 320 : 512)) {
+        const uint64_t squared = (uint64_t)rows * (dtype == OGQ_FP32 ? 25000 : 5000) / (outs * cols);
         const uint64_t most = rows / 64 < 512 / tiles ? rows / 64 : 512 / tiles;
         while (p.parts < most && (uint64_t)(p.parts + 1) * (p.parts + 1) <= squared) ++p.parts;
     }
