@@ -274,7 +274,7 @@ template <class T, int IN, int OUT, int GROUPS>
 __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
                                                                       float* out)
 {
-    constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
+    constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 || IN == kSmall ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
     using Feed = Feeder<T, IN, OUT, kSets>;
     __shared__ __align__(16) char lds[kSets * Feed::kStage];
     const uint32_t tiles = s.tiles_in * s.tiles_out, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
@@ -301,8 +301,8 @@ __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* d
                 }
         }
     };
-    // 16-bit types: two steps are on their way while one is multiplied, in two stages of LDS with one barrier a step.  fp32: one of each, which leaves room for
-    // more workgroups on a CU (4096 x 25088 sums of 256 rows in tiles of 128 x 128: 209 us, 270 with two).
+    // Two steps are on their way while one is multiplied, in two stages of LDS with one barrier a step; one of each for fp32 in tiles of 256 x 128, whose second stage would fill
+    // LDS (4096 x 4096 sums of 4096 rows 364 us, 414 with two; in tiles of 128 x 128, of which a CU has one or two, 2048 x 2048 sums of 512 rows 33.0 us with one and 27.0 with two).
     const auto step = [&](uint32_t n, int set) __attribute__((always_inline)) {
         if (kSets == 1) __syncthreads();
         feed.bring(set, set);
@@ -491,15 +491,15 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // 16-bit types: 256 x 256 where such tiles fill most of the chip and a tile's own costs (its first steps, 256 KB of sums to store, with one workgroup on a CU) are
 // spread over 640 rows: 4096 x 4096 sums of 512 rows 27.9 us and 28.6 with 128 x 128, of 768 34.6 and 38.3, of 2048 68 and 86; 8192 x 8192 of 512 rows 114 and 99, of
 // 1024 167 and 195; 2560 x 4096 (160 tiles) of 4096 rows 100 and 115, 2048 x 4096 (128) of 2048 rows 58 and 47.  256 x 128: not better than 128 x 128 anywhere.
-// fp32: 256 x 128 where such tiles fill the chip, because LDS holds three pieces of dy beside one of the inputs: 4096 x 4096 of 2048 rows 176 us and 256 with 128 x
-// 128, 4096 x 25088 of 256 rows 194 and 225; 1024 x 1024 (32 tiles) of 8192 rows in the best parts 68 and 79, 1000 x 4096 (128) of 1000 rows 47 and 49, 512 x 512 of
-// 1024 rows 20 and 19.
-// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.45 us in fp32 and 0.4 in 16 bits where it has the CU alone.  As
+// fp32: 256 x 128 where such tiles fill the chip, because LDS holds three pieces of dy beside one of the inputs: 4096 x 4096 of 2048 rows 179 us and 256 with 128 x
+// 128, of 128 rows 24.5 and 27.5, 4096 x 25088 of 256 rows 201 and 235; 1024 x 1024 (32 tiles) of 8192 rows in the best parts 68 and 77, 1000 x 4096 (128) of 1000 rows 47
+// and 48, 512 x 512 of 1024 rows 20 and 17.
+// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.1 us in fp32 and 0.4 in 16 bits where it has the CU alone.  As
 // many parts as make the two together little, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us.  us of both launches, by parts, at
 // outputs x inputs of rows; 16 bits: 512 x 512 of 8192: 8 23.8, 12 20.5 (12 by this), 16 18.7, 32 21.3; 1024 x 1024 of 4096: 2 37.6, 4 27.6 (4), 6 28.1, 8 27.3, 12 31.1; 221 x 7969 of
 // 2280: 1 39.2, 2 30.7 (2), 4 28.8, 6 32.4; 2048 x 2048 of 2048: 1 35.3 (1), 2 37.8; 1733 x 1216 of 1249: 1 25.0 (1), 2 26.5, 3 23.9; 200 x 333 of 16385: 16 23.2, 32 18.6 (35), 65 19.4.
-// fp32: 512 x 512 of 8192: 8 59.3, 16 37.8, 24 33.7, 32 31.6 (27); 1024 x 1024 of 4096: 4 65.3, 6 55.5, 8 48.7 (8), 12 48.7; 1733 x 1216 of 1249: 1 68.8, 2 50.6, 3 40.8 (3), 4 41.2; 237 x
-// 5423 of 416: 1 25.4, 2 24.5 (2), 4 22.7; 1024 x 1024 of 256: 1 15.4 (1), 2 18.6.
+// fp32: 512 x 512 of 8192: 8 48.4, 16 33.1, 24 33.2, 32 31.6 (27); 1024 x 1024 of 4096: 4 53.6, 8 46.8 (8), 12 53.7; 864 x 977 of 1689: 1 67.3, 3 33.6, 6 29.4 (7), 8 27.7; 2048 x 2048 of
+// 2048: 1 87.8, 2 75.6 (2), 3 82.8; 237 x 5423 of 416: 1 21.7, 2 23.2 (2), 4 22.2; 1024 x 1024 of 256: 1 13.2 (1), 2 17.5.
 struct Plan {
     uint32_t tile_in, tile_out, tiles_in, tiles_out, parts, part;
 };
@@ -558,7 +558,7 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     const auto codes = static_cast<const uint8_t*>(x.codes);
     const auto go = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        auto kernel = weight_gradient_kernel<T, kSmall, kSmall, 3>;
+        auto kernel = weight_gradient_kernel<T, kSmall, kSmall, sizeof(T) == 4 ? 2 : 3>;
         if (plan.tile_in == kLarge) {
             if constexpr (sizeof(T) == 4) kernel = weight_gradient_kernel<T, kLarge, kSmall, 2>;
             else kernel = large_weight_gradient_kernel<T>;
