@@ -96,8 +96,8 @@ int ogq_activation_backward(const void* d_dy, size_t dy_stride, const void* d_co
 
 /* The gradient of a linear layer's weights from the gradient of its outputs and its checkpointed inputs (8 bits):
  *   dw[o][i] = sum over the rows t of dy[t][o] * x^[t][i],  0 <= o < outs, 0 <= i < cols,
- * or that added to what dw holds (accumulate != 0).  Products are exact (fp32 gradients are cut into three pieces of bf16), sums are
- * held in fp32 in an order that the sizes alone decide.  For fp16 gradients the checkpoint is one of an fp16 tensor.
+ * or that added to what dw holds (accumulate != 0).  Products are exact (fp32 gradients are cut into three pieces of bf16, in which
+ * what a value has below 2^-133 is lost), sums are held in fp32 in an order that the sizes alone decide.  For fp16 gradients the checkpoint is one of an fp16 tensor.
  * d_workspace: ogq_weight_gradient_workspace bytes, 16-byte aligned, may be NULL where that is 0. */
 size_t ogq_weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params);
 int ogq_weight_gradient(const void* d_dy, size_t dy_stride, uint32_t dtype, const void* d_codes, const uint8_t* d_exponents,
@@ -106,8 +106,9 @@ int ogq_weight_gradient(const void* d_dy, size_t dy_stride, uint32_t dtype, cons
 
 /* Tokens times the transpose of weights held in 4 bits (codes and exponents of a tensor [outs, cols]):
  *   y[t][o] = sum over i of x[t][i] * w^[o][i],  0 <= t < tokens, 0 <= o < outs.
- * Products are exact (x is cut into pieces of bf16: one for bf16, two for fp16, three for fp32), sums are held in fp32 in an order that the
- * sizes alone decide and rounded once.  Workspace as above. */
+ * Products are exact (for the matrix cores x is cut into pieces of bf16: one for bf16, two for fp16, three for fp32; on the vector unit, which
+ * takes up to four tokens, they are those of a dot product or a fused multiply-add; what an fp32 value has below 2^-133 may be lost in
+ * the pieces), sums are held in fp32 in an order that the sizes alone decide and rounded once.  Workspace as above. */
 size_t ogq_group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params);
 int ogq_group_matvec(const void* d_codes, const uint8_t* d_exponents, size_t outs, size_t cols, const ogq_group_params_t* params,
                      const void* d_x, size_t x_stride, size_t tokens, uint32_t dtype, void* d_y, size_t y_stride,

@@ -269,7 +269,9 @@ __device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t
 }
 
 // Tiles of IN x OUT sums, a quarter in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
-// next).
+// next).  Bound by LDS, to which every step goes and from which each factor is read twice, where a CU has two workgroups, and by a step's latency where it has one: 2048 x 2048 sums of
+// 8192 rows in bf16 95 us, 720 TFLOP/s; fp32, whose three products count: the same 257 us, 800 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
+// 4096 x 25088 of 256 rows 180 us, 870 TFLOP/s beside 2.3 TB/s of sums written.
 template <class T, int IN, int OUT, int GROUPS>
 __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
                                                                       float* out)
@@ -375,6 +377,8 @@ __device__ __forceinline__ void interleave()
 // Tiles of 256 x 256 sums, 128 x 128 in each of four wavefronts, one to a SIMD, which has all of its registers: 256 hold the sums.  While a wavefront
 // multiplies what it holds of a step, it reads its share of the next one from LDS and brings the one after that there; the step behind that is on its
 // way from memory.  One barrier a step, behind which all that the matrix cores need is in registers.
+// 16384 x 4096 sums of 8192 rows in bf16 890 us, 1.24 PFLOP/s; the library's product of two bf16 matrices of these sizes takes 907.  The matrix cores are busy for 0.64 of the
+// cycles, at a clock that is down to 1.7 GHz under their load.
 template <class T>
 __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
                                                                        bool accumulate, float* out)

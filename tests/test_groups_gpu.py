@@ -374,6 +374,21 @@ def test_matvec_of_few_tokens(dtype, tokens, outs, cols, group, pad):
     test_matvec(dtype, tokens, outs, cols, group, pad)
 
 
+@pytest.mark.parametrize("tokens", [1, 2, 5, 40])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_products_of_the_smallest_values(dtype, tokens):
+    """Subnormal values: each may lose what it has below 2^-133 (times a weight of at most 6 * 2^e), and a sum its last bit."""
+    t = TYPES[dtype]
+    p = ogq.make_group_params(32, 4)
+    codes, exponents = ogq.ogq_group_quantize(values(50, 300, torch.float32, 3), p)
+    held = ref.values(ref.unpack(codes, 4), exponents, 300)
+    x = (values(tokens, 300, torch.float32, 5) * 2.0 ** (-130 if t != torch.float16 else -20)).to(t)
+    exact = x.double() @ held.t().contiguous()
+    y = ogq.ogq_group_matvec(codes, exponents, 300, p, x).double()
+    terms, last = (x.double().abs() @ held.abs().t().contiguous()) * 300 * 2.0 ** -23, 2.0 ** (-149 if t == torch.float32 else -133 if t == torch.bfloat16 else -24)
+    assert ((y - exact).abs() <= terms + 300 * (2.0 ** -133 * held.abs().max() + 2.0 ** -149) + exact.abs() * 2.0 ** -8 + last).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_matvec_of_what_is_not_finite(dtype):
     t = TYPES[dtype]
