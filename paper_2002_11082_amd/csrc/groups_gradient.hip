@@ -146,12 +146,12 @@ struct Feeder {
     uint32_t byte[SETS][kInUnits];
 
     __device__ __forceinline__ Feeder(const T* dy_, const uint8_t* codes_, const uint8_t* exponents_, const GradientShape& s, uint32_t i0, uint32_t o0, uint32_t first_,
-                                      uint32_t last_, char* lds)
+                                      uint32_t last_, uint32_t thread, char* lds)
         : dy(dy_), codes(codes_), exponents(exponents_), dy_stride(s.dy_stride), pitch((uint64_t)s.groups << s.group_log2), groups(s.groups),
           group_log2(s.group_log2), first(first_), last(last_)
     {
-        const uint32_t in_chunk = threadIdx.x % (IN / 16), out_chunk = threadIdx.x % (OUT / 16);
-        in_row = threadIdx.x / (IN / 16), out_row = threadIdx.x / (OUT / 16);
+        const uint32_t in_chunk = thread % (IN / 16), out_chunk = thread % (OUT / 16);
+        in_row = thread / (IN / 16), out_row = thread / (OUT / 16);
         i_mine = i0 + in_chunk * 16, o_mine = o0 + out_chunk * 16;
         has_codes = i_mine < pitch;
         valid = o_mine >= s.outs ? 0 : (int)min(16u, s.outs - o_mine);
@@ -268,22 +268,26 @@ __device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t
         }
 }
 
-// Tiles of IN x OUT sums, a quarter in each of four wavefronts.  `out` is dw, or the workspace where the sum is cut into parts (out_part values from one part to the
-// next).  Bound by LDS, to which every step goes and from which each factor is read twice, where a CU has two workgroups, and by a step's latency where it has one: 2048 x 2048 sums of
-// 8192 rows in bf16 95 us, 720 TFLOP/s; fp32, whose three products count: the same 257 us, 800 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
+// Tiles of IN x OUT sums, a quarter in each of a team's four wavefronts; two teams have half of the rows each.  `out` is dw, or the workspace where the sum is cut into parts (out_part
+// values from one part to the next).  Bound by LDS, to which every step goes and from which each factor is read twice, where a CU has two workgroups, and by a step's latency where it has
+// one: 2048 x 2048 sums of 8192 rows in bf16 88 us, 780 TFLOP/s; fp32, whose three products count: the same 257 us, 800 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
 // 4096 x 25088 of 256 rows 180 us, 870 TFLOP/s beside 2.3 TB/s of sums written.
-template <class T, int IN, int OUT, int GROUPS>
-__global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s, bool accumulate,
-                                                                      float* out)
+template <class T, int IN, int OUT, int GROUPS, int TEAMS>
+__global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
+                                                                              bool accumulate, float* out)
 {
     constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 || IN == kSmall ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
     using Feed = Feeder<T, IN, OUT, kSets>;
-    __shared__ __align__(16) char lds[kSets * Feed::kStage];
+    __shared__ __align__(16) char all_lds[TEAMS * kSets * Feed::kStage];
     const uint32_t tiles = s.tiles_in * s.tiles_out, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
     const uint32_t i0 = tile % s.tiles_in * IN, o0 = tile / s.tiles_in * OUT;  // (neighbours along a row of sums: 8192 x 16384 of 32 rows 97 us, 131 in tile_of's order)
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
-    const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * (IN / 2), o_wave = (threadIdx.x >> 7) * (OUT / 2);
-    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
+    const uint32_t wave = TEAMS == 1 ? threadIdx.x >> 6 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = TEAMS == 1 ? 0 : wave >> 2;
+    const uint32_t lane = threadIdx.x & 63, i_wave = (wave & 1) * (IN / 2), o_wave = (wave >> 1 & 1) * (OUT / 2);
+    char* lds = all_lds + team * kSets * Feed::kStage;
+    Feed feed(dy, codes, exponents, s, i0, o0, first, last, TEAMS == 1 ? threadIdx.x : threadIdx.x & 255, lds);
+    feed.whole /= TEAMS;
+    feed.first += team * feed.whole * kDepth;
     const OperandPlaces<kIn, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
     const OperandPlaces<kOut, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
     f32x16 sum[kIn][kOut] = {};
@@ -334,14 +338,44 @@ __global__ __launch_bounds__(256, GROUPS) void weight_gradient_kernel(const T* d
         }
         if (n < feed.whole) step(n, 0);
     }
-    for (uint32_t t = first + feed.whole * kDepth; t < last; t += kDepth) {
+    for (uint32_t all = first + TEAMS * feed.whole * kDepth; all < last; all += TEAMS * kDepth) {
+        const uint32_t t = all + team * kDepth;
         __syncthreads();
-        feed.bring_asking(t);
+        if (t < last) feed.bring_asking(t);
         __syncthreads();
-        products(0);
+        if (t < last) products(0);
     }
     __syncthreads();
-    store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, lds + (threadIdx.x >> 6) * kTurnBytes);
+    char* space = all_lds + wave * kTurnBytes;
+    if constexpr (TEAMS == 1) {
+        store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, space);
+    } else {
+        // each team stores the sums of one half of the outputs, and has the other one's share of them through LDS
+        static_assert(TEAMS == 2 && kOut == 2 && sizeof all_lds >= 2 * 256 * kIn * 64);
+        f32x4* exchange = reinterpret_cast<f32x4*>(all_lds);
+        const auto place = [&](uint32_t of, int i, int m) { return ((of * 4 + (wave & 3)) * kIn + i) * 256 + m * 64 + lane; };
+        const auto send = [&](const f32x16& v, int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) exchange[place(team, i, m)] = f32x4{v[4 * m], v[4 * m + 1], v[4 * m + 2], v[4 * m + 3]};
+        };
+        f32x16 mine[kIn][1];
+#pragma unroll
+        for (int i = 0; i < kIn; ++i) {
+            if (team == 0) send(sum[i][1], i), mine[i][0] = sum[i][0];
+            else send(sum[i][0], i), mine[i][0] = sum[i][1];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kIn; ++i)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const f32x4 v = exchange[place(team ^ 1, i, m)];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mine[i][0][4 * m + r] += v[r];
+            }
+        __syncthreads();
+        store_tile(mine, i0 + i_wave, o0 + o_wave + 32 * team, lane, s, accumulate, out + part * s.out_part, space);
+    }
 }
 
 // Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the inputs by eight along the outputs at a
@@ -391,7 +425,7 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
     const uint32_t i0 = tile.x * kLarge, o0 = tile.y * kLarge;
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
     const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * 128, o_wave = (threadIdx.x >> 7) * 128;
-    Feed feed(dy, codes, exponents, s, i0, o0, first, last, lds);
+    Feed feed(dy, codes, exponents, s, i0, o0, first, last, threadIdx.x, lds);
     const OperandPlaces<4, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
     const OperandPlaces<4, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
     using Operands = s16x8[4][2];
@@ -509,14 +543,18 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // fp32: 256 x 128 where such tiles fill the chip, because LDS holds three pieces of dy beside one of the inputs: 4096 x 4096 of 2048 rows 179 us and 256 with 128 x
 // 128, of 128 rows 24.5 and 27.5, 4096 x 25088 of 256 rows 201 and 235; 1024 x 1024 (32 tiles) of 8192 rows in the best parts 68 and 77, 1000 x 4096 (128) of 1000 rows 47
 // and 48, 512 x 512 of 1024 rows 20 and 17.
-// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.1 us in fp32 and 0.4 in 16 bits where it has the CU alone.  As
-// many parts as make the two together little, up to 512 workgroups and 64 rows, where the steps saved are worth the second launch's 4 us.  us of both launches, by parts, at
-// outputs x inputs of rows; 16 bits: 512 x 512 of 8192: 8 23.8, 12 20.5 (12 by this), 16 18.7, 32 21.3; 1024 x 1024 of 4096: 2 37.6, 4 27.6 (4), 6 28.1, 8 27.3, 12 31.1; 221 x 7969 of
-// 2280: 1 39.2, 2 30.7 (2), 4 28.8, 6 32.4; 2048 x 2048 of 2048: 1 35.3 (1), 2 37.8; 1733 x 1216 of 1249: 1 25.0 (1), 2 26.5, 3 23.9; 200 x 333 of 16385: 16 23.2, 32 18.6 (35), 65 19.4.
+// 16 bits in tiles of 128 x 128: two teams of four wavefronts share a tile's rows where there are up to two workgroups to a CU, which leave its latencies open: 2048 x 2048 of 2048
+// rows 28.3 us and 32.2 with one team, 1733 x 1216 of 1249 19.7 and 23.4, 2500 x 2500 (400 tiles) of 3000 64.8 and 69.0; but 2560 x 4096 (640) of 1024 37.5 and 35.8, 4096 x 4096 of
+// 256 22.7 and 19.5, and 512 x 512 of 32 rows, one step, 5.4 and 5.0.  fp32: 1733 x 1216 of 1249 rows 47 us with two teams in the best parts, 38.6 with one.
+// A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.1 us in fp32 and 0.28 in 16 bits where it has the CU alone.  As
+// many parts as make the two together little, up to 512 workgroups (256 of two teams) and 64 rows, where the steps saved are worth the second launch (4 us and what it reads).  us of both launches,
+// by parts, at outputs x inputs of rows; 16 bits: 512 x 512 of 8192: 8 20.2, 12 18.7, 16 18.2 (16 by this), 24 23.0; 1024 x 1024 of 4096: 1 40.8, 2 29.4, 4 24.0 (4), 6 28.4; 864 x 977 of
+// 1689: 1 21.2, 3 18.6 (4), 4 17.3, 6 21.8; 1024 x 1024 of 1024: 1 14.2 (1), 2 18.0; 221 x 7969 of 2280: 1 28.8, 2 26.3 (2), 3 31.0; 2048 x 2048 of 8192: 1 90.9 (1), 2 96.7; 200 x 333 of
+// 16385: 16 21.1, 24 18.1, 32 19.2 (42).
 // fp32: 512 x 512 of 8192: 8 48.4, 16 33.1, 24 33.2, 32 31.6 (27); 1024 x 1024 of 4096: 4 53.6, 8 46.8 (8), 12 53.7; 864 x 977 of 1689: 1 67.3, 3 33.6, 6 29.4 (7), 8 27.7; 2048 x 2048 of
-// 2048: 1 87.8, 2 75.6 (2), 3 82.8; 237 x 5423 of 416: 1 21.7, 2 23.2 (2), 4 22.2; 1024 x 1024 of 256: 1 13.2 (1), 2 17.5.
+// 2048: 1 87.8, 2 75.6 (2), 3 82.8; 237 x 5423 of 416: 1 21.7, 2 23.2 (2), 4 22.2; 1024 x 1024 of 256: 1 13.2 (1), 2 17.5.  16 bits, 128 x 128 of 1200: 1 15.2, 18 9.6 (18).
 struct Plan {
-    uint32_t tile_in, tile_out, tiles_in, tiles_out, parts, part;
+    uint32_t tile_in, tile_out, tiles_in, tiles_out, parts, part, teams;
 };
 
 Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
@@ -532,12 +570,18 @@ Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
     p.tiles_in = ceil_div(cols, p.tile_in), p.tiles_out = ceil_div(outs, p.tile_out);
     const uint64_t tiles = tiles_of(p.tile_in, p.tile_out);
     p.parts = 1;
-    if (p.tile_in == kSmall && tiles < 512 && rows >= (dtype == OGQ_FP32 ? 320 : 512)) {
-        const uint64_t squared = (uint64_t)rows * (dtype == OGQ_FP32 ? 25000 : 5000) / (outs * cols);
-        const uint64_t most = rows / 64 < 512 / tiles ? rows / 64 : 512 / tiles;
-        while (p.parts < most && (uint64_t)(p.parts + 1) * (p.parts + 1) <= squared) ++p.parts;
+    const bool fp32 = dtype == OGQ_FP32;
+    const uint64_t fill = fp32 ? 512 : 256;
+    if (p.tile_in == kSmall && tiles < fill) {
+        const uint64_t squared = (uint64_t)rows * (fp32 ? 25000 : 9000) / (outs * cols);
+        const uint64_t most = rows / 64 < fill / tiles ? rows / 64 : fill / tiles;
+        uint32_t parts = 1;
+        while (parts < most && (uint64_t)(parts + 1) * (parts + 1) <= squared) ++parts;
+        const double saved = rows / 32.0 * (fp32 ? 1.1 : 0.28) * (1.0 - 1.0 / parts), cost = 4.0 + 1e-6 * parts * (double)outs * (double)cols;
+        if (saved > cost) p.parts = parts;
     }
     p.part = ceil_div(ceil_div(rows, p.parts), kDepth) * kDepth;
+    p.teams = dtype != OGQ_FP32 && p.tile_in == kSmall && tiles * p.parts <= 512 && rows > kDepth ? 2 : 1;
     return p;
 }
 
@@ -569,14 +613,16 @@ void launch_weight_gradient(const Values& dy, uint32_t dtype, const Groups& x, s
     // 202 and 194; but 2700 x 6890, whose lines two rows share, of 9 rows 48.4 and 18.9 through them).
     s.stream = parts == 1 && outs * cols >= ((size_t)8 << 20) && ((reinterpret_cast<uintptr_t>(out) | s.out_stride * 4) & 63) == 0;
     const bool add = accumulate && parts == 1;
-    const dim3 grid(s.tiles_in * s.tiles_out * parts), block(256);
+    const dim3 grid(s.tiles_in * s.tiles_out * parts), block(256 * plan.teams);
     const auto codes = static_cast<const uint8_t*>(x.codes);
     const auto go = [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        auto kernel = weight_gradient_kernel<T, kSmall, kSmall, sizeof(T) == 4 ? 2 : 3>;
-        if (plan.tile_in == kLarge) {
-            if constexpr (sizeof(T) == 4) kernel = weight_gradient_kernel<T, kLarge, kSmall, 2>;
-            else kernel = large_weight_gradient_kernel<T>;
+        auto kernel = weight_gradient_kernel<T, kSmall, kSmall, sizeof(T) == 4 ? 2 : 3, 1>;
+        if constexpr (sizeof(T) == 4) {
+            if (plan.tile_in == kLarge) kernel = weight_gradient_kernel<T, kLarge, kSmall, 2, 1>;
+        } else {
+            if (plan.teams == 2) kernel = weight_gradient_kernel<T, kSmall, kSmall, 2, 2>;
+            if (plan.tile_in == kLarge) kernel = large_weight_gradient_kernel<T>;
         }
         launch_kernel(kernel, grid, block, st, static_cast<const T*>(dy.data), codes, x.exponents, s, add, out);
     };
