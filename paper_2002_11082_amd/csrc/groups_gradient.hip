@@ -545,7 +545,7 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // and 48, 512 x 512 of 1024 rows 20 and 17.
 // 16 bits in tiles of 128 x 128: two teams of four wavefronts share a tile's rows where there are up to two workgroups to a CU, which leave its latencies open: 2048 x 2048 of 2048
 // rows 28.3 us and 32.2 with one team, 1733 x 1216 of 1249 19.7 and 23.4, 2500 x 2500 (400 tiles) of 3000 64.8 and 69.0; but 2560 x 4096 (640) of 1024 37.5 and 35.8, 4096 x 4096 of
-// 256 22.7 and 19.5, and 512 x 512 of 32 rows, one step, 5.4 and 5.0.  fp32: 1733 x 1216 of 1249 rows 47 us with two teams in the best parts, 38.6 with one.
+// 256 22.7 and 19.5, 512 x 512 of 32 rows, one step, 5.4 and 5.0, and 128 x 128 of 1200 in 18 parts 10.4 and 9.8.  fp32: 1733 x 1216 of 1249 rows 47 us with two teams in the best parts, 38.6 with one.
 // A part's sums are written and read once more, 8 bytes each at about 3 TB/s; a workgroup's step of 32 rows takes 1.1 us in fp32 and 0.28 in 16 bits where it has the CU alone.  As
 // many parts as make the two together little, up to 512 workgroups (256 of two teams) and 64 rows, where the steps saved are worth the second launch (4 us and what it reads).  us of both launches,
 // by parts, at outputs x inputs of rows; 16 bits: 512 x 512 of 8192: 8 20.2, 12 18.7, 16 18.2 (16 by this), 24 23.0; 1024 x 1024 of 4096: 1 40.8, 2 29.4, 4 24.0 (4), 6 28.4; 864 x 977 of
@@ -580,8 +580,9 @@ Plan plan_of(size_t rows, size_t outs, size_t cols, uint32_t dtype)
         const double saved = rows / 32.0 * (fp32 ? 1.1 : 0.28) * (1.0 - 1.0 / parts), cost = 4.0 + 1e-6 * parts * (double)outs * (double)cols;
         if (saved > cost) p.parts = parts;
     }
-    p.part = ceil_div(ceil_div(rows, p.parts), kDepth) * kDepth;
-    p.teams = dtype != OGQ_FP32 && p.tile_in == kSmall && tiles * p.parts <= 512 && rows > kDepth ? 2 : 1;
+    p.teams = !fp32 && p.tile_in == kSmall && tiles * p.parts <= 512 && rows / p.parts >= (p.parts == 1 ? kDepth + 1 : 6 * kDepth) ? 2 : 1;
+    const uint32_t steps = kDepth * p.teams;  // (a step more for one team would be one that asks)
+    p.part = ceil_div(ceil_div(rows, p.parts), steps) * steps;
     return p;
 }
 
