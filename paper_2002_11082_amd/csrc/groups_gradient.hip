@@ -270,7 +270,7 @@ __device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t
 
 // Tiles of IN x OUT sums, a quarter in each of a team's four wavefronts; two teams have half of the rows each.  `out` is dw, or the workspace where the sum is cut into parts (out_part
 // values from one part to the next).  Bound by LDS, to which every step goes and from which each factor is read twice, where a CU has two workgroups, and by a step's latency where it has
-// one: 2048 x 2048 sums of 8192 rows in bf16 88 us, 780 TFLOP/s; fp32, whose three products count: the same 257 us, 800 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
+// one: 2048 x 2048 sums of 8192 rows in bf16 91 us, 755 TFLOP/s; fp32, whose three products count: the same 250 us, 825 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
 // 4096 x 25088 of 256 rows 180 us, 870 TFLOP/s beside 2.3 TB/s of sums written.
 template <class T, int IN, int OUT, int GROUPS, int TEAMS>
 __global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
