@@ -270,6 +270,18 @@ GRADIENTS = [  # rows, outs, cols, group, pad
     (640, 4096, 3136, 32, 0), (641, 4100, 3330, 64, 3), (671, 3585, 4100, 128, 0), (703, 8200, 1600, 32, 8), (1030, 3600, 4000, 32, 1), (20, 4099, 4098, 32, 0)]
 
 
+# Rows shared by two teams of wavefronts: no whole step for either, one for each, an odd number, a rest of one and of two steps; parts of a sum for two teams and for one; more
+# than 512 tiles, which have one team.
+TEAMS = [(63, 100, 100, 32, 0), (65, 130, 260, 32, 3), (97, 20, 40, 64, 0), (129, 257, 129, 32, 0), (161, 128, 512, 128, 0), (190, 111, 222, 32, 8), (1300, 140, 150, 32, 0),
+    (4097, 300, 500, 64, 1), (16390, 100, 40, 32, 0), (2300, 513, 1030, 32, 0), (70, 4001, 2700, 32, 0), (510, 3300, 2200, 128, 8)]
+
+
+@pytest.mark.parametrize("rows,outs,cols,group,pad", TEAMS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weight_gradient_of_teams_and_parts(dtype, rows, outs, cols, group, pad):
+    test_weight_gradient(dtype, rows, outs, cols, group, pad)
+
+
 @pytest.mark.parametrize("rows,outs,cols,group,pad", GRADIENTS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_weight_gradient(dtype, rows, outs, cols, group, pad):
