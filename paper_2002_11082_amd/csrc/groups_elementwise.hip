@@ -118,13 +118,64 @@ __global__ __launch_bounds__(kBlock) void group_dequantize_kernel(const void* co
     }
 }
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
+constexpr float kLog2e = 1.44269504088896f, kLog2eRest = 1.92596299112662e-8f;  // log2(e) in two pieces
+
+// exp(a + b), |b| far below |a|, to 3 * 2^-24: a whole power of two, and the instruction's power of a fraction of at most a half, whose rounding is 2^-25 of the result.
+__device__ __forceinline__ float exp_of(float a, float b)
+{
+    const float n = rintf(a * kLog2e);
+    const float f = __builtin_fmaf(b, kLog2e, __builtin_fmaf(a, kLog2eRest, __builtin_fmaf(a, kLog2e, -n)));
+    return ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+}
+
+// 1 / d for 1 <= d < 2^64, to 2^-24.
+__device__ __forceinline__ float reciprocal(float d)
+{
+    const float r = __builtin_amdgcn_rcpf(d);
+    return __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e)); }
+
+// p = (1 + erf(x / sqrt(2))) / 2 without the difference that cancels for negative x, and g = exp(-x^2 / 2), which the slope has too.  With z = |x|, the smaller one of p and 1 - p is
+// R(z) * g, where R(z) = exp(z^2 / 2) * erfc(z / sqrt(2)) / 2 falls slowly from 1/2 like 1 / z: t times a polynomial of t = 1 / (1 + 0.3 z), whose coefficients are least squares of the
+// relative error on 0 <= z <= 16, weighted until it was even.  EXACT: nine steps, off by 2^-28, and the exponential of x^2 with what its rounding leaves; otherwise seven, off by 2^-22.
+template <bool EXACT>
+__device__ __forceinline__ void normal_distribution(float x, float& p, float& g)
+{
+    float t, r;
+    if constexpr (EXACT) {
+        const float z = fminf(fabsf(x), 16.0f), square = z * z;  // (exp(-128) is below the least number)
+        g = exp_of(-0.5f * square, -0.5f * __builtin_fmaf(z, z, -square));
+        t = reciprocal(__builtin_fmaf(z, 0.3f, 1.0f));
+        r = __builtin_fmaf(-0.020629964768886566f, t, 0.11247210204601288f);
+        r = __builtin_fmaf(r, t, -0.22830256819725037f);
+        r = __builtin_fmaf(r, t, 0.1919078826904297f);
+        r = __builtin_fmaf(r, t, -0.07953041791915894f);
+        r = __builtin_fmaf(r, t, 0.09621681272983551f);
+        r = __builtin_fmaf(r, t, 0.0783679336309433f);
+        r = __builtin_fmaf(r, t, 0.11024031043052673f);
+        r = __builtin_fmaf(r, t, 0.11957119405269623f);
+        r = __builtin_fmaf(r, t, 0.11968672275543213f);
+    } else {
+        g = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+        t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(x), 0.3f, 1.0f));
+        r = __builtin_fmaf(0.034704964607954025f, t, -0.15318746864795685f);
+        r = __builtin_fmaf(r, t, 0.19948841631412506f);
+        r = __builtin_fmaf(r, t, -0.04742685705423355f);
+        r = __builtin_fmaf(r, t, 0.12529200315475464f);
+        r = __builtin_fmaf(r, t, 0.10088922083377838f);
+        r = __builtin_fmaf(r, t, 0.12060054391622543f);
+        r = __builtin_fmaf(r, t, 0.1196390762925148f);
+    }
+    const float smaller = r * t * g;
+    p = x < 0.0f ? smaller : 1.0f - smaller;
+}
 
 constexpr float kTanhScale = 0.797884560802865f, kCubic = 0.044715f;  // sqrt(2 / pi)
 
 // act(x) and act'(x).
-template <uint32_t ACT>
+template <uint32_t ACT, bool EXACT>
 __device__ __forceinline__ void activation(float x, float& value, float& slope)
 {
     if constexpr (ACT == OGQ_RELU) {
@@ -135,9 +186,10 @@ __device__ __forceinline__ void activation(float x, float& value, float& slope)
         value = x * s;
         slope = s * (1.0f + x * (1.0f - s));
     } else if constexpr (ACT == OGQ_GELU) {
-        const float p = 0.5f * (1.0f + erff(x * 0.707106781186548f));
+        float p, g;
+        normal_distribution<EXACT>(x, p, g);
         value = x * p;
-        slope = p + x * (0.398942280401433f * exp_of(-0.5f * x * x));
+        slope = p + x * (0.398942280401433f * g);
     } else {
         // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).  The square is limited: behind 10 the slope's second term is 0, where an infinite square
         // would make it NaN.
@@ -151,10 +203,11 @@ __device__ __forceinline__ void activation(float x, float& value, float& slope)
 template <uint32_t ACT, int N, class F>
 __device__ __forceinline__ void each(const float (&x)[N], F f)
 {
+    constexpr bool kExact = N == kPiece<float>;  // (a piece of 32-bit values)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float value, slope;
-        activation<ACT>(x[i], value, slope);
+        activation<ACT, kExact>(x[i], value, slope);
         f(i, value, slope);
     }
 }

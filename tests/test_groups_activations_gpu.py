@@ -1,0 +1,79 @@
+"""Activations of libogq_groups over all of their range, on the GPU against the definitions in 64 bits, by bounds that are relative to the results: the tails
+where an activation is a small difference or a small quotient are held to as many bits as the rest.
+
+In 32 bits, u = 2^-24: the exponential is off by 3 u at most (its instruction by 2, its argument's fraction by 1), a sum, a reciprocal with its correction
+and a product by one u each: 16 u for gelu, whose polynomial takes nine steps; a slope is off by as much of the sum of its terms' magnitudes.
+In 16 bits an approximation of 2^-15 at most is rounded once; the hardware's exponential takes what is below 2^-126 for 0."""
+import math
+
+import pytest
+import torch
+
+import paper_2002_11082_amd as ogq
+from tests import groups_reference as ref
+from tests.test_groups_gpu import ACTS, DEV, ROUNDING, TYPES, say
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def exact(act, x):
+    """(act(x), act'(x), the sum of the magnitudes of the slope's terms, how many u they may be off by)."""
+    if act == "relu":
+        return x.clamp(min=0.0), (x > 0.0).double(), (x > 0.0).double(), torch.zeros_like(x)
+    p, term = 0.5 * torch.erfc(-x / math.sqrt(2.0)), x * torch.exp(-0.5 * x * x) / math.sqrt(2.0 * math.pi)
+    return x * p, p + term, p + term.abs(), torch.full_like(x, 16.0)
+
+
+def within(out, expected, size, units, what):
+    dtype = out.dtype
+    if dtype == torch.float32:
+        bound = units.clamp(max=2.0 ** 12) * U * size + 2.0 ** -140
+    else:
+        bound = 2.0 ** -15 * size + ROUNDING[dtype] * (1.0 + 2.0 ** -8) * expected.abs() + max(2.0 ** -119, torch.finfo(dtype).smallest_normal * ROUNDING[dtype])
+    off = (out.double() - expected).abs() - bound
+    at = off.argmax().item()
+    assert bool((off <= 0.0).all()), (what, int((off > 0.0).sum()), out.flatten()[at].item(), expected.flatten()[at].item())
+
+
+def all_values(dtype):
+    """Every finite value of a 16-bit type; in 32 bits a dense set of those between which anything happens, and all sizes."""
+    if dtype == torch.float32:
+        x = torch.cat([torch.linspace(-110.0, 110.0, 1 << 20, dtype=torch.float64), torch.linspace(-15.0, 15.0, 1 << 20, dtype=torch.float64),
+                       torch.logspace(-44.0, 38.4, 1 << 15, dtype=torch.float64), -torch.logspace(-44.0, 38.4, 1 << 15, dtype=torch.float64)]).float()
+    else:
+        x = torch.arange(-1 << 15, 1 << 15, dtype=torch.int16).view(dtype)
+    x = x[torch.isfinite(x)]
+    return x[: x.numel() // 256 * 256].view(-1, 256).to(DEV)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activations_of_all_values(dtype, act):
+    x = all_values(TYPES[dtype])
+    say("all values", dtype, act, tuple(x.shape))
+    y = ogq.ogq_activation_forward(x, ACTS[act], ogq.make_group_params(32, 8))[0]
+    value, _, _, units = exact(act, x.double())
+    if TYPES[dtype] == torch.float16:
+        value = value.clamp(-65504.0, 65504.0)
+    within(y, value, value.abs(), units, (dtype, act))
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_slopes_of_all_values(dtype, act):
+    """Every number of the format at every power of two between which a slope changes."""
+    q = torch.arange(-127, 128, dtype=torch.float64)
+    q = torch.cat([q, q[-1:]])
+    x = torch.cat([q[None, :] * 2.0 ** e for e in range(-20, 2)]).view(-1, 32)
+    x = x.to(TYPES[dtype]).to(DEV)
+    p = ogq.make_group_params(32, 8)
+    codes, exponents = ogq.ogq_group_quantize(x, p)
+    held = ref.held(x, 32, 8)
+    value, slope, size, units = exact(act, held)
+    one = torch.ones_like(x)
+    up_codes, up_exponents = ogq.ogq_group_quantize(one, p)
+    within(ogq.ogq_activation_backward(one, ACTS[act], codes, exponents, p), slope, size, units, (dtype, act))
+    dx, dup = ogq.ogq_activation_backward(one, ACTS[act], codes, exponents, p, up_codes, up_exponents)
+    within(dx, slope, size, units, (dtype, act, "gated"))
+    within(dup, value, value.abs(), units, (dtype, act, "dup"))
