@@ -135,7 +135,19 @@ __device__ __forceinline__ float reciprocal(float d)
     return __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e)); }
+// s = 1 / (1 + exp(-x)) and 1 - s.  EXACT: to a few roundings of 32 bits, both of them, whatever x; otherwise to 2^-17 where exp(-x) is below 2^126, which is for 16-bit results.
+template <bool EXACT>
+__device__ __forceinline__ void sigmoid(float x, float& s, float& rest)
+{
+    if constexpr (EXACT) {
+        const float e = exp_of(-fminf(fabsf(x), 200.0f), 0.0f), r = reciprocal(1.0f + e);
+        s = x < 0.0f ? e * r : r;
+        rest = x < 0.0f ? r : e * r;
+    } else {
+        s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
+        rest = 1.0f - s;
+    }
+}
 
 // p = (1 + erf(x / sqrt(2))) / 2 without the difference that cancels for negative x, and g = exp(-x^2 / 2), which the slope has too.  With z = |x|, the smaller one of p and 1 - p is
 // R(z) * g, where R(z) = exp(z^2 / 2) * erfc(z / sqrt(2)) / 2 falls slowly from 1/2 like 1 / z: t times a polynomial of t = 1 / (1 + 0.3 z), whose coefficients are least squares of the
@@ -182,21 +194,23 @@ __device__ __forceinline__ void activation(float x, float& value, float& slope)
         value = x < 0.0f ? 0.0f : x;  // (NaN stays)
         slope = x > 0.0f ? 1.0f : x == x ? 0.0f : x;
     } else if constexpr (ACT == OGQ_SILU) {
-        const float s = sigmoid(x);
+        float s, rest;
+        sigmoid<EXACT>(x, s, rest);
         value = x * s;
-        slope = s * (1.0f + x * (1.0f - s));
+        slope = s * (1.0f + x * rest);
     } else if constexpr (ACT == OGQ_GELU) {
         float p, g;
         normal_distribution<EXACT>(x, p, g);
         value = x * p;
         slope = p + x * (0.398942280401433f * g);
     } else {
-        // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).  The square is limited: behind 10 the slope's second term is 0, where an infinite square
+        // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).  The square is limited: behind 100 the slope's second term is 0, where an infinite square
         // would make it NaN.
-        const float square = fminf(x * x, 100.0f);
-        const float s = sigmoid(2.0f * kTanhScale * x * (1.0f + kCubic * square));
+        const float square = fminf(x * x, 10000.0f);
+        float s, rest;
+        sigmoid<EXACT>(2.0f * kTanhScale * x * (1.0f + kCubic * square), s, rest);
         value = x * s;
-        slope = s + x * s * (1.0f - s) * 2.0f * kTanhScale * (1.0f + 3.0f * kCubic * square);
+        slope = s + x * s * rest * 2.0f * kTanhScale * (1.0f + 3.0f * kCubic * square);
     }
 }
 

@@ -1,9 +1,10 @@
 """Activations of libogq_groups over all of their range, on the GPU against the definitions in 64 bits, by bounds that are relative to the results: the tails
 where an activation is a small difference or a small quotient are held to as many bits as the rest.
 
-In 32 bits, u = 2^-24: the exponential is off by 3 u at most (its instruction by 2, its argument's fraction by 1), a sum, a reciprocal with its correction
-and a product by one u each: 16 u for gelu, whose polynomial takes nine steps; a slope is off by as much of the sum of its terms' magnitudes.
-In 16 bits an approximation of 2^-15 at most is rounded once; the hardware's exponential takes what is below 2^-126 for 0."""
+In 32 bits, u = 2^-24: the exponential is off by 3 u at most (its instruction by 2, its argument's fraction by 1), the sum with 1, the reciprocal with its correction,
+and the products by one u each (a reciprocal's error counts with the one before it): 12 u for a sigmoid times x and 16 u for gelu, whose polynomial takes nine steps; a slope is off by as much of
+the sum of its terms' magnitudes.  gelu_tanh's exponent has five roundings more, 5 u of the exponent itself.
+In 16 bits an approximation of 2^-15 at most is rounded once; the hardware's exponential takes what is below 2^-126 for 0, which is less than 2^-119 times x."""
 import math
 
 import pytest
@@ -21,8 +22,16 @@ def exact(act, x):
     """(act(x), act'(x), the sum of the magnitudes of the slope's terms, how many u they may be off by)."""
     if act == "relu":
         return x.clamp(min=0.0), (x > 0.0).double(), (x > 0.0).double(), torch.zeros_like(x)
-    p, term = 0.5 * torch.erfc(-x / math.sqrt(2.0)), x * torch.exp(-0.5 * x * x) / math.sqrt(2.0 * math.pi)
-    return x * p, p + term, p + term.abs(), torch.full_like(x, 16.0)
+    if act == "gelu":
+        p, term = 0.5 * torch.erfc(-x / math.sqrt(2.0)), x * torch.exp(-0.5 * x * x) / math.sqrt(2.0 * math.pi)
+        return x * p, p + term, p + term.abs(), torch.full_like(x, 16.0)
+    w, dw = x, torch.ones_like(x)
+    if act == "gelu_tanh":  # (1 + tanh(w / 2)) / 2 = 1 / (1 + exp(-w))
+        c = 2.0 * math.sqrt(2.0 / math.pi)
+        w, dw = c * (x + 0.044715 * x ** 3), c * (1.0 + 3.0 * 0.044715 * x * x)
+    s, rest = torch.sigmoid(w), torch.sigmoid(-w)
+    term = x * s * rest * dw
+    return x * s, s + term, s + term.abs(), 12.0 + (8.0 * w.abs() if act == "gelu_tanh" else 0.0) + torch.zeros_like(x)
 
 
 def within(out, expected, size, units, what):
@@ -47,7 +56,7 @@ def all_values(dtype):
     return x[: x.numel() // 256 * 256].view(-1, 256).to(DEV)
 
 
-@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_activations_of_all_values(dtype, act):
     x = all_values(TYPES[dtype])
@@ -59,7 +68,7 @@ def test_activations_of_all_values(dtype, act):
     within(y, value, value.abs(), units, (dtype, act))
 
 
-@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_slopes_of_all_values(dtype, act):
     """Every number of the format at every power of two between which a slope changes."""
