@@ -137,7 +137,8 @@ struct Feeder {
     uint64_t dy_stride, pitch;
     uint32_t groups, group_log2, first, last, in_row, out_row, i_mine, o_mine;
     uint32_t at_codes, at_byte, at_dy;
-    uint32_t whole;  // steps that are there in all rows, and can be read without asking
+    uint32_t whole;  // steps that are there in all rows
+    bool readable;   // whether these can be read without asking
     bool has_codes;
     int valid;
     char *in_to, *out_to;
@@ -163,8 +164,8 @@ struct Feeder {
         const bool partial = o0 + OUT > s.outs && s.outs % 16 != 0;
         whole = first < last ? (last - first) / kDepth : 0;
         if (partial && whole != 0 && first + whole * kDepth == s.rows) --whole;
-        // (a thread's place in a unit's rows is held in 32 bits; reading on needs a next row)
-        if ((dy_stride | pitch) >= (1u << 24) || (partial && dy_stride < 16)) whole = 0;
+        // (a thread's place in a unit's rows is held in 32 bits; reading on needs a next row.  `whole` stays what the sizes make it: two teams share the rows by it.)
+        readable = (dy_stride | pitch) < (1u << 24) && !(partial && dy_stride < 16);
         const uint32_t i = has_codes ? i_mine : i0, o = valid != 0 ? o_mine : o0;
         at_codes = in_row * (uint32_t)pitch + i;
         at_byte = in_row * groups + (i >> group_log2);
@@ -286,8 +287,9 @@ __global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(co
     const uint32_t lane = threadIdx.x & 63, i_wave = (wave & 1) * (IN / 2), o_wave = (wave >> 1 & 1) * (OUT / 2);
     char* lds = all_lds + team * kSets * Feed::kStage;
     Feed feed(dy, codes, exponents, s, i0, o0, first, last, TEAMS == 1 ? threadIdx.x : threadIdx.x & 255, lds);
-    feed.whole /= TEAMS;
-    feed.first += team * feed.whole * kDepth;
+    const uint32_t share = feed.whole / TEAMS;  // steps of a team, one behind the other; what is left goes round
+    feed.first += team * share * kDepth;
+    feed.whole = feed.readable ? share : 0;
     const OperandPlaces<kIn, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
     const OperandPlaces<kOut, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
     f32x16 sum[kIn][kOut] = {};
@@ -338,8 +340,8 @@ __global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(co
         }
         if (n < feed.whole) step(n, 0);
     }
-    for (uint32_t all = first + TEAMS * feed.whole * kDepth; all < last; all += TEAMS * kDepth) {
-        const uint32_t t = all + team * kDepth;
+    for (uint32_t n = feed.whole; first + TEAMS * n * kDepth < last; ++n) {
+        const uint32_t t = n < share ? feed.first + n * kDepth : first + (TEAMS * n + team) * kDepth;
         __syncthreads();
         if (t < last) feed.bring_asking(t);
         __syncthreads();
@@ -426,6 +428,7 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
     const uint32_t lane = threadIdx.x & 63, i_wave = (threadIdx.x >> 6 & 1) * 128, o_wave = (threadIdx.x >> 7) * 128;
     Feed feed(dy, codes, exponents, s, i0, o0, first, last, threadIdx.x, lds);
+    if (!feed.readable) feed.whole = 0;
     const OperandPlaces<4, Feed::kInBytes> from_in(lds, lane, i_wave / 16);
     const OperandPlaces<4, Feed::kOutBytes> from_out(lds + Feed::kInPlane, lane, o_wave / 16);
     using Operands = s16x8[4][2];
