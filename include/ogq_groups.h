@@ -98,7 +98,8 @@ int ogq_activation_backward(const void* d_dy, size_t dy_stride, const void* d_co
 /* The gradient of a linear layer's weights from the gradient of its outputs and its checkpointed inputs (8 bits):
  *   dw[o][i] = sum over the rows t of dy[t][o] * x^[t][i],  0 <= o < outs, 0 <= i < cols,
  * or that added to what dw holds (accumulate != 0).  Products are exact (fp32 gradients are cut into three pieces of bf16, in which
- * what a value has below 2^-133 is lost), sums are held in fp32 in an order that the sizes alone decide.  For fp16 gradients the checkpoint is one of an fp16 tensor.
+ * what a value has below 2^-133 is lost), sums are held in fp32 in an order that the sizes alone decide.  The checkpoint may be one of any type; fp16 gradients are multiplied
+ * fastest where its exponents are an fp16 tensor's (-24 .. 9): tiles of sums that meet others are made again, as products of bf16 in an order of their own.
  * d_workspace: ogq_weight_gradient_workspace bytes, 16-byte aligned, may be NULL where that is 0. */
 size_t ogq_weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params);
 int ogq_weight_gradient(const void* d_dy, size_t dy_stride, uint32_t dtype, const void* d_codes, const uint8_t* d_exponents,

@@ -31,6 +31,23 @@ struct Rows16 {
         else load_some<T, 16>(from, valid, raw);
     }
     __device__ __forceinline__ void store(char* to, int) const { memcpy(to, raw, 32); }
+    // fp16 in two pieces of bf16, whose sum each value is.
+    __device__ __forceinline__ void store_split(char* to, int plane) const
+    {
+        T v[16];
+        memcpy(v, raw, 32);
+        uint32_t w[2][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t a[3], b[3];
+            split3((float)v[2 * i], a[0], a[1], a[2]);
+            split3((float)v[2 * i + 1], b[0], b[1], b[2]);
+#pragma unroll
+            for (int p = 0; p < 2; ++p) w[p][i] = __builtin_amdgcn_perm(b[p], a[p], 0x07060302u);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) memcpy(to + p * plane, w[p], 32);
+    }
 };
 template <>
 struct Rows16<float> {
@@ -79,6 +96,9 @@ __device__ __forceinline__ void store_codes(const uint4& codes, uint32_t byte, c
     }
     memcpy(to, w, 32);
 }
+
+// An fp16 tensor's exponents as bytes: the lowest, and how far behind it the others are.  What a group with another one holds (NaN among it) may lie outside of fp16.
+constexpr uint32_t kHalfLow = ExponentLimits<_Float16, 8>::kLow + 127, kHalfSpan = ExponentLimits<_Float16, 8>::kHigh - ExponentLimits<_Float16, 8>::kLow;
 
 template <int ROW_BYTES>
 __device__ __forceinline__ s16x8 read_transposed(const char* at)
@@ -140,6 +160,7 @@ struct Feeder {
     uint32_t whole;  // steps that are there in all rows
     bool readable;   // whether these can be read without asking
     bool has_codes;
+    uint64_t outside = 0;  // fp16: the lanes that have brought a group whose exponent is none of an fp16 tensor (in scalar registers)
     int valid;
     char *in_to, *out_to;
     Rows16<T> g[SETS][kOutUnits];
@@ -183,7 +204,11 @@ struct Feeder {
         const uint32_t t = first + min(n, whole - 1) * kDepth + kOutRows * u;
         g[set][u].load(dy + t * dy_stride + at_dy);
     }
-    __device__ __forceinline__ void bring_codes(uint32_t stage, int set, int u) { store_codes<T>(q[set][u], byte[set][u], in_to + stage * kStage + u * kInRows * kInBytes); }
+    __device__ __forceinline__ void bring_codes(uint32_t stage, int set, int u)
+    {
+        store_codes<T>(q[set][u], byte[set][u], in_to + stage * kStage + u * kInRows * kInBytes);
+        if constexpr (__is_same(T, _Float16)) outside |= __builtin_amdgcn_ballot_w64(byte[set][u] - kHalfLow > kHalfSpan);
+    }
     __device__ __forceinline__ void bring_dy(uint32_t stage, int set, int u) { g[set][u].store(out_to + stage * kStage + u * kOutRows * kOutBytes, kOutPlane); }
     __device__ __forceinline__ void fetch(uint32_t n, int set)
     {
@@ -199,8 +224,8 @@ struct Feeder {
 #pragma unroll
         for (int u = 0; u < kInUnits; ++u) bring_codes(stage, set, u);
     }
-    // Rows t ... of any step, what is not there as 0, to the first stage.
-    __device__ __forceinline__ void bring_asking(uint32_t t)
+    // Rows t ... of any step, what is not there as 0, on their way.
+    __device__ __forceinline__ void fetch_asking(uint32_t t)
     {
 #pragma unroll
         for (int u = 0; u < kInUnits; ++u) {
@@ -217,7 +242,21 @@ struct Feeder {
             const uint32_t mine = t + out_row + kOutRows * u;
             g[0][u].load(dy + mine * dy_stride + o_mine, mine < last ? valid : 0);
         }
+    }
+    __device__ __forceinline__ void bring_asking(uint32_t t)
+    {
+        fetch_asking(t);
         bring(0, 0);
+    }
+    // The same for fp16 gradients and any checkpoint: both factors as bf16, dy in two pieces.
+    static_assert(kInPlane + 2 * kOutPlane <= SETS * kStage || !__is_same(T, _Float16));
+    __device__ __forceinline__ void bring_split(uint32_t t)
+    {
+        fetch_asking(t);
+#pragma unroll
+        for (int u = 0; u < kOutUnits; ++u) g[0][u].store_split(out_to + u * kOutRows * kOutBytes, kOutPlane);
+#pragma unroll
+        for (int u = 0; u < kInUnits; ++u) store_codes<__bf16>(q[0][u], byte[0][u], in_to + u * kInRows * kInBytes);
     }
 };
 
@@ -234,6 +273,39 @@ struct OperandPlaces {
     // Operand n of the upper or lower 16 rows of a step, `bytes` behind the plane that the places are in.
     __device__ __forceinline__ s16x8 read(int n, int half, uint32_t bytes) const { return read_transposed<ROW_BYTES>(at[n] + bytes + half * 16 * ROW_BYTES); }
 };
+
+// The sums of a wavefront again, for fp16 gradients and a checkpoint that holds what fp16 does not (one of a bf16 or fp32 tensor): as products of bf16, of which dy takes two.  All of the
+// workgroup's threads call it where one has met such a group; nothing of what they hold but the tile is needed, so that the usual way keeps its registers.
+template <class FEED, int TEAMS, int NI, int NO>
+__device__ __forceinline__ void sums_of_any_checkpoint(const _Float16* dy, const uint8_t* codes, const uint8_t* exponents, const GradientShape& s, uint32_t i0, uint32_t o0,
+                                                       uint32_t first, uint32_t last, uint32_t thread, uint32_t team, char* lds, f32x16 (&sum)[NI][NO])
+{
+    asm("" : "+v"(thread));  // (the places below are made here, not held since the start)
+    FEED feed(dy, codes, exponents, s, i0, o0, first, last, thread, lds);
+    const OperandPlaces<NI, FEED::kInBytes> from_in(lds, thread & 63, (thread >> 6 & 1) * NI * 2);
+    const OperandPlaces<NO, FEED::kOutBytes> from_out(lds + FEED::kInPlane, thread & 63, (thread >> 7) * NO * 2);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NO; ++j) sum[i][j] = f32x16{};
+    for (uint32_t t = first + team * kDepth; t < last + team * kDepth; t += TEAMS * kDepth) {
+        if (t < last) feed.bring_split(t);
+        __syncthreads();
+        if (t < last) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+                for (int p = 1; p >= 0; --p)
+#pragma unroll
+                    for (int j = 0; j < NO; ++j) {
+                        const s16x8 b = from_out.read(j, h, p * FEED::kOutPlane);
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) sum[i][j] = multiply_add32<__bf16>(from_in.read(i, h, 0), b, sum[i][j]);
+                    }
+        }
+        __syncthreads();
+    }
+}
 
 // The sums of a wavefront, 32 * NI inputs from i and 32 * NO outputs from o, to dw or the workspace.  A lane holds pieces of 16 bytes of one row; through LDS (`space`, 4608
 // bytes of the wavefront's own) eight lanes get the 128 bytes of one, so that lines are written whole.
@@ -274,12 +346,14 @@ __device__ __forceinline__ void store_tile(const f32x16 (&sum)[NI][NO], uint32_t
 // one: 2048 x 2048 sums of 8192 rows in bf16 91 us, 755 TFLOP/s; fp32, whose three products count: the same 250 us, 825 TFLOP/s, and 4096 x 4096 of 4096 rows in tiles of 256 x 128 345 us, 1190 TFLOP/s;
 // 4096 x 25088 of 256 rows 180 us, 870 TFLOP/s beside 2.3 TB/s of sums written.
 template <class T, int IN, int OUT, int GROUPS, int TEAMS>
-__global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
+__global__ __launch_bounds__(256 * TEAMS, GROUPS * TEAMS) void weight_gradient_kernel(const T* dy, const uint8_t* codes, const uint8_t* exponents, GradientShape s,
                                                                               bool accumulate, float* out)
 {
     constexpr int kPieces = Rows16<T>::kPieces, kSets = kPieces == 1 || IN == kSmall ? 2 : 1, kIn = IN / 64, kOut = OUT / 64;
     using Feed = Feeder<T, IN, OUT, kSets>;
     __shared__ __align__(16) char all_lds[TEAMS * kSets * Feed::kStage];
+    __shared__ uint32_t any_outside;
+    if (__is_same(T, _Float16) && threadIdx.x == 0) any_outside = 0;
     const uint32_t tiles = s.tiles_in * s.tiles_out, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
     const uint32_t i0 = tile % s.tiles_in * IN, o0 = tile / s.tiles_in * OUT;  // (neighbours along a row of sums: 8192 x 16384 of 32 rows 97 us, 131 in tile_of's order)
     const uint32_t first = part * s.part, last = min(s.rows, first + s.part);
@@ -347,7 +421,10 @@ __global__ __launch_bounds__(256 * TEAMS, GROUPS) void weight_gradient_kernel(co
         __syncthreads();
         if (t < last) products(0);
     }
+    if (__is_same(T, _Float16) && feed.outside != 0) any_outside = 1;
     __syncthreads();
+    if constexpr (__is_same(T, _Float16))
+        if (any_outside != 0) sums_of_any_checkpoint<Feed, TEAMS>(dy, codes, exponents, s, i0, o0, first, last, (wave & 3) * 64 + lane, team, lds, sum);
     char* space = all_lds + wave * kTurnBytes;
     if constexpr (TEAMS == 1) {
         store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, space);
@@ -422,6 +499,8 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
     static_assert(Rows16<T>::kPieces == 1);
     using Feed = Feeder<T, kLarge, kLarge, 2>;
     __shared__ __align__(16) char lds[2 * Feed::kStage];
+    __shared__ uint32_t any_outside;
+    if (__is_same(T, _Float16) && threadIdx.x == 0) any_outside = 0;
     const uint32_t tiles = s.tiles_in * s.tiles_out, part = blockIdx.x / tiles;
     const uint2 tile = tile_of(blockIdx.x % tiles, s.tiles_in, s.tiles_out);
     const uint32_t i0 = tile.x * kLarge, o0 = tile.y * kLarge;
@@ -512,7 +591,10 @@ __global__ __launch_bounds__(256, 1) void large_weight_gradient_kernel(const T* 
         for (int eighth = 0; eighth < 8; ++eighth) products(a, b, eighth);
         __syncthreads();
     }
+    if (__is_same(T, _Float16) && feed.outside != 0) any_outside = 1;
     __syncthreads();
+    if constexpr (__is_same(T, _Float16))
+        if (any_outside != 0) sums_of_any_checkpoint<Feed, 1>(dy, codes, exponents, s, i0, o0, first, last, threadIdx.x, 0, lds, sum);
     store_tile(sum, i0 + i_wave, o0 + o_wave, lane, s, accumulate, out + part * s.out_part, lds + (threadIdx.x >> 6) * kTurnBytes);
 }
 

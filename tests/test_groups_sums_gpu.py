@@ -35,3 +35,25 @@ def test_the_order_of_a_gradients_sum_does_not_depend_on_strides(dtype, rows, ou
         assert torch.equal(ogq.ogq_weight_gradient(view, codes, exponents, cols, p), first), name
     one = dy[rows // 3:rows // 3 + 1].expand(rows, outs)
     assert torch.equal(ogq.ogq_weight_gradient(one, codes, exponents, cols, p), ogq.ogq_weight_gradient(one.contiguous(), codes, exponents, cols, p))
+
+
+# ----------------------------------------------------------------------------------------------------------------------
+# fp16 gradients
+# ----------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,outs,cols", [(1, 16, 32), (40, 48, 96), (33, 200, 333), (200, 10, 1000), (129, 257, 129), (4100, 33, 65), (1300, 140, 150), (641, 4100, 2570)])
+@pytest.mark.parametrize("held_as", ["bf16", "fp32"])
+def test_fp16_gradients_with_a_checkpoint_of_another_type(held_as, rows, outs, cols):
+    """Inputs beyond what fp16 holds, at both ends, beside ordinary ones."""
+    p = ogq.make_group_params(32, 8)
+    x = values(rows, cols, torch.float32, 1)
+    powers = torch.tensor([2.0 ** 20, 1.0, 2.0 ** -30, 2.0 ** 8, 2.0 ** 60, 2.0 ** -100])
+    for n, column in enumerate(range(0, cols, 32)):
+        x[:, column:column + 32] *= float(powers[n % 6])
+    x[rows // 2, :32] = 3.0 * 2.0 ** 12  # (one group of a column alone)
+    codes, exponents = ogq.ogq_group_quantize(x.to(TYPES[held_as]), p)
+    dy = values(rows, outs, torch.float16, 2, scale=0.05)
+    check_gradient(dy, codes, exponents, cols, p, "other type")
+    x = values(rows, cols, torch.float32, 1) * 0.01
+    x[-1, -1] = 1e6  # one value in the whole checkpoint
+    codes, exponents = ogq.ogq_group_quantize(x.to(TYPES[held_as]), p)
+    check_gradient(dy, codes, exponents, cols, p, "one group")
