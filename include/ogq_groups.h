@@ -27,6 +27,8 @@
  *   - d_codes must be 16-byte aligned; values (d_x, d_y and so on) need the alignment of their type.
  *   - A tensor of values has consecutive values in a row and `stride` values from one row to the next: at least cols for
  *     outputs, any for inputs (0: the same row again and again).
+ *   - Rows and columns are below 2^31, rows * (columns + 127) of every tensor below 2^40; of sums, outs * cols and (for more than one token) tokens * outs below 2^38 and 2^37 in whole
+ *     tiles of 128 x 128 and 64 x 128.  Else OGQ_ERR_SIZE.
  *   - Outputs overlap neither inputs nor each other.
  *   - A tensor without values (0 rows or 0 columns) is a successful no-op, apart from sums over nothing, which are 0.
  *   - A call with a workspace may be two launches; where the runtime refuses the second, the first is enqueued all the same.

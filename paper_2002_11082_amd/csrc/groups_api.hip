@@ -40,7 +40,7 @@ int check_params(const ogq_group_params_t* p, uint32_t bits)
     return OGQ_OK;
 }
 
-// Sizes for which every offset fits 64 bits and every grid 31.
+// Sizes for which every offset fits 64 bits and the pieces of a tensor 31 bits of workgroups.
 int check_size(size_t rows, size_t cols)
 {
     constexpr size_t kMost = (size_t)1 << 31;
@@ -79,6 +79,23 @@ int first_of(std::initializer_list<int> checks)
 }
 
 int check_dtype(uint32_t dtype) { return dtype <= OGQ_FP16 ? OGQ_OK : OGQ_ERR_DTYPE; }
+
+// The least tiles that the kernels for sums cut `a` by `b` of them into, `wide` of b to one, to workgroups of 256 threads in one dimension: 2^32 threads are too many for a launch.
+int check_tiles(size_t a, size_t b, size_t wide)
+{
+    return (a + 127) / 128 * ((b + wide - 1) / wide) < ((size_t)1 << 24) ? OGQ_OK : OGQ_ERR_SIZE;
+}
+
+int check_gradient(size_t rows, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params)
+{
+    return first_of({check_params(params, 8), check_dtype(dtype), check_size(rows, cols), check_size(rows, outs), check_size(outs, cols), check_tiles(outs, cols, 128)});
+}
+
+int check_product(size_t tokens, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params)
+{
+    return first_of({check_params(params, 4), check_dtype(dtype), check_size(outs, cols), check_size(tokens, cols), check_size(tokens, outs),
+                     tokens > 1 ? check_tiles(outs, tokens, 64) : OGQ_OK});
+}
 
 // As in ogq.h: the status is the one the runtime returned for this call's launches.
 void begin_launches() { ogq::launch_status() = hipSuccess; }
@@ -176,7 +193,7 @@ int ogq_activation_backward(const void* d_dy, size_t dy_stride, const void* d_co
 
 size_t ogq_weight_gradient_workspace(size_t rows, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params)
 {
-    if (first_of({check_params(params, 8), check_dtype(dtype), check_size(rows, cols), check_size(rows, outs), check_size(outs, cols)}) != OGQ_OK) return 0;
+    if (check_gradient(rows, outs, cols, dtype, params) != OGQ_OK) return 0;
     if (outs == 0 || cols == 0) return 0;
     return ogq::weight_gradient_workspace(rows, outs, cols, dtype);
 }
@@ -185,7 +202,7 @@ int ogq_weight_gradient(const void* d_dy, size_t dy_stride, uint32_t dtype, cons
                         size_t outs, size_t cols, const ogq_group_params_t* params, int accumulate, float* d_dw, size_t dw_stride,
                         void* d_workspace, size_t workspace_bytes, void* hip_stream)
 {
-    int rc = first_of({check_params(params, 8), check_dtype(dtype), check_size(rows, cols), check_size(rows, outs), check_size(outs, cols)});
+    int rc = check_gradient(rows, outs, cols, dtype, params);
     if (rc != OGQ_OK) return rc;
     if (outs == 0 || cols == 0 || (rows == 0 && accumulate)) return OGQ_OK;
     rc = check_result(d_dw, dw_stride, outs, cols, OGQ_FP32);
@@ -207,7 +224,7 @@ int ogq_weight_gradient(const void* d_dy, size_t dy_stride, uint32_t dtype, cons
 
 size_t ogq_group_matvec_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, const ogq_group_params_t* params)
 {
-    if (first_of({check_params(params, 4), check_dtype(dtype), check_size(outs, cols), check_size(tokens, cols), check_size(tokens, outs)}) != OGQ_OK) return 0;
+    if (check_product(tokens, outs, cols, dtype, params) != OGQ_OK) return 0;
     if (tokens == 0 || outs == 0) return 0;
     return ogq::group_matvec_workspace(tokens, outs, cols, dtype);
 }
@@ -216,7 +233,7 @@ int ogq_group_matvec(const void* d_codes, const uint8_t* d_exponents, size_t out
                      size_t x_stride, size_t tokens, uint32_t dtype, void* d_y, size_t y_stride, void* d_workspace, size_t workspace_bytes,
                      void* hip_stream)
 {
-    int rc = first_of({check_params(params, 4), check_dtype(dtype), check_size(outs, cols), check_size(tokens, cols), check_size(tokens, outs)});
+    int rc = check_product(tokens, outs, cols, dtype, params);
     if (rc != OGQ_OK) return rc;
     if (tokens == 0 || outs == 0) return OGQ_OK;
     rc = check_result(d_y, y_stride, tokens, outs, dtype);

@@ -19,6 +19,18 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// HIP takes less than 2^32 threads along a dimension of a grid: more than 2^22 workgroups go to rows of 2^22.  The last row is as long as the others: its workgroups behind the last
+// one have nothing to do.
+constexpr uint32_t kGridRowLog2 = 22;
+
+inline dim3 grid_of_blocks(uint64_t blocks)
+{
+    constexpr uint64_t kRow = (uint64_t)1 << kGridRowLog2;
+    return blocks <= kRow ? dim3((uint32_t)blocks) : dim3((uint32_t)kRow, (uint32_t)((blocks + kRow - 1) >> kGridRowLog2));
+}
+
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y << kGridRowLog2 | blockIdx.x; }
+
 // The types of ogq_dtype_t.
 template <uint32_t DTYPE>
 struct ValueOf;

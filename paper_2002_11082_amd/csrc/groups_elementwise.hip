@@ -85,7 +85,7 @@ constexpr int kItems = sizeof(T) == 4 ? 2 : 1;
 template <class T>
 __device__ __forceinline__ uint64_t piece_of(int item)
 {
-    return ((uint64_t)blockIdx.x * kItems<T> + item) * kBlock + threadIdx.x;
+    return ((uint64_t)block_number() * kItems<T> + item) * kBlock + threadIdx.x;
 }
 
 // Bound by memory: 8192 x 4096 of bf16 into 8 bits 20.0 us, 5.1 TB/s read and written (a copy reaches 4.85); 4096 x 25088 of fp32 into 4 bits 78 us, 6.0 TB/s; one row of 4096
@@ -311,7 +311,7 @@ template <class T>
 dim3 grid_of(const Pieces& s)
 {
     constexpr uint32_t kEach = kItems<T> * kBlock;
-    return dim3((uint32_t)((s.total + kEach - 1) / kEach));
+    return grid_of_blocks((s.total + kEach - 1) / kEach);
 }
 
 // f(a value's type, whether a tensor is larger than the eight 4 MB caches of the chip together): such a one is read and written past them (4096 x 25088 of fp32

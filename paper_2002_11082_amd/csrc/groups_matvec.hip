@@ -168,7 +168,8 @@ __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* 
     __shared__ float parts[kFew][kFew * NT];
     __shared__ uint4 turn[kTurned ? kFew : 1][kTurned ? 64 * kLaneWords<T> / 4 : 1];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), teams = blockDim.x / (64 * s.team);
-    const uint32_t o0 = (blockIdx.x * teams + wave / s.team) * kFew;
+    const uint32_t first_out = block_number() * teams * kFew, o0 = first_out + wave / s.team * kFew;
+    if (first_out >= s.outs) return;
     const uint32_t pitch = s.groups << s.group_log2;
     float sum[kFew * NT] = {};
     for (uint32_t chunk = wave % s.team; chunk < s.steps; chunk += s.team) {
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(64 * kFew) void group_matvec_kernel(const uint8_t* 
     parts[wave][index] = sum[0];  // (several lanes write the same)
     __syncthreads();
     if (threadIdx.x < teams * kFew * NT) {
-        const uint32_t r = threadIdx.x / NT, t = threadIdx.x % NT, o = blockIdx.x * teams * kFew + r, first = r / kFew * s.team, at = threadIdx.x % (kFew * NT);
+        const uint32_t r = threadIdx.x / NT, t = threadIdx.x % NT, o = first_out + r, first = r / kFew * s.team, at = threadIdx.x % (kFew * NT);
         if (o >= s.outs || t >= s.tokens) return;
         float all = parts[first][at];
         for (uint32_t k = 1; k < s.team; ++k) all += parts[first + k][at];
@@ -498,7 +499,7 @@ void launch_of(const Groups& w, MatvecShape s, const T* x, uint32_t dtype, T* y,
         s.team = rounds ? ceil_div(s.steps, rounds) : 1;
         // Several teams to a workgroup where 512 workgroups are left: one token in fp32, 1 and 4 teams: 16384 x 1024 8.0 and 5.7 us, 8192 x 1024 5.2 and 4.2, 2048 x 1024 3.2 and 3.8.
         const uint32_t teams = min(kFew / s.team, max(1u, ceil_div(s.outs, kFew) / 512));
-        launch_few(dim3(ceil_div(s.outs, kFew * teams)), dim3(64 * s.team * teams), codes, w.exponents, x, s, y, st);
+        launch_few(grid_of_blocks(ceil_div(s.outs, kFew * teams)), dim3(64 * s.team * teams), codes, w.exponents, x, s, y, st);
         return;
     }
     const Plan p = plan_of(s.tokens, s.outs, s.cols, dtype);
