@@ -12,7 +12,7 @@ import torch
 
 import paper_2002_11082_amd as ogq
 from tests import groups_reference as ref
-from tests.test_groups_gpu import ACTS, DEV, ROUNDING, TYPES, say
+from tests.test_groups_gpu import ACTS, DEV, ROUNDING, TYPES, near, same, say, slack_of, values
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -86,3 +86,44 @@ def test_slopes_of_all_values(dtype, act):
     dx, dup = ogq.ogq_activation_backward(one, ACTS[act], codes, exponents, p, up_codes, up_exponents)
     within(dx, slope, size, units, (dtype, act, "gated"))
     within(dup, value, value.abs(), units, (dtype, act, "dup"))
+
+
+# A tensor larger than the chip's caches is read and written past them, by kernels of their own: as one long row, and row by row.
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activations_larger_than_the_caches(dtype, gated):
+    t = TYPES[dtype]
+    for act, (rows, cols, group, pad) in zip(ACTS, ((4100, 4096, 64, 0), (2100, 8005, 128, 3), (8192, 2080, 32, 8), (4097, 4096, 128, 0))):
+        say("large activation", dtype, act, gated, rows, cols, group, pad)
+        p = ogq.make_group_params(group, 8)
+        x, up, dy = (values(rows, cols, t, k, pad, scale=s) for k, s in ((1, 2.0), (2, 1.0), (3, 0.01)))
+        if pad == 0:
+            x, up, dy = x.contiguous(), up.contiguous(), dy.contiguous()
+        held, u, held_up = ref.held(x, group, 8), 1.0, torch.ones(1, dtype=torch.float64, device=DEV)
+        if gated:
+            y, codes, exponents, up_codes, up_exponents = ogq.ogq_activation_forward(x, ACTS[act], p, up)
+            dx, dup = ogq.ogq_activation_backward(dy, ACTS[act], codes, exponents, p, up_codes, up_exponents)
+            u, held_up = up.double(), ref.held(up, group, 8)
+            same(ogq.ogq_group_dequantize(up_codes, up_exponents, cols, p, t), held_up, "up")
+        else:
+            y, codes, exponents = ogq.ogq_activation_forward(x, ACTS[act], p)
+            dx = ogq.ogq_activation_backward(dy, ACTS[act], codes, exponents, p)
+        same(ogq.ogq_group_dequantize(codes, exponents, cols, p, t), held, "x")
+        near(y, exact(act, x.double())[0] * u, slack_of(x.double(), u * x.double()), t, "y")
+        value, slope = exact(act, held)[:2]
+        near(dx, dy.double() * held_up * slope, slack_of(held, dy.double() * held_up), t, "dx")
+        if gated:
+            near(dup, dy.double() * value, slack_of(held, dy.double() * held), t, "dup")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_groups_larger_than_the_caches(dtype, bits):
+    t = TYPES[dtype]
+    for rows, cols, group, pad in ((4100, 4096, 64, 0), (2100, 8005, 128, 3), (8192, 2080, 32, 8)):
+        x = values(rows, cols, t, 1, pad)
+        x = x.contiguous() if pad == 0 else x
+        say("large groups", dtype, bits, rows, cols, group, pad)
+        p = ogq.make_group_params(group, bits)
+        codes, exponents = ogq.ogq_group_quantize(x, p)
+        same(ogq.ogq_group_dequantize(codes, exponents, cols, p, t), ref.held(x, group, bits), "held")
