@@ -31,16 +31,6 @@ inline dim3 grid_of_blocks(uint64_t blocks)
 
 __device__ __forceinline__ uint32_t block_number() { return blockIdx.y << kGridRowLog2 | blockIdx.x; }
 
-// The types of ogq_dtype_t.
-template <uint32_t DTYPE>
-struct ValueOf;
-template <>
-struct ValueOf<OGQ_FP32> { using type = float; };
-template <>
-struct ValueOf<OGQ_BF16> { using type = __bf16; };
-template <>
-struct ValueOf<OGQ_FP16> { using type = _Float16; };
-
 // The limits of a group's exponent: every q * 2^e is a value of T.
 template <class T, int BITS>
 struct ExponentLimits {
