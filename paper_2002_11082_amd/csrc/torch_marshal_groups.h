@@ -175,6 +175,12 @@ void call_library(const at::Tensor& on, F f)
     check_groups(status);
 }
 
+// A tensor of the caller has been written: autograd, which may have kept it for a backward pass, is told so.
+void written(PyObject* given, const at::Tensor& t)
+{
+    if (given != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject* pack(std::initializer_list<at::Tensor> tensors)
 {
     PyObject* all = PyTuple_New(static_cast<Py_ssize_t>(tensors.size()));
@@ -196,6 +202,7 @@ PyObject* group_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         void* codes = to.codes.data_ptr();
         uint8_t* exponents = to.exponents_out();
         call_library(x.t, [&](void* st) { return bound_groups.quantize(from, x.stride, x.rows, x.cols, x.dtype, &p, codes, exponents, st); });
+        written(args[2], to.codes), written(args[3], to.exponents);
         return pack({to.codes, to.exponents});
     });
 }
@@ -214,6 +221,7 @@ PyObject* group_dequantize(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         const void* codes = x.codes.const_data_ptr();
         void* to = out.out();
         call_library(out.t, [&](void* st) { return bound_groups.dequantize(codes, x.exponents_in(), x.rows, cols, &p, to, out.stride, out.dtype, st); });
+        written(args[5], out.t);
         return THPVariable_Wrap(out.t);
     });
 }
@@ -246,6 +254,8 @@ PyObject* activation_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs)
                 return bound_groups.forward(from, x.stride, up_from, up.stride, x.rows, x.cols, x.dtype, act, &p, out, y.stride, codes, exponents, up_codes,
                                             up_exponents, st);
             });
+        written(args[4], y.t), written(args[5], to.codes), written(args[6], to.exponents);
+        if (gated) written(args[7], up_to.codes), written(args[8], up_to.exponents);
         return gated ? pack({y.t, to.codes, to.exponents, up_to.codes, up_to.exponents}) : pack({y.t, to.codes, to.exponents});
     });
 }
@@ -282,6 +292,8 @@ PyObject* activation_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs
                 return bound_groups.backward(from, dy.stride, codes, x.exponents_in(), up_codes, up_exponents, dy.rows, dy.cols, dy.dtype, act, &p, out,
                                              dx.stride, up_out, dup.stride, st);
             });
+        written(args[7], dx.t);
+        if (gated) written(args[8], dup.t);
         return gated ? pack({dx.t, dup.t}) : THPVariable_Wrap(dx.t);
     });
 }
@@ -310,6 +322,7 @@ PyObject* weight_gradient(PyObject*, PyObject* const* args, Py_ssize_t nargs)
             return bound_groups.gradient(from, dy.stride, dy.dtype, codes, x.exponents_in(), dy.rows, dy.cols, cols, &p, accumulate, out, dw.stride,
                                          workspace, bytes, st);
         });
+        written(args[5], dw.t);
         return THPVariable_Wrap(dw.t);
     });
 }
@@ -334,6 +347,7 @@ PyObject* group_matvec(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         call_library(x.t, [&](void* st) {
             return bound_groups.matvec(codes, w.exponents_in(), w.rows, cols, &p, from, x.stride, x.rows, x.dtype, out, y.stride, workspace, bytes, st);
         });
+        written(args[5], y.t);
         return THPVariable_Wrap(y.t);
     });
 }

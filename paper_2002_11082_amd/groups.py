@@ -2,7 +2,11 @@
 them.  As in binding.py: argument marshalling only, the extension module _marshal for the calls on tensors (two dimensions, CUDA,
 float32, bfloat16 or float16, consecutive values in a row), work enqueued on torch's current stream, no CPU fallback.
 
-Codes are uint8 [rows, bytes of a row], exponents uint8 [rows, groups of a row]; see the header for what they stand for."""
+Codes are uint8 [rows, bytes of a row], exponents uint8 [rows, groups of a row]; see the header for what they stand for.
+
+None of the calls is differentiated: a tensor that requires a gradient is read like any other, and the results are not part of its graph.  A program calls the
+backward pass itself (checkpointed_block.py), or from a torch.autograd.Function.  Outputs of the caller that a call has written get a new version, so that autograd
+refuses a backward pass that had kept their old values."""
 from __future__ import annotations
 
 import ctypes
@@ -113,8 +117,8 @@ def ogq_group_dequantize(codes, exponents, cols: int, params: GroupParams, dtype
 
 def ogq_activation_forward(x, activation: int, params: GroupParams, up=None, y=None, codes=None, exponents=None, up_codes=None,
                            up_exponents=None):
-    """y = act(x), or act(x) * up; x (and up) are left in 8 bits for the backward pass.  activation: RELU, GELU, GELU_TANH or SILU.
-    Returns (y, codes, exponents), with up also (up_codes, up_exponents) behind them."""
+    """y = act(x), or act(x) * up; x (and up) are left in 8 bits for the backward pass, ogq_activation_backward (y is in no graph of autograd's).
+    activation: RELU, GELU, GELU_TANH or SILU.  Returns (y, codes, exponents), with up also (up_codes, up_exponents) behind them."""
     return (_marshal or _load_marshal()).activation_forward(x, activation, params, up, y, codes, exponents, up_codes, up_exponents)
 
 
