@@ -150,38 +150,42 @@ __device__ __forceinline__ void sigmoid(float x, float& s, float& rest)
 }
 
 // p = (1 + erf(x / sqrt(2))) / 2 without the difference that cancels for negative x, and g = exp(-x^2 / 2), which the slope has too.  With z = |x|, the smaller one of p and 1 - p is
-// R(z) * g, where R(z) = exp(z^2 / 2) * erfc(z / sqrt(2)) / 2 falls slowly from 1/2 like 1 / z: t times a polynomial of t = 1 / (1 + 0.3 z), whose coefficients are least squares of the
-// relative error on 0 <= z <= 16, weighted until it was even.  EXACT: nine steps, off by 2^-28, and the exponential of x^2 with what its rounding leaves; otherwise seven, off by 2^-22.
+// R(z) * g, where R(z) = exp(z^2 / 2) * erfc(z / sqrt(2)) / 2 falls slowly from 1/2 like 1 / z: t times a polynomial of t = 1 / (1 + c z), whose coefficients are least squares of the
+// relative error up to z = 16, weighted until it was even.  16 bits: seven steps, off by 2^-22.  EXACT: six for z >= 1, off by 2^-23.3, and the exponential of x^2 with what its rounding
+// leaves; for z < 1, where p and 1 - p are alike, 1/2 + x times a polynomial of x^2, found in the same way, off by 2^-31, which has fewer roundings.
 template <bool EXACT>
 __device__ __forceinline__ void normal_distribution(float x, float& p, float& g)
 {
-    float t, r;
     if constexpr (EXACT) {
         const float z = fminf(fabsf(x), 16.0f), square = z * z;  // (exp(-128) is below the least number)
         g = exp_of(-0.5f * square, -0.5f * __builtin_fmaf(z, z, -square));
-        t = reciprocal(__builtin_fmaf(z, 0.3f, 1.0f));
-        r = __builtin_fmaf(-0.020629964768886566f, t, 0.11247210204601288f);
-        r = __builtin_fmaf(r, t, -0.22830256819725037f);
-        r = __builtin_fmaf(r, t, 0.1919078826904297f);
-        r = __builtin_fmaf(r, t, -0.07953041791915894f);
-        r = __builtin_fmaf(r, t, 0.09621681272983551f);
-        r = __builtin_fmaf(r, t, 0.0783679336309433f);
-        r = __builtin_fmaf(r, t, 0.11024031043052673f);
-        r = __builtin_fmaf(r, t, 0.11957119405269623f);
-        r = __builtin_fmaf(r, t, 0.11968672275543213f);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(z, 0.4f, 1.0f));
+        float r = __builtin_fmaf(0.06771772354841232f, t, -0.18541577458381653f);
+        r = __builtin_fmaf(r, t, 0.10434761643409729f);
+        r = __builtin_fmaf(r, t, 0.05605988949537277f);
+        r = __builtin_fmaf(r, t, 0.13886022567749023f);
+        r = __builtin_fmaf(r, t, 0.1591196209192276f);
+        r = __builtin_fmaf(r, t, 0.15959471464157104f);
+        const float smaller = r * t * g;
+        float c = __builtin_fmaf(-7.66467837820528e-06f, square, 0.00011351265129633248f);
+        c = __builtin_fmaf(c, square, -0.0011863530380651355f);
+        c = __builtin_fmaf(c, square, 0.009973331354558468f);
+        c = __builtin_fmaf(c, square, -0.06649035960435867f);
+        c = __builtin_fmaf(c, square, 0.3989422917366028f);
+        p = z < 1.0f ? __builtin_fmaf(x, c, 0.5f) : x < 0.0f ? smaller : 1.0f - smaller;
     } else {
         g = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
-        t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(x), 0.3f, 1.0f));
-        r = __builtin_fmaf(0.034704964607954025f, t, -0.15318746864795685f);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(x), 0.3f, 1.0f));
+        float r = __builtin_fmaf(0.034704964607954025f, t, -0.15318746864795685f);
         r = __builtin_fmaf(r, t, 0.19948841631412506f);
         r = __builtin_fmaf(r, t, -0.04742685705423355f);
         r = __builtin_fmaf(r, t, 0.12529200315475464f);
         r = __builtin_fmaf(r, t, 0.10088922083377838f);
         r = __builtin_fmaf(r, t, 0.12060054391622543f);
         r = __builtin_fmaf(r, t, 0.1196390762925148f);
+        const float smaller = r * t * g;
+        p = x < 0.0f ? smaller : 1.0f - smaller;
     }
-    const float smaller = r * t * g;
-    p = x < 0.0f ? smaller : 1.0f - smaller;
 }
 
 constexpr float kTanhScale = 0.797884560802865f, kCubic = 0.044715f;  // sqrt(2 / pi)
@@ -197,20 +201,20 @@ __device__ __forceinline__ void activation(float x, float& value, float& slope)
         float s, rest;
         sigmoid<EXACT>(x, s, rest);
         value = x * s;
-        slope = s * (1.0f + x * rest);
+        slope = s * __builtin_fmaf(x, rest, 1.0f);
     } else if constexpr (ACT == OGQ_GELU) {
         float p, g;
         normal_distribution<EXACT>(x, p, g);
         value = x * p;
-        slope = p + x * (0.398942280401433f * g);
+        slope = __builtin_fmaf(x, 0.398942280401433f * g, p);
     } else {
         // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)).  The square is limited: behind 100 the slope's second term is 0, where an infinite square
         // would make it NaN.
         const float square = fminf(x * x, 10000.0f);
         float s, rest;
-        sigmoid<EXACT>(2.0f * kTanhScale * x * (1.0f + kCubic * square), s, rest);
+        sigmoid<EXACT>(2.0f * kTanhScale * x * __builtin_fmaf(kCubic, square, 1.0f), s, rest);
         value = x * s;
-        slope = s + x * s * rest * 2.0f * kTanhScale * (1.0f + 3.0f * kCubic * square);
+        slope = __builtin_fmaf(x * s * rest, 2.0f * kTanhScale * __builtin_fmaf(3.0f * kCubic, square, 1.0f), s);
     }
 }
 
