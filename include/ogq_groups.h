@@ -83,7 +83,7 @@ int ogq_group_dequantize(const void* d_codes, const uint8_t* d_exponents, size_t
 /* The forward pass of an activation, which leaves what the backward pass needs in 8 bits:
  *   y = act(x), or y = act(x) * up where d_up is given,
  * from the values as they are, and x (and up) in groups.  Computed in fp32 and rounded once: fp32 results are off by 12 to 16 roundings
- * (gelu_tanh: and 8 |x + 0.045 x^3| more), for 16 bits the value that is rounded is off by 2^-15 of itself and may be 0 below 2^-119.  d_up, d_up_codes and
+ * (gelu_tanh: and 13 |x + 0.045 x^3| more), for 16 bits the value that is rounded is off by 2^-15 of itself and may be 0 below 2^-119.  d_up, d_up_codes and
  * d_up_exponents are all given or all NULL. */
 int ogq_activation_forward(const void* d_x, size_t x_stride, const void* d_up, size_t up_stride, size_t rows, size_t cols,
                            uint32_t dtype, uint32_t activation, const ogq_group_params_t* params, void* d_y, size_t y_stride,
