@@ -1,4 +1,4 @@
-"""Builds libogq.so and libogq_groups.so (HIP kernels + C ABI) for gfx950 with hipcc, and _marshal.so (the extension module
+"""Builds libogq.so, libogq_groups.so and libogq_layers.so (HIP kernels + C ABI) for gfx950 with hipcc, and _marshal.so (the extension module
 that hands torch tensors to them) with g++.  Run: python -m paper_2002_11082_amd.build
 
 The libraries are compiled as several object files in parallel (the random-rounding kernels once per bucket
@@ -19,6 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libogq.so")
 GROUPS_LIB = os.path.join(PKG, "libogq_groups.so")
+LAYERS_LIB = os.path.join(PKG, "libogq_layers.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 
 HIPCC_FLAGS = [
@@ -38,6 +39,7 @@ UNITS = [("rounding_part.hip", [f"-DOGQ_PART={part}"], f"rounding_{part}.o") for
     ("api.hip", [], "api.o"),
 ]
 GROUPS_UNITS = [(f"groups_{part}.hip", [], f"groups_{part}.o") for part in ("gradient", "elementwise", "matvec", "api")]
+LAYERS_UNITS = [(f"layers_{part}.hip", [], f"layers_{part}.o") for part in ("linear", "few", "norm", "distill", "embedding", "api")]
 
 
 def _run(cmd, verbose):
@@ -61,16 +63,16 @@ def _marshal_command():
 
 def build(verbose: bool = False, jobs: int = 0) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    units = UNITS + GROUPS_UNITS
+    units = UNITS + GROUPS_UNITS + LAYERS_UNITS
     jobs = jobs or max(1, min(len(units), os.cpu_count() or 1, int(os.environ.get("MAX_JOBS", "16"))))
     shutil.rmtree(OBJ, ignore_errors=True)
     os.makedirs(OBJ)
-    objects = {LIB: [], GROUPS_LIB: []}
+    objects = {LIB: [], GROUPS_LIB: [], LAYERS_LIB: []}
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as pool:
         futures = []
         for src, extra, obj in units:
             out = os.path.join(OBJ, obj)
-            objects[GROUPS_LIB if src.startswith("groups_") else LIB].append(out)
+            objects[GROUPS_LIB if src.startswith("groups_") else LAYERS_LIB if src.startswith("layers_") else LIB].append(out)
             futures.append(pool.submit(_run, [hipcc, *HIPCC_FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", out], verbose))
         futures.append(pool.submit(_run, _marshal_command(), verbose))
         for f in futures:

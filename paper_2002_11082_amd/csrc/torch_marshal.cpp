@@ -2,7 +2,7 @@
 // ogq_quantize and ogq_dequantize_average do for every call, without the interpreter.  It checks the tensors (the kernels
 // trust their sizes), allocates the outputs the caller left out, and calls the library through the addresses that
 // binding.py hands to bind(); nothing of the path runs here and nothing links against libogq.  The calls of ogq_groups.h are
-// in torch_marshal_groups.h.
+// in torch_marshal_groups.h, those of ogq_layers.h in torch_marshal_layers.h.
 //
 // Why native: a call is one kernel launch (2.3 us on the host), and for gradients below about a million elements the
 // kernels take less than what the same checks cost in Python with ctypes (n = 1728, host time per call: quantize
@@ -24,6 +24,7 @@
 
 #include "ogq.h"
 #include "ogq_groups.h"
+#include "ogq_layers.h"
 
 namespace {
 
@@ -293,6 +294,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 }
 
 #include "torch_marshal_groups.h"
+#include "torch_marshal_layers.h"
 
 template <class F>
 PyCFunction as_method(F f)
@@ -311,6 +313,15 @@ PyMethodDef methods[] = {
     {"activation_backward", as_method(activation_backward), METH_FASTCALL, "ogq_activation_backward on tensors; after bind_groups()"},
     {"weight_gradient", as_method(weight_gradient), METH_FASTCALL, "ogq_weight_gradient on tensors; after bind_groups()"},
     {"group_matvec", as_method(group_matvec), METH_FASTCALL, "ogq_group_matvec on tensors; after bind_groups()"},
+    {"bind_layers", as_method(bind_layers), METH_FASTCALL, "the entry points of ogq_layers.h and their check"},
+    {"layer_norm_forward", as_method(layer_norm_forward), METH_FASTCALL, "ogq_layer_norm_forward on tensors; after bind_layers()"},
+    {"layer_norm_backward", as_method(layer_norm_backward), METH_FASTCALL, "ogq_layer_norm_backward on tensors; after bind_layers()"},
+    {"linear", as_method(linear), METH_FASTCALL, "ogq_linear on tensors; after bind_layers()"},
+    {"linear_backward", as_method(linear_backward), METH_FASTCALL, "ogq_linear_backward on tensors; after bind_layers()"},
+    {"embedding_forward", as_method(embedding_forward), METH_FASTCALL, "ogq_embedding_forward on tensors; after bind_layers()"},
+    {"embedding_gradient", as_method(embedding_gradient), METH_FASTCALL, "ogq_embedding_gradient on tensors; after bind_layers()"},
+    {"distill_loss", as_method(distill_loss), METH_FASTCALL, "ogq_distill_loss on tensors; after bind_layers()"},
+    {"distill_gradient", as_method(distill_gradient), METH_FASTCALL, "ogq_distill_gradient on tensors; after bind_layers()"},
     {nullptr, nullptr, 0, nullptr},
 };
 
