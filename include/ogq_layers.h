@@ -18,7 +18,7 @@
  *   - d_workspace: as many bytes as the size helper beside the entry point says, 16-byte aligned, may be NULL where that is 0.  Its contents before the call do not matter.  Calls that may
  *     run at the same time, replays of captured graphs among them, need workspaces of their own.
  *   - A call may be several launches; where the runtime refuses one, those before it are enqueued all the same.
- *   - Sums are held in fp32 (or more) in an order that the sizes alone decide: results are the same from call to call.  Values are rounded once, to the type of the output.
+ *   - Sums are held in fp32 (or more) in an order that the sizes alone decide (and the tokens, where a text below says so): results are the same from call to call.  Values are rounded once, to the type of the output.
  */
 #ifndef OGQ_LAYERS_H
 #define OGQ_LAYERS_H
@@ -78,7 +78,8 @@ int ogq_embedding_forward(const void* d_tokens, uint32_t integer, size_t tokens,
                           void* d_y, size_t y_stride, void* hip_stream);
 
 /* The table's gradient [vocab, cols] in fp32, dtable[v] = scale * sum of dy[t] over the t with token[t] = v (0 where there is none), or that added to what dtable holds.  Tokens outside
- * of the table have no part in it.  The rows of a token are added in their order in groups that their number alone decides.  tokens below 2^30. */
+ * of the table have no part in it.  The rows of a token are added in their order, in groups that all of the tokens
+ * decide.  tokens below 2^30. */
 size_t ogq_embedding_gradient_workspace(size_t tokens, size_t vocab, size_t cols);
 int ogq_embedding_gradient(const void* d_tokens, uint32_t integer, size_t tokens, const void* d_dy, size_t dy_stride, size_t vocab, size_t cols, uint32_t dtype, float scale,
                            int accumulate, float* d_dtable, size_t dtable_stride, void* d_workspace, size_t workspace_bytes, void* hip_stream);

@@ -9,6 +9,18 @@
 
 namespace ogq {
 
+// HIP takes less than 2^32 threads along a dimension of a grid: more than 2^20 workgroups, of up to 1024 threads, go to rows of 2^20.  The last row is as long as the others: its workgroups
+// behind the last one have nothing to do.
+constexpr uint32_t kRowOfBlocksLog2 = 20;
+
+inline dim3 grid_of(uint64_t blocks)
+{
+    constexpr uint64_t kRow = (uint64_t)1 << kRowOfBlocksLog2;
+    return blocks <= kRow ? dim3((uint32_t)blocks) : dim3((uint32_t)kRow, (uint32_t)((blocks + kRow - 1) >> kRowOfBlocksLog2));
+}
+
+__device__ __forceinline__ uint32_t this_block() { return blockIdx.y << kRowOfBlocksLog2 | blockIdx.x; }
+
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 // Two sums over a workgroup of WAVES wavefronts, in all of its threads: across lanes, then the wavefronts' in their order.  `space` is used by the next call but one.

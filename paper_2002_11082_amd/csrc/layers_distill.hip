@@ -43,7 +43,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
     __shared__ float weight_of[GRADIENT ? kMostTop : 1];
     BlockSums<kWaves> sums{space};
     const uint32_t thread = threadIdx.x;
-    const uint64_t row = block_number();
+    const uint64_t row = this_block();
     if (row >= s.rows) return;
     const T* from = logits + row * s.stride;
     T* to = GRADIENT ? dlogits + row * s.out_stride : nullptr;
@@ -216,7 +216,7 @@ void launch_distill(const Values& logits, size_t rows, size_t cols, uint32_t dty
         const auto go = [&](auto gradient) {
             constexpr bool kGradient = decltype(gradient)::value;
             const auto kernel = shape.threads == 256 ? kernel_of<T, kGradient, 256>(shape.pieces) : kernel_of<T, kGradient, 1024>(shape.pieces);
-            launch_kernel(kernel, grid_of_blocks(rows), dim3(shape.threads), st, static_cast<const T*>(logits.data), s, static_cast<T*>(dlogits.data));
+            launch_kernel(kernel, grid_of(rows), dim3(shape.threads), st, static_cast<const T*>(logits.data), s, static_cast<T*>(dlogits.data));
         };
         if (dlogits.data != nullptr) go(std::true_type{});
         else go(std::false_type{});

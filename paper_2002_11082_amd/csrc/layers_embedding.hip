@@ -1,7 +1,8 @@
 // libogq_layers: rows of a table by tokens, and the table's gradient.
 //
 // The gradient's rows are sums over equal tokens.  The tokens are sorted with their positions first, so that a sum has its rows one behind the other, in their order, whatever the
-// order in which workgroups come: keys of 64 bits, the token above the position, no two of them alike.  Bound by memory: the table's gradient is written once, most of it zeros.
+// order in which workgroups come: keys of 64 bits, the token above the position, no two of them alike.  A wavefront then adds the rows of 64 neighbouring keys, so that a frequent token
+// is as much work as many rare ones.  Bound by memory: the table's gradient is written once, most of it zeros, behind which the sorting hides.
 #include "layers_common.h"
 
 namespace ogq {
@@ -10,7 +11,7 @@ namespace {
 
 constexpr uint32_t kRun = 1024;   // keys that a workgroup sorts
 constexpr uint32_t kWays = 32;    // sorted runs that a launch makes one of
-constexpr uint32_t kGroup = 64;   // rows of a token, where it has at least two such groups, that are summed on their own; the last group has up to twice as many, less one
+constexpr uint32_t kWindow = 64;  // neighbouring keys whose rows a wavefront adds
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // Token n, or kNone where it names no row.
@@ -26,7 +27,7 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(const void* tokens, b
                                                          uint32_t threads_log2, float scale, T* y, uint64_t y_stride)
 {
     constexpr int N = kPiece<T>, kAhead = 2;
-    const uint64_t row = ((uint64_t)block_number() << (8 - threads_log2)) + (threadIdx.x >> threads_log2);
+    const uint64_t row = ((uint64_t)this_block() << (8 - threads_log2)) + (threadIdx.x >> threads_log2);
     if (row >= number) return;
     const uint32_t threads = 1u << threads_log2, thread = threadIdx.x & (threads - 1), token = token_of(tokens, wide, row, vocab);
     const T* from = table + (uint64_t)(token == kNone ? 0 : token) * table_stride;
@@ -59,11 +60,42 @@ __device__ __forceinline__ uint32_t count_below(const uint64_t* run, uint32_t le
     return below;
 }
 
-// 1024 keys to a workgroup: every wavefront places its 64 by counting, then a key's place among all is its own place and what the other fifteen have below it.
-__global__ __launch_bounds__(kRun) void sort_runs_kernel(const void* tokens, bool wide, uint32_t number, uint32_t vocab, uint64_t* keys)
+// Zeros for the table's gradient: rows of `length` values in units of kUnit, `units` of them to a row (one row where the table has no gaps).
+constexpr uint32_t kUnit = 16384;
+struct Fill {
+    float* to;
+    uint64_t length, stride, units, first, last;  // units first ... last of all rows' are this launch's
+};
+
+__device__ __forceinline__ void fill_unit(const Fill& f, uint64_t unit)
+{
+    const uint64_t row = f.units == 1 ? unit : unit / f.units, begin = (unit - row * f.units) * kUnit;
+    float* to = f.to + row * f.stride + begin;
+    const uint64_t left = f.length - begin;
+    const f32x4 zero = {};
+#pragma unroll
+    for (uint32_t n = 0; n < kUnit / 4 / kRun; ++n) {
+        const uint32_t at = (n * kRun + threadIdx.x) * 4;
+        if (at + 4 <= left) {
+            memcpy(to + at, &zero, sizeof zero);
+        } else {
+            for (uint32_t i = at; i < at + 4; ++i)
+                if (i < left) to[i] = 0.0f;
+        }
+    }
+}
+
+// The first `runs` workgroups sort 1024 keys each: every wavefront places its 64 by counting, then a key's place among all is its own place and what the other fifteen have below it.
+// The others fill.
+__global__ __launch_bounds__(kRun) void sort_runs_kernel(const void* tokens, bool wide, uint32_t number, uint32_t vocab, uint32_t runs, uint64_t* keys, Fill fill)
 {
     __shared__ uint64_t sorted[kRun];
-    const uint32_t position = blockIdx.x * kRun + threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (this_block() >= runs) {
+        const uint64_t unit = fill.first + (this_block() - runs);
+        if (unit < fill.last) fill_unit(fill, unit);
+        return;
+    }
+    const uint32_t position = this_block() * kRun + threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // (behind the last token: keys above all others)
     const uint32_t token = position < number ? token_of(tokens, wide, position, vocab) : kNone;
     uint64_t key = (uint64_t)token << 32 | position;
@@ -80,14 +112,20 @@ __global__ __launch_bounds__(kRun) void sort_runs_kernel(const void* tokens, boo
 #pragma unroll
     for (uint32_t w = 0; w < kRun / 64; ++w)
         if (w != wave) place += count_below(sorted + w * 64, 64, 7, key);
-    keys[blockIdx.x * kRun + place] = key;
+    keys[this_block() * kRun + place] = key;
 }
 
-// Runs of `run` sorted keys into runs of kWays times as many: a key's place is its own and what the other runs have below it.  `total` is a multiple of kRun.
-__global__ __launch_bounds__(kBlock) void merge_runs_kernel(const uint64_t* from, uint64_t* to, uint32_t total, uint32_t run, uint32_t run_log2)
+// Runs of `run` sorted keys into runs of kWays times as many: a key's place is its own and what the other runs have below it.  `total` is a multiple of kRun.  The workgroups behind
+// those that the keys need fill.
+__global__ __launch_bounds__(kRun) void merge_runs_kernel(const uint64_t* from, uint64_t* to, uint32_t total, uint32_t run, uint32_t run_log2, Fill fill)
 {
-    const uint32_t at = blockIdx.x * kBlock + threadIdx.x;  // (all of a workgroup's are of one run)
-    const uint32_t mine = (blockIdx.x * kBlock) >> run_log2, base = mine / kWays * kWays;
+    if (this_block() >= total / kRun) {
+        const uint64_t unit = fill.first + (this_block() - total / kRun);
+        if (unit < fill.last) fill_unit(fill, unit);
+        return;
+    }
+    const uint32_t at = this_block() * kRun + threadIdx.x;  // (all of a workgroup's are of one run)
+    const uint32_t mine = (this_block() * kRun) >> run_log2, base = mine / kWays * kWays;
     const uint64_t key = from[at];
     uint32_t place = at - (mine << run_log2);
     // eight searches at a time, whose loads are under way together
@@ -115,14 +153,6 @@ __global__ __launch_bounds__(kBlock) void merge_runs_kernel(const uint64_t* from
     to[((uint64_t)base << run_log2) + place] = key;
 }
 
-// starts[v]: the first key of token v or one above it, for v = 0 ... vocab.
-__global__ __launch_bounds__(kBlock) void starts_kernel(const uint64_t* keys, uint32_t number, uint32_t vocab, uint32_t* starts)
-{
-    const uint64_t v = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (v > vocab) return;
-    starts[v] = count_below(keys, number, 32 - __builtin_clz(number), v << 32);
-}
-
 // The columns of a lane: a piece of a row, which lies as PieceAt says where the row has as many values.
 template <class T>
 struct Piece {
@@ -131,148 +161,161 @@ struct Piece {
     bool whole;
     __device__ __forceinline__ Piece(uint32_t col, uint32_t cols) : at(col, max(cols, (uint32_t)kPiece<T>)), valid(valid_of<T>(col, cols)), whole(cols >= kPiece<T>) {}
     __device__ __forceinline__ bool there() const { return valid > 0; }
-    __device__ __forceinline__ void add(const T* row, float (&sum)[kPiece<T>]) const
+    __device__ __forceinline__ uint4 load(const T* row) const { return whole ? load_whole(row + at.col) : load_raw(row, valid); }
+    __device__ __forceinline__ uint32_t col() const { return whole ? at.col : 0; }
+    // A row of the table's gradient, of which a lane has these values.  Added to what is there, the ones that the last piece has twice count once.
+    template <bool ACCUMULATE>
+    __device__ __forceinline__ void store(float* row, float scale, const float (&sum)[kPiece<T>]) const
     {
-        float v[kPiece<T>];
-        values_of<T>(whole ? load_whole(row + at.col) : load_raw(row, valid), v);
+        constexpr int N = kPiece<T>;
+        if (!there()) return;
+        float v[N];
 #pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) sum[i] += v[i];
+        for (int i = 0; i < N; ++i) v[i] = sum[i] * scale;
+        float* out = row + col();
+        if (whole && (!ACCUMULATE || at.again == 0)) {
+            if constexpr (ACCUMULATE) {
+                float old[N];
+                memcpy(old, out, sizeof old);
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] += old[i];
+            }
+            memcpy(out, v, sizeof v);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (whole ? at.counts(i) : i < valid) out[i] = ACCUMULATE ? out[i] + v[i] : v[i];
     }
 };
 
-// The rows of keys first ... last, added one after the other.  All of the wavefront's lanes call it.
-template <class T>
-__device__ __forceinline__ void add_rows(const uint64_t* keys, uint32_t first, uint32_t last, const T* dy, uint64_t dy_stride, const Piece<T>& piece, float (&sum)[kPiece<T>])
-{
-    const uint32_t lane = threadIdx.x & 63;
-    for (uint32_t at = first; at < last; at += 64) {
-        const uint32_t here = min(64u, last - at), mine = (uint32_t)keys[at + min(lane, here - 1)];
-        uint32_t n = 0;
-        for (; n + 8 <= here; n += 8) {
-            float v[8][kPiece<T>];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-#pragma unroll
-                for (int i = 0; i < kPiece<T>; ++i) v[k][i] = 0.0f;
-                piece.add(dy + (uint64_t)__builtin_amdgcn_readlane(mine, n + k) * dy_stride, v[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-#pragma unroll
-                for (int i = 0; i < kPiece<T>; ++i) sum[i] += v[k][i];
-        }
-        for (; n < here; ++n) piece.add(dy + (uint64_t)__builtin_amdgcn_readlane(mine, n) * dy_stride, sum);
-    }
-}
-
 struct Table {
-    uint32_t number, vocab, cols, blocks, pitch;  // blocks: of 64 pieces, along a row
-    uint64_t dy_stride;
+    uint32_t number, cols, blocks, pitch;  // blocks: of 64 pieces, along a row
+    uint64_t dy_stride, dtable_stride;
     float scale;
 };
 
-// The groups of tokens that have two or more of them.  A token's groups begin kGroup keys apart, so that of kGroup keys at most one begins a group, and a wavefront that looks at these
-// keys sums it: sums[n] is the group that begins among keys n * kGroup ...
-template <class T>
-__global__ __launch_bounds__(kBlock) void add_groups_kernel(const uint64_t* keys, const uint32_t* starts, const T* dy, Table s, float* sums)
+// The token of a key, kNone for what is not there.
+__device__ __forceinline__ uint32_t token_at(const uint64_t* keys, uint32_t number, uint64_t at) { return at < number ? (uint32_t)(keys[at] >> 32) : kNone; }
+
+// kWindow neighbouring keys to a wavefront: the rows of each token among them are added one after the other.  A token whose keys all lie here is finished; of the others (the first one may have begun
+// before, the last one may go on) the sums wait for the next kernel, sums[2 n] of one that had begun before window n, sums[2 n + 1] of one that begins there.
+template <class T, bool ACCUMULATE>
+__global__ __launch_bounds__(kBlock) void add_windows_kernel(const uint64_t* keys, const T* dy, Table s, float* sums, float* dtable)
 {
-    const uint64_t unit = (uint64_t)block_number() * 4 + (threadIdx.x >> 6);
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t slot = unit / s.blocks;
-    if (slot * kGroup >= s.number) return;
-    const uint32_t at = (uint32_t)(slot * kGroup) + lane;
-    bool begins = false;
-    uint32_t last = 0;
-    if (at < s.number) {
-        const uint32_t token = (uint32_t)(keys[at] >> 32);
-        if (token != kNone) {
-            const uint32_t first = starts[token], end = starts[token + 1], group = (at - first) / kGroup, groups = (end - first) / kGroup;
-            begins = groups >= 2 && (at - first) % kGroup == 0 && group < groups;
-            last = group + 1 == groups ? end : at + kGroup;
+    constexpr int N = kPiece<T>, kAhead = 8;
+    const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), window = unit / s.blocks;
+    if (window * kWindow >= s.number) return;
+    const uint32_t lane = threadIdx.x & 63, first = (uint32_t)window * kWindow;
+    const uint64_t key = first + lane < s.number ? keys[first + lane] : ~0ull;
+    const uint32_t token = (uint32_t)(key >> 32), position = (uint32_t)key;
+    const uint32_t before = window == 0 ? kNone : token_at(keys, s.number, first - 1), behind = token_at(keys, s.number, (uint64_t)first + kWindow);
+    const uint32_t here = __builtin_popcountll(__builtin_amdgcn_ballot_w64(token != kNone));  // (keys of no token are the last ones)
+    if (here == 0) return;
+    const uint32_t left = __shfl_up(token, 1);
+    const uint64_t begins = __builtin_amdgcn_ballot_w64(lane == 0 || token != left);
+    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * N, s.cols);
+    uint4 next[kAhead];
+    const auto fetch = [&](uint32_t n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) next[k] = piece.load(dy + (uint64_t)__builtin_amdgcn_readlane(position, min(n + k, here - 1)) * s.dy_stride);
+    };
+    float sum[N];
+    fetch(0);
+    for (uint32_t n = 0; n < here; n += kAhead) {
+        uint4 now[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) now[k] = next[k];
+        fetch(n + kAhead);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const uint32_t at = n + k;
+            if (at >= here) break;
+            const bool begin = begins >> at & 1, end = at + 1 == here || (begins >> (at + 1) & 1);
+            float v[N];
+            values_of<T>(now[k], v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = begin ? v[i] : sum[i] + v[i];
+            if (!end) continue;
+            const uint32_t mine = __builtin_amdgcn_readlane(token, at);
+            // (whether its first key here is the window's first, and of a token that the key before names)
+            const bool begun = mine == before && mine == (uint32_t)__builtin_amdgcn_readfirstlane(token), goes_on = at + 1 == kWindow && mine == behind;
+            if (!begun && !goes_on) {
+                piece.template store<ACCUMULATE>(dtable + (uint64_t)mine * s.dtable_stride, s.scale, sum);
+            } else if (piece.there()) {
+                memcpy(sums + (2 * window + (begun ? 0 : 1)) * s.pitch + piece.col(), sum, sizeof sum);
+            }
         }
     }
-    const uint64_t which = __builtin_amdgcn_ballot_w64(begins);
-    if (which == 0) return;
-    const int leader = __builtin_ctzll(which);
-    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * kPiece<T>, s.cols);
-    float sum[kPiece<T>] = {};
-    add_rows(keys, __builtin_amdgcn_readlane(at, leader), __builtin_amdgcn_readlane(last, leader), dy, s.dy_stride, piece, sum);
-    if (!piece.there()) return;
-    float* out = sums + slot * s.pitch + (piece.whole ? piece.at.col : 0);
-    memcpy(out, sum, sizeof sum);
 }
 
-// A row of the table's gradient, 64 pieces of it, to a wavefront: zeros, the sum of its rows, or the sum of its groups.
+// The tokens whose keys lie in several windows: the wavefront of the window in which a token's last key lies adds the sums of its windows, in their order.
 template <class T, bool ACCUMULATE>
-__global__ __launch_bounds__(kBlock) void table_gradient_kernel(const uint64_t* keys, const uint32_t* starts, const T* dy, Table s, const float* sums, float* dtable,
-                                                              uint64_t dtable_stride)
+__global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* keys, Table s, const float* sums, float* dtable)
 {
     constexpr int N = kPiece<T>;
-    const uint64_t unit = (uint64_t)block_number() * 4 + (threadIdx.x >> 6), token = unit / s.blocks;
-    if (token >= s.vocab) return;
-    const uint32_t first = __builtin_amdgcn_readfirstlane(starts[token]), last = __builtin_amdgcn_readfirstlane(starts[token + 1]);
-    if (ACCUMULATE && first == last) return;
-    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + (threadIdx.x & 63)) * N, s.cols);
-    float sum[N] = {};
-    const uint32_t groups = (last - first) / kGroup;
-    if (groups >= 2) {
-        const float* from = sums + (uint64_t)(first / kGroup) * s.pitch + (piece.whole ? piece.at.col : 0);
-#pragma unroll 4
-        for (uint32_t n = 0; n < groups; ++n) {
-            float v[N];
-            memcpy(v, from + (uint64_t)n * s.pitch, sizeof v);
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] += v[i];
+    const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), window = unit / s.blocks + 1;
+    if (window * kWindow >= s.number) return;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t first = window * kWindow;
+    const uint32_t token = token_at(keys, s.number, first);
+    if (token == kNone || token != token_at(keys, s.number, first - 1) || token == token_at(keys, s.number, first + kWindow)) return;
+    // the windows before this one into which the token had gone on: the nearest that the key before does not name is where it begins
+    uint64_t begin = window;
+    for (;;) {
+        const uint64_t at = begin - 1 - lane;  // (one below 0 is none)
+        const bool on = begin >= 1 + (uint64_t)lane && at != 0 && token_at(keys, s.number, at * kWindow - 1) == token;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(on);
+        if (~all == 0) {
+            begin -= 64;
+            continue;
         }
-    } else if (first != last) {
-        add_rows(keys, first, last, dy, s.dy_stride, piece, sum);
+        begin -= 1 + __builtin_ctzll(~all);
+        break;
     }
+    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * N, s.cols);
     if (!piece.there()) return;
-    float* out = dtable + token * dtable_stride + (piece.whole ? piece.at.col : 0);
+    float sum[N];
+    memcpy(sum, sums + (2 * begin + 1) * s.pitch + piece.col(), sizeof sum);
+#pragma unroll 8
+    for (uint64_t n = begin + 1; n <= window; ++n) {
+        float v[N];
+        memcpy(v, sums + 2 * n * s.pitch + piece.col(), sizeof v);
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] *= s.scale;
-    if (piece.whole && piece.at.again == 0) {
-        if (ACCUMULATE) {
-            float old[N];
-            memcpy(old, out, sizeof old);
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] += old[i];
-        }
-        memcpy(out, sum, sizeof sum);
-        return;
+        for (int i = 0; i < N; ++i) sum[i] += v[i];
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (piece.whole ? piece.at.counts(i) : i < piece.valid) out[i] = ACCUMULATE ? out[i] + sum[i] : sum[i];
+    piece.template store<ACCUMULATE>(dtable + (uint64_t)token * s.dtable_stride, s.scale, sum);
 }
 
 // The gradient of no tokens.
-__global__ __launch_bounds__(kBlock) void zero_table_kernel(float* dtable, uint64_t stride, uint32_t rows, uint32_t cols)
+__global__ __launch_bounds__(kRun) void fill_kernel(Fill fill)
 {
-    const uint64_t unit = (uint64_t)block_number(), blocks = (cols + kBlock * 4 - 1) / (kBlock * 4), row = unit / blocks;
-    if (row >= rows) return;
-    const uint32_t col = (uint32_t)(unit % blocks * kBlock + threadIdx.x) * 4;
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i)
-        if (col + i < cols) dtable[row * stride + col + i] = 0.0f;
+    if (this_block() < fill.last) fill_unit(fill, this_block());
 }
 
 // What lies where in the workspace.
 struct Space {
-    size_t keys, starts, sums, bytes;  // bytes of one of two buffers of keys, of starts, of the groups' sums, of all
+    size_t keys, sums, bytes;  // bytes of one of two buffers of keys, of the windows' sums, of all
 };
 
-size_t whole16(size_t n) { return (n + 15) / 16 * 16; }
 size_t pitch_of(size_t cols) { return (cols + 7) / 8 * 8; }
 
-Space space_of(size_t number, size_t vocab, size_t cols)
+Space space_of(size_t number, size_t cols)
 {
     Space s;
     s.keys = ceil_div(number, kRun) * kRun * sizeof(uint64_t);
-    s.starts = whole16((vocab + 1) * sizeof(uint32_t));
-    s.sums = number >= 2 * kGroup ? ceil_div(number, kGroup) * pitch_of(cols) * sizeof(float) : 0;
-    s.bytes = 2 * s.keys + s.starts + s.sums;
+    s.sums = number > kWindow ? 2 * ceil_div(number, kWindow) * pitch_of(cols) * sizeof(float) : 0;
+    s.bytes = (number > kRun ? 2 : 1) * s.keys + s.sums;
     return s;
+}
+
+Fill fill_of(const Result& dtable, size_t vocab, size_t cols)
+{
+    const bool gaps = dtable.stride != cols && vocab > 1;
+    Fill f{static_cast<float*>(dtable.data), gaps ? cols : vocab * cols, dtable.stride, 0, 0, 0};
+    f.units = ceil_div(f.length, kUnit);
+    f.last = f.units * (gaps ? vocab : 1);
+    return f;
 }
 
 }  // namespace
@@ -285,44 +328,55 @@ void launch_embedding_forward(const Integers& tokens, size_t number, const Value
         const uint64_t pieces = ceil_div(cols, kPiece<T>);
         uint32_t log2 = 0;
         while (log2 < 8 && ((uint64_t)2 << log2) <= pieces) ++log2;
-        launch_kernel(embedding_kernel<T>, grid_of_blocks(ceil_div(number, kBlock >> log2)), dim3(kBlock), st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)number,
+        launch_kernel(embedding_kernel<T>, grid_of(ceil_div(number, kBlock >> log2)), dim3(kBlock), st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)number,
                       static_cast<const T*>(table.data), table.stride, (uint32_t)vocab, (uint32_t)cols, log2, scale, static_cast<T*>(y.data), y.stride);
     });
 }
 
-size_t embedding_gradient_workspace(size_t number, size_t vocab, size_t cols) { return space_of(number, vocab, cols).bytes; }
+size_t embedding_gradient_workspace(size_t number, size_t, size_t cols) { return space_of(number, cols).bytes; }
 
 void launch_embedding_gradient(const Integers& tokens, size_t number, const Values& dy, size_t vocab, size_t cols, uint32_t dtype, float scale, bool accumulate,
                                const Result& dtable, void* workspace, hipStream_t st)
 {
     float* out = static_cast<float*>(dtable.data);
+    const Fill fill = fill_of(dtable, vocab, cols);
     if (number == 0) {
-        launch_kernel(zero_table_kernel, grid_of_blocks(vocab * ceil_div(cols, kBlock * 4)), dim3(kBlock), st, out, dtable.stride, (uint32_t)vocab, (uint32_t)cols);
+        launch_kernel(fill_kernel, grid_of(fill.last), dim3(kRun), st, fill);
         return;
     }
-    const Space space = space_of(number, vocab, cols);
-    char* at = static_cast<char*>(workspace);
-    uint64_t *keys = reinterpret_cast<uint64_t*>(at), *other = reinterpret_cast<uint64_t*>(at + space.keys);
-    uint32_t* starts = reinterpret_cast<uint32_t*>(at + 2 * space.keys);
-    float* sums = reinterpret_cast<float*>(at + 2 * space.keys + space.starts);
+    const Space space = space_of(number, cols);
+    uint64_t *keys = static_cast<uint64_t*>(workspace), *other = keys + space.keys / sizeof(uint64_t);
     const uint32_t runs = (uint32_t)ceil_div(number, kRun), total = runs * kRun;
-    launch_kernel(sort_runs_kernel, dim3(runs), dim3(kRun), st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)number, (uint32_t)vocab, keys);
-    uint32_t log2 = 10;
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.bytes - space.sums);
+    // the launches that sort fill the table as well, each an equal part
+    uint32_t launches = 1;
+    for (uint64_t run = kRun; run < total; run *= kWays) ++launches;
+    const auto part = [&](uint32_t n) {
+        Fill f = fill;
+        f.first = fill.last * n / launches, f.last = fill.last * (n + 1) / launches;
+        if (accumulate) f.last = f.first;
+        return f;
+    };
+    Fill now = part(0);
+    launch_kernel(sort_runs_kernel, grid_of(runs + now.last - now.first), dim3(kRun), st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)number, (uint32_t)vocab, runs, keys,
+                  now);
+    uint32_t log2 = 10, n = 1;
     for (uint64_t run = kRun; run < total; run *= kWays, log2 += 5) {
-        launch_kernel(merge_runs_kernel, dim3(total / kBlock), dim3(kBlock), st, static_cast<const uint64_t*>(keys), other, total, (uint32_t)run, log2);
+        now = part(n++);
+        launch_kernel(merge_runs_kernel, grid_of(total / kRun + now.last - now.first), dim3(kRun), st, static_cast<const uint64_t*>(keys), other, total, (uint32_t)run, log2,
+                      now);
         std::swap(keys, other);
     }
-    launch_kernel(starts_kernel, dim3((uint32_t)ceil_div(vocab + 1, kBlock)), dim3(kBlock), st, static_cast<const uint64_t*>(keys), (uint32_t)number, (uint32_t)vocab, starts);
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
-        const Table s{(uint32_t)number, (uint32_t)vocab, (uint32_t)cols, blocks, (uint32_t)pitch_of(cols), dy.stride, scale};
-        const auto from = static_cast<const T*>(dy.data);
-        if (space.sums != 0)
-            launch_kernel(add_groups_kernel<T>, grid_of_blocks(ceil_div(ceil_div(number, kGroup) * blocks, 4)), dim3(kBlock), st, static_cast<const uint64_t*>(keys),
-                          static_cast<const uint32_t*>(starts), from, s, sums);
-        launch_kernel(accumulate ? table_gradient_kernel<T, true> : table_gradient_kernel<T, false>, grid_of_blocks(ceil_div((uint64_t)vocab * blocks, 4)), dim3(kBlock), st,
-                      static_cast<const uint64_t*>(keys), static_cast<const uint32_t*>(starts), from, s, static_cast<const float*>(sums), out, dtable.stride);
+        const Table s{(uint32_t)number, (uint32_t)cols, blocks, (uint32_t)pitch_of(cols), dy.stride, dtable.stride, scale};
+        const dim3 grid = grid_of(ceil_div(ceil_div(number, kWindow) * blocks, 4));
+        launch_kernel(accumulate ? add_windows_kernel<T, true> : add_windows_kernel<T, false>, grid, dim3(kBlock), st, static_cast<const uint64_t*>(keys),
+                      static_cast<const T*>(dy.data), s, sums, out);
+        if (number > kWindow)
+            launch_kernel(accumulate ? join_windows_kernel<T, true> : join_windows_kernel<T, false>, grid, dim3(kBlock), st, static_cast<const uint64_t*>(keys), s,
+                          static_cast<const float*>(sums), out);
     });
 }
 

@@ -12,7 +12,7 @@ __global__ __launch_bounds__(kBlock) void few_tokens_kernel(const T* x, const T*
 {
     constexpr int N = kPiece<T>;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = SPLIT == 1 ? 0 : wave;
-    const uint32_t first = (block_number() * (4 / SPLIT) + (SPLIT == 1 ? wave : 0)) * ROWS;
+    const uint32_t first = (this_block() * (4 / SPLIT) + (SPLIT == 1 ? wave : 0)) * ROWS;
     float sum[ROWS][TOKENS] = {};
     if (first < s.outs) {
         const T* rows[ROWS];
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kBlock) void few_tokens_across_kernel(const T* x, c
 {
     constexpr int N = kPiece<T>, kAhead = 8;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t block = block_number() % s.tiles_out, part = block_number() / s.tiles_out;
+    const uint32_t block = this_block() % s.tiles_out, part = this_block() / s.tiles_out;
     if (part >= s.parts) return;
     const uint32_t out = (block * 64 + lane) * N;
     const int valid = valid_of<T>(out, s.outs);
@@ -172,12 +172,12 @@ void launch_few(const FewPlan& plan, const T* x, const T* weight, bool transpose
         constexpr int kTokens = decltype(number)::value;
         if (s.tokens != kTokens) return;
         if (transposed) {
-            launch_kernel(few_tokens_across_kernel<T, kTokens>, grid_of_blocks((uint64_t)s.tiles_out * s.parts), dim3(kBlock), st, x, weight, s, e);
+            launch_kernel(few_tokens_across_kernel<T, kTokens>, grid_of((uint64_t)s.tiles_out * s.parts), dim3(kBlock), st, x, weight, s, e);
             return;
         }
-        if (plan.rows == 1) launch_kernel(few_tokens_kernel<T, kTokens, 1, 4>, grid_of_blocks(s.outs), dim3(kBlock), st, x, weight, s, e);
-        else if (plan.split == 4) launch_kernel(few_tokens_kernel<T, kTokens, 4, 4>, grid_of_blocks(ceil_div(s.outs, 4)), dim3(kBlock), st, x, weight, s, e);
-        else launch_kernel(few_tokens_kernel<T, kTokens, 4, 1>, grid_of_blocks(ceil_div(s.outs, 16)), dim3(kBlock), st, x, weight, s, e);
+        if (plan.rows == 1) launch_kernel(few_tokens_kernel<T, kTokens, 1, 4>, grid_of(s.outs), dim3(kBlock), st, x, weight, s, e);
+        else if (plan.split == 4) launch_kernel(few_tokens_kernel<T, kTokens, 4, 4>, grid_of(ceil_div(s.outs, 4)), dim3(kBlock), st, x, weight, s, e);
+        else launch_kernel(few_tokens_kernel<T, kTokens, 4, 1>, grid_of(ceil_div(s.outs, 16)), dim3(kBlock), st, x, weight, s, e);
     };
     go(std::integral_constant<int, 1>{}), go(std::integral_constant<int, 2>{}), go(std::integral_constant<int, 3>{}), go(std::integral_constant<int, 4>{});
     go(std::integral_constant<int, 5>{}), go(std::integral_constant<int, 6>{}), go(std::integral_constant<int, 7>{}), go(std::integral_constant<int, 8>{});

@@ -49,11 +49,15 @@ struct Chunk {
 };
 
 // ROWS rows along k of a factor: a step of each is a row in LDS, chunk c of row r at place(r, c), so that sixteen lanes that read chunk c of sixteen rows meet all banks.
-template <class T, int ROWS, int THREADS = 256>
+// NEAR: the rows of a tile lie within 2^32 bytes, and are held as one address and 32 bits to each.
+template <class T, int ROWS, bool NEAR>
 struct Along {
+    static constexpr int THREADS = 256;
     static constexpr int kChunks = kDepth<T> / 8, kRowBytes = kDepth<T> * 2, kPlane = ROWS * kRowBytes, kUnits = ROWS * kChunks / THREADS, kUnitRows = THREADS / kChunks;
     static_assert(kUnits * THREADS == ROWS * kChunks);
-    const T* rows[kUnits];
+    using Offset = std::conditional_t<NEAR, uint32_t, uint64_t>;
+    const T* data;          // the tile's first row
+    Offset offset[kUnits];  // of a thread's values in a step, in bytes
     uint32_t last, mine;
     char* to;
     Chunk<T> held[kUnits];
@@ -61,30 +65,43 @@ struct Along {
     static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk) { return row * kRowBytes + ((chunk ^ (row / (256 / kRowBytes) & (kChunks - 1))) * 16); }
 
     // Rows `first` ... of `number`; what lies behind the last row is any row that is there: its sums are not stored.
-    __device__ __forceinline__ Along(const T* data, uint64_t stride, uint32_t first, uint32_t number, uint32_t last_, uint32_t thread, char* lds) : last(last_)
+    __device__ __forceinline__ Along(const T* data_, uint64_t stride, uint32_t first, uint32_t number, uint32_t, uint32_t last_, uint32_t thread, char* lds)
+        : data(data_ + first * stride), last(last_)
     {
         const uint32_t row = thread / kChunks, chunk = thread % kChunks;
         mine = chunk * 8;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) rows[u] = data + (uint64_t)min(first + row + u * kUnitRows, number - 1) * stride + mine;
+        for (int u = 0; u < kUnits; ++u) offset[u] = ((Offset)min(row + u * kUnitRows, number - 1 - first) * (Offset)stride + mine) * sizeof(T);
         static_assert(kUnitRows % 16 == 0);  // (then place moves the chunks of all of a thread's rows alike)
         to = lds + place(row, chunk);
     }
+    // How many whole steps from `first` on can be fetched without asking.
+    __device__ __forceinline__ uint32_t readable(uint32_t first) const { return (last - first) / kDepth<T>; }
+    __device__ __forceinline__ const T* at(uint32_t k, int u) const { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(data + k) + offset[u]); }
+    __device__ __forceinline__ void fetch_unit(uint32_t k, int u) { held[u].load(at(k, u)); }
     __device__ __forceinline__ void fetch(uint32_t k)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) held[u].load(rows[u] + k);
+        for (int u = 0; u < kUnits; ++u) fetch_unit(k, u);
     }
+    __device__ __forceinline__ void fetch_unit_asking(uint32_t k, int u) { held[u].load(at(k, u), k + mine >= last ? 0 : (int)min(8u, last - k - mine)); }
     __device__ __forceinline__ void fetch_asking(uint32_t k)
     {
-        const int valid = k + mine >= last ? 0 : (int)min(8u, last - k - mine);
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) held[u].load(rows[u] + k, valid);
+        for (int u = 0; u < kUnits; ++u) fetch_unit_asking(k, u);
     }
+    __device__ __forceinline__ void bring_unit(uint32_t stage_bytes, int u) { held[u].store(to + stage_bytes + u * kUnitRows * kRowBytes, kPlane); }
     __device__ __forceinline__ void bring(uint32_t stage_bytes)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) held[u].store(to + stage_bytes + u * kUnitRows * kRowBytes, kPlane);
+        for (int u = 0; u < kUnits; ++u) bring_unit(stage_bytes, u);
+    }
+    // Where a lane finds its part of the first operand in 32 rows from `row` (a multiple of 32): the others lie kOperand bytes apart, and those of k = 16 h ... at this place ^ 32 h.
+    static constexpr int kOperand = 32 * kRowBytes;
+    static __device__ __forceinline__ uint32_t operand(uint32_t row, uint32_t lane) { return place(row + (lane & 31), lane >> 5); }
+    static __device__ __forceinline__ s16x8 read_operand(const char* lds, uint32_t at, uint32_t bytes, int n, int h)
+    {
+        return *reinterpret_cast<const s16x8*>(lds + (at ^ (32 * h)) + bytes + n * kOperand);
     }
     // Where a lane finds its part of an operand: 32 rows from `row`, k = 16 h + lane / 32 * 8 ...
     static __device__ __forceinline__ s16x8 read(const char* plane, uint32_t row, int h, uint32_t lane)
@@ -94,61 +111,79 @@ struct Along {
 };
 
 // The same for rows across k: a step is kDepth rows of COLS values, of which the columns are the operand's rows.  Chunk c (32 bytes) of row k lies at c ^ twist(k).
-template <class T, int COLS, int THREADS = 256>
+template <class T, int COLS, bool NEAR>
 struct Across {
+    static constexpr int THREADS = 256;
     static constexpr int kChunks = COLS / 16, kRowBytes = COLS * 2, kPlane = kDepth<T> * kRowBytes, kUnits = kDepth<T> * kChunks / THREADS, kUnitRows = THREADS / kChunks;
     static_assert(kUnits * THREADS == kDepth<T> * kChunks && kUnitRows % 4 == 0);
     const T* data;
     uint64_t stride;
+    std::conditional_t<NEAR, uint32_t, uint64_t> offset;  // of a thread's values in a step, in bytes
     uint32_t last, row, mine;
     int valid;
+    bool partial, whole_factor;
     char* to;
     Chunk<T> held[kUnits][2];
 
     static __device__ __forceinline__ uint32_t twist(uint32_t k) { return (k & (kChunks >= 8 ? 3u : 1u)) * 2u; }
 
-    // Columns `first` ... of `number`; what lies behind the last one is 0.
-    __device__ __forceinline__ Across(const T* data_, uint64_t stride_, uint32_t first, uint32_t number, uint32_t last_, uint32_t thread, char* lds)
+    // Columns `first` ... of `number`, rows below `last`, of which the factor has `rows`.  What lies behind the last column is any value that is there: its sums are not stored.
+    __device__ __forceinline__ Across(const T* data_, uint64_t stride_, uint32_t first, uint32_t number, uint32_t rows, uint32_t last_, uint32_t thread, char* lds)
         : data(data_), stride(stride_), last(last_)
     {
         const uint32_t chunk = thread % kChunks;
         row = thread / kChunks;
         mine = first + chunk * 16;
         valid = mine >= number ? 0 : (int)min(16u, number - mine);
+        partial = first + COLS > number && number % 16 != 0;
+        whole_factor = last_ == rows;
+        offset = (row * (decltype(offset))stride + (valid == 0 ? first : mine)) * sizeof(T);
         to = lds + row * kRowBytes + ((chunk ^ twist(row)) * 32);
     }
-    __device__ __forceinline__ void load(int u, uint32_t k)
+    // How many whole steps from `first` on can be fetched without asking: a thread whose sixteen columns reach beyond the last one reads on into the next row, which the last row does not have.
+    __device__ __forceinline__ uint32_t readable(uint32_t first) const
     {
-        const T* from = data + (uint64_t)k * stride + mine;
-        held[u][0].load(from, valid);
-        held[u][1].load(from + 8, valid - 8);
+        const uint32_t whole = (last - first) / kDepth<T>;
+        if (!partial || whole == 0) return whole;
+        if (stride < 16) return 0;
+        return whole_factor && first + whole * kDepth<T> == last ? whole - 1 : whole;
+    }
+    __device__ __forceinline__ void fetch_unit(uint32_t k, int u)
+    {
+        const T* from = reinterpret_cast<const T*>(reinterpret_cast<const char*>(data + (uint64_t)(k + u * kUnitRows) * stride) + offset);
+        held[u][0].load(from);
+        held[u][1].load(from + 8);
     }
     __device__ __forceinline__ void fetch(uint32_t k)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) load(u, k + row + u * kUnitRows);
+        for (int u = 0; u < kUnits; ++u) fetch_unit(k, u);
+    }
+    __device__ __forceinline__ void fetch_unit_asking(uint32_t k, int u)
+    {
+        const uint32_t at = k + row + u * kUnitRows;
+        const T* from = data + (uint64_t)at * stride + mine;
+        held[u][0].load(from, at < last ? valid : 0);
+        held[u][1].load(from + 8, at < last ? valid - 8 : 0);
     }
     __device__ __forceinline__ void fetch_asking(uint32_t k)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const uint32_t at = k + row + u * kUnitRows;
-            if (at < last) {
-                load(u, at);
-            } else {
-#pragma unroll
-                for (int i = 0; i < (int)(2 * sizeof(T)); ++i) held[u][0].raw[i] = held[u][1].raw[i] = 0;
-            }
-        }
+        for (int u = 0; u < kUnits; ++u) fetch_unit_asking(k, u);
+    }
+    __device__ __forceinline__ void bring_unit(uint32_t stage_bytes, int u)
+    {
+        held[u][0].store(to + stage_bytes + u * kUnitRows * kRowBytes, kPlane);
+        held[u][1].store(to + stage_bytes + u * kUnitRows * kRowBytes + 16, kPlane);
     }
     __device__ __forceinline__ void bring(uint32_t stage_bytes)
     {
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            held[u][0].store(to + stage_bytes + u * kUnitRows * kRowBytes, kPlane);
-            held[u][1].store(to + stage_bytes + u * kUnitRows * kRowBytes + 16, kPlane);
-        }
+        for (int u = 0; u < kUnits; ++u) bring_unit(stage_bytes, u);
     }
+    // (`at` of operands has no part for the columns: these move the chunks)
+    static __device__ __forceinline__ uint32_t operand(uint32_t col, uint32_t lane) { return col << 16 | lane; }
+    static __device__ __forceinline__ s16x8 read_operand(const char* lds, uint32_t at, uint32_t bytes, int n, int h) { return read(lds + bytes, (at >> 16) + 32 * n, h, at & 63); }
     static __device__ __forceinline__ s16x8 read(const char* plane, uint32_t col, int h, uint32_t lane)
     {
         typedef __attribute__((address_space(3))) s16x4* Lds;
@@ -256,8 +291,8 @@ __device__ __forceinline__ void each_pair(F f)
 template <class T, int OUT, int TOKENS, bool TRANSPOSED>
 __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
 {
-    using FeedW = std::conditional_t<TRANSPOSED, Across<T, OUT>, Along<T, OUT>>;
-    using FeedX = Along<T, TOKENS>;
+    using FeedW = std::conditional_t<TRANSPOSED, Across<T, OUT, false>, Along<T, OUT, false>>;
+    using FeedX = Along<T, TOKENS, false>;
     constexpr int kBytesW = kPlanes<T> * FeedW::kPlane, kStage = kBytesW + kPlanes<T> * FeedX::kPlane, NO = OUT / 64, NT = TOKENS / 64;
     constexpr int kBytes = kStage > 4 * kTurn<NO> ? kStage : 4 * kTurn<NO>;
     __shared__ __align__(16) char lds[kBytes];
@@ -265,11 +300,12 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
     const uint32_t tiles = s.tiles_out * s.tiles_token, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
     const uint32_t out = tile % s.tiles_out * OUT, token = tile / s.tiles_out * TOKENS, out_wave = (wave & 1) * (OUT / 2), token_wave = (wave >> 1) * (TOKENS / 2);
     const uint32_t first = part * s.part, last = min(s.cols, first + s.part);
-    FeedW feed_w(weight, s.weight_stride, out, s.outs, last, threadIdx.x, lds);
-    FeedX feed_x(x, s.x_stride, token, s.tokens, last, threadIdx.x, lds + kBytesW);
+    FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, last, threadIdx.x, lds);
+    FeedX feed_x(x, s.x_stride, token, s.tokens, s.cols, last, threadIdx.x, lds + kBytesW);
     f32x16 sum[NO][NT] = {};
+    const uint32_t whole = first + (first < last ? feed_w.readable(first) : 0) * kDepth<T>;  // the first column of a step that asks
     const auto fetch = [&](uint32_t k) __attribute__((always_inline)) {
-        if (k + kDepth<T> <= last) {
+        if (k < whole) {
             feed_w.fetch(k);
             feed_x.fetch(k);
         } else if (k < last) {
@@ -303,12 +339,152 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
     finish_tile<T>(sum, out + out_wave, token + token_wave, lane, s, part, e, lds + wave * kTurn<NO>);
 }
 
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, four along the outputs by eight along the tokens at a time.
+__device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_out, uint32_t tiles_token)
+{
+    constexpr uint32_t kXcds = 8, kWide = 4;
+    const uint32_t tiles = tiles_out * tiles_token, each = tiles / kXcds, more = tiles % kXcds, xcd = id % kXcds;
+    const uint32_t n = xcd * each + min(xcd, more) + id / kXcds;
+    const uint32_t panel = n / (kWide * tiles_token), rest = n % (kWide * tiles_token), width = min(kWide, tiles_out - panel * kWide);
+    return make_uint2(panel * kWide + rest % width, rest / width);
+}
+
+// The order of instructions in a quarter of a step: behind its sixteen products, which the matrix core takes 32 cycles for each, reads of operands, writes to LDS and loads in turn.
+template <int READS, int WRITES, int LOADS>
+__device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+        if (READS > 8 ? true : i % 2 == 0) {
+            if (i * READS / 16 < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+        }
+        if (i % 2 == 1 && i / 2 < WRITES) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS write
+        if (i % 2 == 1 && i / 2 < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // memory read
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles of 256 x 256 sums of 16-bit products, 128 x 128 in each of four wavefronts, one to a SIMD, which has all of its registers: 256 hold the sums.  A step of 64 columns is multiplied in four
+// quarters; while one is, the next one's operands come from LDS.  Two stages of LDS: the step behind the next one goes where the last one was, and the one behind that sets off from
+// memory.  One barrier a step, in front of the last quarter, which reads the next step's first operands.
+template <class T, bool TRANSPOSED>
+__global__ __launch_bounds__(256, 1) void large_linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
+{
+    static_assert(kPlanes<T> == 1);
+    using FeedW = std::conditional_t<TRANSPOSED, Across<T, 256, true>, Along<T, 256, true>>;
+    using FeedX = Along<T, 256, true>;
+    constexpr int kStage = FeedW::kPlane + FeedX::kPlane, kW = FeedW::kUnits, kX = FeedX::kUnits;
+    static_assert(kX == 8 && (kW == 8 || kW == 4) && 2 * kStage >= 4 * kTurn<4>);
+    __shared__ __align__(256) char lds[2 * kStage];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint2 tile = tile_of(blockIdx.x, s.tiles_out, s.tiles_token);
+    const uint32_t out = tile.x * 256, token = tile.y * 256, out_wave = (wave & 1) * 128, token_wave = (wave >> 1) * 128;
+    FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, s.cols, threadIdx.x, lds);
+    FeedX feed_x(x, s.x_stride, token, s.tokens, s.cols, s.cols, threadIdx.x, lds + FeedW::kPlane);
+    const uint32_t whole = feed_w.readable(0);
+    f32x16 sum[4][4] = {};
+    struct Operands {
+        s16x8 w[4], x[4];
+    };
+    uint32_t w_at = FeedW::operand(out_wave, lane), x_at = FeedX::operand(token_wave, lane);
+    const auto read = [&](Operands& r, uint32_t stage, int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = FeedW::read_operand(lds, w_at, stage * kStage, i, h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r.x[j] = FeedX::read_operand(lds, x_at, stage * kStage + FeedW::kPlane, j, h);
+    };
+    const auto products = [&](const Operands& r, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = from; i < to; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[i][j] = multiply_add<T>(r.w[i], r.x[j], sum[i][j]);
+    };
+    // (one behind the last whole step is the last one again, and not used)
+    const auto column = [&](uint32_t n) __attribute__((always_inline)) { return min(n, whole - 1) * kDepth<T>; };
+    // Units first ... of both factors' sixteen (two of W's to a unit of 32 bytes): to stage `stage`, and their places in step n set off.
+    const auto pass_on = [&](uint32_t stage, uint32_t n, int first, int last) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = first; u < last; ++u) {
+            if (u < 8) {
+                feed_x.bring_unit(stage * kStage, u);
+                feed_x.fetch_unit(column(n), u);
+            } else if (kW == 8 || (u & 1) == 0) {
+                feed_w.bring_unit(stage * kStage, (u - 8) * kW / 8);
+                feed_w.fetch_unit(column(n), (u - 8) * kW / 8);
+            }
+        }
+    };
+    Operands a, b;
+    constexpr int kReads = TRANSPOSED ? 12 : 8;
+    // Step n, of which `a` holds the first quarter's operands, in stage `here`; step n + 1 is in registers on its way to the other stage ...
+    const auto step = [&](uint32_t n, uint32_t here) __attribute__((always_inline)) {
+        const uint32_t next = here ^ 1;
+        if constexpr (!TRANSPOSED) asm volatile("" : "+v"(w_at));  // (places are made again every step: there are no registers to hold all of them)
+        asm volatile("" : "+v"(x_at));
+        read(b, here, 1);
+        pass_on(next, n + 2, 0, 6);
+        products(a, 0, 4);
+        interleave<kReads, 6, 6>();
+        read(a, here, 2);
+        pass_on(next, n + 2, 6, 12);
+        products(b, 0, 4);
+        interleave<kReads, 6, 6>();
+        read(b, here, 3);
+        pass_on(next, n + 2, 12, 16);
+        products(a, 0, 3);
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        products(a, 3, 4);
+        read(a, next, 0);
+        products(b, 0, 4);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (whole != 0) {
+        feed_x.fetch(0), feed_w.fetch(0);
+        feed_x.bring(0), feed_w.bring(0);
+        feed_x.fetch(column(1)), feed_w.fetch(column(1));
+        __syncthreads();
+        read(a, 0, 0);
+        uint32_t n = 0;
+        for (; n + 2 <= whole; n += 2) {
+            step(n, 0);
+            step(n + 1, 1);
+        }
+        if (n < whole) step(n, 0);
+    }
+    for (uint32_t k = whole * kDepth<T>; k < s.cols; k += kDepth<T>) {
+        __syncthreads();
+        // (unit after unit: together they would need more registers than there are)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            feed_x.fetch_unit_asking(k, u);
+            feed_x.bring_unit(0, u);
+            __builtin_amdgcn_sched_barrier(0);
+            if (u < kW) {
+                feed_w.fetch_unit_asking(k, u);
+                feed_w.bring_unit(0, u);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            read(a, 0, h);
+            products(a, 0, 4);
+        }
+    }
+    __syncthreads();
+    finish_tile<T>(sum, out + out_wave, token + token_wave, lane, s, 0, e, lds + wave * kTurn<4>);
+}
+
 // The parts' sums of a piece of a token's outputs.
 template <class T>
 __global__ __launch_bounds__(kBlock) void join_parts_kernel(LinearShape s, Epilogue<T> e, uint32_t per_token)
 {
     constexpr int N = kPiece<T>;
-    const uint64_t piece = (uint64_t)block_number() * kBlock + threadIdx.x;
+    const uint64_t piece = (uint64_t)this_block() * kBlock + threadIdx.x;
     const uint64_t token = piece / per_token;
     if (token >= s.tokens) return;
     const uint32_t out = (uint32_t)(piece % per_token) * N;
@@ -328,10 +504,16 @@ struct Plan {
     uint32_t tile_out, tile_token, tiles_out, tiles_token, part, parts;
 };
 
-Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
+// near: whether a tile's rows of both factors lie within 2^32 bytes.
+Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool near)
 {
     Plan p;
     const uint32_t depth = dtype == OGQ_FP32 ? 32 : 64;
+    p.tiles_out = (uint32_t)ceil_div(outs, 256), p.tiles_token = (uint32_t)ceil_div(tokens, 256);
+    if (dtype != OGQ_FP32 && near && tokens > 128 && (uint64_t)p.tiles_out * p.tiles_token >= 160 && cols >= 512) {
+        p.tile_out = p.tile_token = 256, p.part = (uint32_t)cols, p.parts = 1;
+        return p;
+    }
     p.tile_out = 128;
     p.tile_token = tokens <= 64 ? 64 : 128;
     p.tiles_out = (uint32_t)ceil_div(outs, p.tile_out), p.tiles_token = (uint32_t)ceil_div(tokens, p.tile_token);
@@ -355,7 +537,7 @@ template <class T>
 void launch_join_parts(const LinearShape& s, const Epilogue<T>& e, hipStream_t st)
 {
     const uint32_t per_token = (uint32_t)ceil_div(s.outs, kPiece<T>);
-    launch_kernel(join_parts_kernel<T>, grid_of_blocks(ceil_div((uint64_t)s.tokens * per_token, kBlock)), dim3(kBlock), st, s, e, per_token);
+    launch_kernel(join_parts_kernel<T>, grid_of(ceil_div((uint64_t)s.tokens * per_token, kBlock)), dim3(kBlock), st, s, e, per_token);
 }
 
 template void launch_join_parts<float>(const LinearShape&, const Epilogue<float>&, hipStream_t);
@@ -364,7 +546,7 @@ template void launch_join_parts<_Float16>(const LinearShape&, const Epilogue<_Fl
 
 size_t linear_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed)
 {
-    const uint32_t parts = tokens <= kFewTokens ? few_plan(tokens, outs, cols, dtype, transposed).parts : plan_of(tokens, outs, cols, dtype).parts;
+    const uint32_t parts = tokens <= kFewTokens ? few_plan(tokens, outs, cols, dtype, transposed).parts : plan_of(tokens, outs, cols, dtype, true).parts;
     return parts > 1 ? (size_t)parts * tokens * pitch_of(outs) * sizeof(float) : 0;
 }
 
@@ -385,11 +567,15 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
             launch_few(plan, from, w, transposed, s, e, st);
             return;
         }
-        const Plan plan = plan_of(tokens, outs, cols, dtype);
+        // (more parts where they are not near there are not: the large tiles are enough for the chip, and the small ones are more)
+        const bool near = x.stride < ((size_t)1 << 23) && weight.stride < ((size_t)1 << 23) && outs < ((size_t)1 << 30);
+        const Plan plan = plan_of(tokens, outs, cols, dtype, near);
         s.tiles_out = plan.tiles_out, s.tiles_token = plan.tiles_token, s.part = plan.part, s.parts = plan.parts;
         s.sums = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
         auto kernel = transposed ? linear_kernel<T, 128, 128, true> : linear_kernel<T, 128, 128, false>;
         if (plan.tile_token == 64) kernel = transposed ? linear_kernel<T, 128, 64, true> : linear_kernel<T, 128, 64, false>;
+        if constexpr (sizeof(T) == 2)
+            if (plan.tile_out == 256) kernel = transposed ? large_linear_kernel<T, true> : large_linear_kernel<T, false>;
         launch_kernel(kernel, dim3(s.tiles_out * s.tiles_token * s.parts), dim3(256), st, from, w, s, e);
         if (s.sums != nullptr) launch_join_parts(s, e, st);
     });

@@ -13,7 +13,7 @@ constexpr int block_of(int threads) { return threads == 64 ? kBlock : threads; }
 template <int THREADS>
 __device__ __forceinline__ uint64_t first_row()
 {
-    return THREADS == 64 ? (uint64_t)block_number() * 4 + (threadIdx.x >> 6) : block_number();
+    return THREADS == 64 ? (uint64_t)this_block() * 4 + (threadIdx.x >> 6) : this_block();
 }
 
 // P pieces of a row to each of THREADS threads.  `off`, the differences from the mean as it came out of fp32 sums, are summed too: what is left of the mean's rounding is taken off
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* 
 {
     __shared__ float2 space[2][16];
     BlockSums<16> sums{space};
-    const uint64_t row = block_number();
+    const uint64_t row = this_block();
     if (row >= rows) return;
     const T* from = x + row * x_stride;
     float v[kPiece<T>], total = 0.0f;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
     __shared__ float2 space[2][kWaves];
     BlockSums<kWaves> sums{space};
     const uint32_t thread = threadIdx.x & (THREADS - 1), mine = THREADS == 64 ? threadIdx.x >> 6 : 0;
-    const uint32_t first = block_number() * s.part, last = min(s.rows, first + s.part);
+    const uint32_t first = this_block() * s.part, last = min(s.rows, first + s.part);
     const auto at = [&](int p) __attribute__((always_inline)) { return piece_at<T, THREADS, P>(p, thread, s.cols); };
     float w[P][N], dw[P][N], db[P][N];
 #pragma unroll
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
         }
     }
     if (s.parts == nullptr) return;
-    float* out = s.parts + (uint64_t)block_number() * 2 * s.pitch;
+    float* out = s.parts + (uint64_t)this_block() * 2 * s.pitch;
     if constexpr (THREADS == 64) {
         __shared__ float shared[2][64 * P * N];
         // wavefront after wavefront, in their order
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
     constexpr int N = kPiece<T>;
     __shared__ float2 space[2][16];
     BlockSums<16> sums{space};
-    const uint64_t row = block_number();
+    const uint64_t row = this_block();
     if (row >= rows) return;
     const float m = mean[row], r = rstd[row];
     float u[N], g[N], w[N];
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
 {
     constexpr int N = kPiece<T>, kVectors = WHAT == Columns::kNorm ? 2 : 1, kAhead = 4;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t block = block_number(), part = block / blocks, col = (block % blocks * 64 + lane) * N;
+    const uint32_t block = this_block(), part = block / blocks, col = (block % blocks * 64 + lane) * N;
     const uint64_t first = (uint64_t)part * s.part, last = min((uint64_t)s.rows, first + s.part);
     if (first >= s.rows) return;  // (behind the last part, in the last row of a large grid)
     const int valid = valid_of<T>(col, s.cols);
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kBlock) void add_vectors_kernel(const float* parts,
                                                            float* second, bool accumulate)
 {
     __shared__ f32x4 shared[32][8];
-    const uint32_t lane = threadIdx.x & 7, turn = threadIdx.x >> 3, vector = block_number() / blocks, col = (block_number() % blocks * 8 + lane) * 4;
+    const uint32_t lane = threadIdx.x & 7, turn = threadIdx.x >> 3, vector = this_block() / blocks, col = (this_block() % blocks * 8 + lane) * 4;
     if (vector >= vectors) return;
     f32x4 v = {};
     if (col < cols) {
@@ -419,7 +419,7 @@ void launch_columns(const Values& dy, const Values& x, size_t rows, size_t cols,
 {
     const RowParts s{(uint32_t)rows, (uint32_t)cols, cut.part, pitch_of(cols), 0.0f, parts};
     const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
-    launch_kernel(columns_kernel<T, WHAT>, grid_of_blocks((uint64_t)blocks * cut.parts), dim3(kBlock), st, static_cast<const T*>(dy.data), dy.stride,
+    launch_kernel(columns_kernel<T, WHAT>, grid_of((uint64_t)blocks * cut.parts), dim3(kBlock), st, static_cast<const T*>(dy.data), dy.stride,
                   static_cast<const T*>(x.data), x.stride, s, blocks, mean, rstd, act, static_cast<T*>(dz.data), dz.stride);
 }
 
@@ -428,7 +428,7 @@ void launch_columns(const Values& dy, const Values& x, size_t rows, size_t cols,
 void launch_add_vectors(const float* parts, uint32_t number, size_t cols, size_t pitch, float* first, float* second, bool accumulate, hipStream_t st)
 {
     const uint32_t blocks = (uint32_t)ceil_div(cols, 32), vectors = second != nullptr ? 2 : 1;
-    launch_kernel(add_vectors_kernel, grid_of_blocks((uint64_t)blocks * vectors), dim3(kBlock), st, parts, number, (uint32_t)cols, (uint32_t)pitch, vectors, blocks, first, second, accumulate);
+    launch_kernel(add_vectors_kernel, grid_of((uint64_t)blocks * vectors), dim3(kBlock), st, parts, number, (uint32_t)cols, (uint32_t)pitch, vectors, blocks, first, second, accumulate);
 }
 
 void launch_layer_norm_forward(const Values& x, size_t rows, size_t cols, uint32_t dtype, const float* weight, const float* bias, float eps, const Result& y, float* mean,
@@ -451,7 +451,7 @@ void launch_layer_norm_forward(const Values& x, size_t rows, size_t cols, uint32
             if (kThreads == 64) blocks = ceil_div(rows, 4);
         };
         pick(std::integral_constant<int, 64>{}), pick(std::integral_constant<int, 256>{}), pick(std::integral_constant<int, 1024>{});
-        launch_kernel(kernel, grid_of_blocks(blocks), dim3(threads), st, static_cast<const T*>(x.data), x.stride, (uint32_t)rows, (uint32_t)cols, weight, bias, eps, per_col,
+        launch_kernel(kernel, grid_of(blocks), dim3(threads), st, static_cast<const T*>(x.data), x.stride, (uint32_t)rows, (uint32_t)cols, weight, bias, eps, per_col,
                       static_cast<T*>(y.data), y.stride, mean, rstd);
     });
 }
@@ -479,7 +479,7 @@ void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, 
         if (shape.threads == 0) {
             // (the sums first: dx may lie where dy is)
             if (parts != nullptr) launch_columns<T, Columns::kNorm>(dy, x, rows, cols, cut, parts, mean, rstd, 0, {nullptr, 0}, st);
-            launch_kernel(layer_norm_backward_long_kernel<T>, grid_of_blocks(rows), dim3(1024), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data),
+            launch_kernel(layer_norm_backward_long_kernel<T>, grid_of(rows), dim3(1024), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data),
                           x.stride, (uint32_t)rows, (uint32_t)cols, per_col, weight, mean, rstd, static_cast<T*>(dx.data), dx.stride);
             return;
         }
@@ -488,7 +488,7 @@ void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, 
             constexpr int kThreads = decltype(n)::value;
             if (shape.threads != kThreads) return;
             const auto kernel = shape.pieces == 1 ? layer_norm_backward_kernel<T, kThreads, 1> : layer_norm_backward_kernel<T, kThreads, 2>;
-            launch_kernel(kernel, grid_of_blocks(cut.parts), dim3(block_of(kThreads)), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data), x.stride, s,
+            launch_kernel(kernel, grid_of(cut.parts), dim3(block_of(kThreads)), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data), x.stride, s,
                           weight, mean, rstd, static_cast<T*>(dx.data), dx.stride);
         };
         pick(std::integral_constant<int, 64>{}), pick(std::integral_constant<int, 256>{}), pick(std::integral_constant<int, 1024>{});

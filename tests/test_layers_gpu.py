@@ -134,7 +134,8 @@ def test_linear(tokens, outs, cols, transposed, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("tokens,outs,cols", [(1, 300, 4100), (5, 4096, 1000), (8, 2000, 700), (9, 520, 2000), (70, 700, 1000), (513, 1030, 516), (1030, 2060, 200), (2048, 4096, 448), (2300, 5000, 130)])
+@pytest.mark.parametrize("tokens,outs,cols", [(1, 300, 4100), (5, 4096, 1000), (8, 2000, 700), (9, 520, 2000), (70, 700, 1000), (513, 1030, 516), (1030, 2060, 200), (2048, 4096, 448), (2300, 5000, 130), (2561, 4097, 520), (300, 40000, 640),
+                                             (2817, 3841, 1111)])
 def test_linear_of_whole_numbers_is_exact(tokens, outs, cols, transposed, dtype):
     """Sums of whole numbers below 2^24 have no rounding, whatever their order."""
     print("[layers] linear, whole numbers", tokens, outs, cols, transposed, dtype, flush=True)
