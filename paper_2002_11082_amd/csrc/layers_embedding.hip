@@ -11,7 +11,7 @@ namespace {
 
 constexpr uint32_t kRun = 1024;   // keys that a workgroup sorts
 constexpr uint32_t kWays = 32;    // sorted runs that a launch makes one of
-constexpr uint32_t kWindow = 64;  // neighbouring keys whose rows a wavefront adds
+constexpr uint32_t kLeast = 8, kMost = 64;  // neighbouring keys whose rows a wavefront adds, a window: a power of two
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // Token n, or kNone where it names no row.
@@ -49,17 +49,6 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(const void* tokens, b
     }
 }
 
-// How many of the `length` keys of a sorted run are less than `key`; `length` is below 2^log2.
-__device__ __forceinline__ uint32_t count_below(const uint64_t* run, uint32_t length, uint32_t log2, uint64_t key)
-{
-    uint32_t below = 0;
-    for (int bit = (int)log2 - 1; bit >= 0; --bit) {
-        const uint32_t probe = below + (1u << bit);
-        if (probe <= length && run[probe - 1] < key) below = probe;
-    }
-    return below;
-}
-
 // Zeros for the table's gradient: rows of `length` values in units of kUnit, `units` of them to a row (one row where the table has no gaps).
 constexpr uint32_t kUnit = 16384;
 struct Fill {
@@ -85,72 +74,92 @@ __device__ __forceinline__ void fill_unit(const Fill& f, uint64_t unit)
     }
 }
 
-// The first `runs` workgroups sort 1024 keys each: every wavefront places its 64 by counting, then a key's place among all is its own place and what the other fifteen have below it.
-// The others fill.
+// The first `runs` workgroups sort 1024 keys each: every wavefront places its 64 by counting, then neighbouring runs become one, four times over: a key's place is its own and what the other run
+// has below it.  The other workgroups fill.
 __global__ __launch_bounds__(kRun) void sort_runs_kernel(const void* tokens, bool wide, uint32_t number, uint32_t vocab, uint32_t runs, uint64_t* keys, Fill fill)
 {
-    __shared__ uint64_t sorted[kRun];
+    __shared__ uint64_t sorted[2][kRun];
     if (this_block() >= runs) {
         const uint64_t unit = fill.first + (this_block() - runs);
         if (unit < fill.last) fill_unit(fill, unit);
         return;
     }
-    const uint32_t position = this_block() * kRun + threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t position = this_block() * kRun + threadIdx.x, lane = threadIdx.x & 63;
     // (behind the last token: keys above all others)
     const uint32_t token = position < number ? token_of(tokens, wide, position, vocab) : kNone;
-    uint64_t key = (uint64_t)token << 32 | position;
-    uint32_t place = 0;
+    uint32_t place = threadIdx.x - lane;
 #pragma unroll 8
-    for (int n = 0; n < 64; ++n) {
-        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(token, n) << 32 | (uint32_t)__builtin_amdgcn_readlane(position, n);
-        place += other < key ? 1 : 0;
+    for (uint32_t n = 0; n < 64; ++n) {  // (a lane's position is above those of the lanes before it)
+        const uint32_t other = __builtin_amdgcn_readlane(token, n);
+        place += other < token || (other == token && n < lane) ? 1 : 0;
     }
-    sorted[wave * 64 + place] = key;
-    __syncthreads();
-    key = sorted[threadIdx.x];
-    place = lane;
-#pragma unroll
-    for (uint32_t w = 0; w < kRun / 64; ++w)
-        if (w != wave) place += count_below(sorted + w * 64, 64, 7, key);
-    keys[this_block() * kRun + place] = key;
+    uint32_t side = 0;
+    sorted[0][place] = (uint64_t)token << 32 | position;
+    uint64_t key;
+    for (uint32_t length = 64;; length *= 2) {
+        __syncthreads();
+        key = sorted[side][threadIdx.x];
+        if (length == kRun) break;
+        const uint64_t* other = &sorted[side][(threadIdx.x ^ length) & ~(length - 1)];
+        uint32_t below = 0;
+        for (uint32_t bit = length; bit != 0; bit /= 2) {
+            const uint32_t probe = below + bit;
+            if (probe <= length && other[probe - 1] < key) below = probe;
+        }
+        side ^= 1;
+        sorted[side][(threadIdx.x & ~(2 * length - 1)) + (threadIdx.x & (length - 1)) + below] = key;
+    }
+    keys[position] = key;
 }
 
-// Runs of `run` sorted keys into runs of kWays times as many: a key's place is its own and what the other runs have below it.  `total` is a multiple of kRun.  The workgroups behind
-// those that the keys need fill.
+// Runs of `run` sorted keys into runs of kWays times as many: a key's place is its own and what the other runs have below it.  Eight lanes to a key, each of which searches four runs, side by
+// side: first among every 128th part of a run, which is in LDS, then in memory.  `total` is a multiple of kRun.  The workgroups behind those that the keys need fill.
+constexpr uint32_t kKeys = kRun / 8;  // of a workgroup
 __global__ __launch_bounds__(kRun) void merge_runs_kernel(const uint64_t* from, uint64_t* to, uint32_t total, uint32_t run, uint32_t run_log2, Fill fill)
 {
-    if (this_block() >= total / kRun) {
-        const uint64_t unit = fill.first + (this_block() - total / kRun);
+    constexpr uint32_t kSide = kWays / 8, kSamplesLog2 = 7, kSamples = 1u << kSamplesLog2;
+    __shared__ uint64_t samples[kWays * kSamples];
+    if (this_block() >= total / kKeys) {
+        const uint64_t unit = fill.first + (this_block() - total / kKeys);
         if (unit < fill.last) fill_unit(fill, unit);
         return;
     }
-    const uint32_t at = this_block() * kRun + threadIdx.x;  // (all of a workgroup's are of one run)
-    const uint32_t mine = (this_block() * kRun) >> run_log2, base = mine / kWays * kWays;
-    const uint64_t key = from[at];
-    uint32_t place = at - (mine << run_log2);
-    // eight searches at a time, whose loads are under way together
-    for (uint32_t r = base; r < base + kWays; r += 8) {
-        if ((uint64_t)r << run_log2 >= total) break;
-        uint32_t below[8] = {}, length[8];
+    const uint32_t at = this_block() * kKeys + threadIdx.x / 8, mine = (this_block() * kKeys) >> run_log2, base = mine / kWays * kWays;  // (all of a workgroup's keys are of one run)
+    const uint32_t apart_log2 = run_log2 - kSamplesLog2, first = threadIdx.x % 8 * kSide;
+    const uint64_t start = (uint64_t)base << run_log2, key = from[at];
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            const uint64_t begin = (uint64_t)(r + k) << run_log2;
-            length[k] = r + k == mine || begin >= total ? 0 : (uint32_t)min((uint64_t)run, total - begin);
-        }
-        for (int bit = (int)run_log2; bit >= 0; --bit) {
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) {
-                const uint32_t probe = below[k] + (1u << bit);
-                const bool inside = probe <= length[k];
-                // (a key that is there in any case)
-                const uint64_t other = from[inside ? ((uint64_t)(r + k) << run_log2) + probe - 1 : at];
-                if (inside && other < key) below[k] = probe;
-            }
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) place += below[k];
+    for (uint32_t k = 0; k < kWays * kSamples / kRun; ++k) {  // sample n is the last of its keys: behind the last key of all, one above them
+        const uint64_t n = k * kRun + threadIdx.x, which = start + ((n + 1) << apart_log2) - 1;
+        samples[n] = which < total ? from[which] : ~0ull;
     }
-    to[((uint64_t)base << run_log2) + place] = key;
+    __syncthreads();
+    uint32_t below[kSide] = {};
+    // how many of a run's samples are below the key: as many times their distance keys are
+#pragma unroll
+    for (int bit = kSamplesLog2; bit >= 0; --bit)
+#pragma unroll
+        for (uint32_t k = 0; k < kSide; ++k) {
+            const uint32_t probe = below[k] + (1u << bit);
+            if (probe <= kSamples && samples[(first + k) * kSamples + min(probe, kSamples) - 1] < key) below[k] = probe;
+        }
+#pragma unroll
+    for (uint32_t k = 0; k < kSide; ++k) below[k] <<= apart_log2;
+    for (int bit = (int)apart_log2 - 1; bit >= 0; --bit)
+#pragma unroll
+        for (uint32_t k = 0; k < kSide; ++k) {
+            const uint32_t probe = below[k] + (1u << bit);
+            const uint64_t which = start + ((uint64_t)(first + k) << run_log2) + probe - 1;
+            const bool inside = probe <= run && which < total;
+            const uint64_t other = from[inside ? which : at];  // (a key that is there in any case)
+            if (inside && other < key) below[k] = probe;
+        }
+    uint32_t place = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kSide; ++k) place += base + first + k != mine ? below[k] : 0;
+    place += dpp_u32<kDppXor1>(place);
+    place += dpp_u32<kDppXor2>(place);
+    place += dpp_u32<kDppHalfMirror>(place);
+    if (first == 0) to[start + (at - (mine << run_log2)) + place] = key;
 }
 
 // The columns of a lane: a piece of a row, which lies as PieceAt says where the row has as many values.
@@ -190,7 +199,7 @@ struct Piece {
 };
 
 struct Table {
-    uint32_t number, cols, blocks, pitch;  // blocks: of 64 pieces, along a row
+    uint32_t number, cols, blocks, pitch, window;  // blocks: of 64 pieces, along a row; window: keys of one
     uint64_t dy_stride, dtable_stride;
     float scale;
 };
@@ -198,18 +207,18 @@ struct Table {
 // The token of a key, kNone for what is not there.
 __device__ __forceinline__ uint32_t token_at(const uint64_t* keys, uint32_t number, uint64_t at) { return at < number ? (uint32_t)(keys[at] >> 32) : kNone; }
 
-// kWindow neighbouring keys to a wavefront: the rows of each token among them are added one after the other.  A token whose keys all lie here is finished; of the others (the first one may have begun
+// A window of neighbouring keys to a wavefront: the rows of each token among them are added one after the other.  A token whose keys all lie here is finished; of the others (the first one may have begun
 // before, the last one may go on) the sums wait for the next kernel, sums[2 n] of one that had begun before window n, sums[2 n + 1] of one that begins there.
 template <class T, bool ACCUMULATE>
 __global__ __launch_bounds__(kBlock) void add_windows_kernel(const uint64_t* keys, const T* dy, Table s, float* sums, float* dtable)
 {
     constexpr int N = kPiece<T>, kAhead = 8;
     const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), window = unit / s.blocks;
-    if (window * kWindow >= s.number) return;
-    const uint32_t lane = threadIdx.x & 63, first = (uint32_t)window * kWindow;
-    const uint64_t key = first + lane < s.number ? keys[first + lane] : ~0ull;
+    if (window * s.window >= s.number) return;
+    const uint32_t lane = threadIdx.x & 63, first = (uint32_t)window * s.window;
+    const uint64_t key = lane < s.window && first + lane < s.number ? keys[first + lane] : ~0ull;
     const uint32_t token = (uint32_t)(key >> 32), position = (uint32_t)key;
-    const uint32_t before = window == 0 ? kNone : token_at(keys, s.number, first - 1), behind = token_at(keys, s.number, (uint64_t)first + kWindow);
+    const uint32_t before = window == 0 ? kNone : token_at(keys, s.number, first - 1), behind = token_at(keys, s.number, (uint64_t)first + s.window);
     const uint32_t here = __builtin_popcountll(__builtin_amdgcn_ballot_w64(token != kNone));  // (keys of no token are the last ones)
     if (here == 0) return;
     const uint32_t left = __shfl_up(token, 1);
@@ -239,7 +248,7 @@ __global__ __launch_bounds__(kBlock) void add_windows_kernel(const uint64_t* key
             if (!end) continue;
             const uint32_t mine = __builtin_amdgcn_readlane(token, at);
             // (whether its first key here is the window's first, and of a token that the key before names)
-            const bool begun = mine == before && mine == (uint32_t)__builtin_amdgcn_readfirstlane(token), goes_on = at + 1 == kWindow && mine == behind;
+            const bool begun = mine == before && mine == (uint32_t)__builtin_amdgcn_readfirstlane(token), goes_on = at + 1 == s.window && mine == behind;
             if (!begun && !goes_on) {
                 piece.template store<ACCUMULATE>(dtable + (uint64_t)mine * s.dtable_stride, s.scale, sum);
             } else if (piece.there()) {
@@ -249,22 +258,22 @@ __global__ __launch_bounds__(kBlock) void add_windows_kernel(const uint64_t* key
     }
 }
 
-// The tokens whose keys lie in several windows: the wavefront of the window in which a token's last key lies adds the sums of its windows, in their order.
+// The tokens whose keys lie in several windows: the workgroup of the window in which a token's last key lies adds the sums of its windows, a quarter of them in each wavefront, one after the
+// other.
 template <class T, bool ACCUMULATE>
 __global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* keys, Table s, const float* sums, float* dtable)
 {
     constexpr int N = kPiece<T>;
-    const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), window = unit / s.blocks + 1;
-    if (window * kWindow >= s.number) return;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t first = window * kWindow;
+    const uint64_t window = this_block() / s.blocks + 1, first = window * s.window;
+    if (first >= s.number) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t token = token_at(keys, s.number, first);
-    if (token == kNone || token != token_at(keys, s.number, first - 1) || token == token_at(keys, s.number, first + kWindow)) return;
+    if (token == kNone || token != token_at(keys, s.number, first - 1) || token == token_at(keys, s.number, first + s.window)) return;
     // the windows before this one into which the token had gone on: the nearest that the key before does not name is where it begins
     uint64_t begin = window;
     for (;;) {
         const uint64_t at = begin - 1 - lane;  // (one below 0 is none)
-        const bool on = begin >= 1 + (uint64_t)lane && at != 0 && token_at(keys, s.number, at * kWindow - 1) == token;
+        const bool on = begin >= 1 + (uint64_t)lane && at != 0 && token_at(keys, s.number, at * s.window - 1) == token;
         const uint64_t all = __builtin_amdgcn_ballot_w64(on);
         if (~all == 0) {
             begin -= 64;
@@ -273,17 +282,29 @@ __global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* ke
         begin -= 1 + __builtin_ctzll(~all);
         break;
     }
-    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * N, s.cols);
-    if (!piece.there()) return;
-    float sum[N];
-    memcpy(sum, sums + (2 * begin + 1) * s.pitch + piece.col(), sizeof sum);
+    const Piece<T> piece((this_block() % s.blocks * 64 + lane) * N, s.cols);
+    const uint64_t number = window - begin + 1, each = (number + 3) / 4, last = min(number, (wave + 1) * each);
+    float sum[N] = {};
+    if (piece.there()) {
 #pragma unroll 8
-    for (uint64_t n = begin + 1; n <= window; ++n) {
-        float v[N];
-        memcpy(v, sums + 2 * n * s.pitch + piece.col(), sizeof v);
+        for (uint64_t n = wave * each; n < last; ++n) {
+            float v[N];
+            memcpy(v, sums + (2 * (begin + n) + (n == 0 ? 1 : 0)) * s.pitch + piece.col(), sizeof v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] += v[i];
+            for (int i = 0; i < N; ++i) sum[i] += v[i];
+        }
     }
+    __shared__ float shared[3][N][64];
+    if (wave != 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) shared[wave - 1][i][lane] = sum[i];
+    }
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += shared[w][i][lane];
     piece.template store<ACCUMULATE>(dtable + (uint64_t)token * s.dtable_stride, s.scale, sum);
 }
 
@@ -296,6 +317,7 @@ __global__ __launch_bounds__(kRun) void fill_kernel(Fill fill)
 // What lies where in the workspace.
 struct Space {
     size_t keys, sums, bytes;  // bytes of one of two buffers of keys, of the windows' sums, of all
+    uint32_t window;
 };
 
 size_t pitch_of(size_t cols) { return (cols + 7) / 8 * 8; }
@@ -304,7 +326,11 @@ Space space_of(size_t number, size_t cols)
 {
     Space s;
     s.keys = ceil_div(number, kRun) * kRun * sizeof(uint64_t);
-    s.sums = number > kWindow ? 2 * ceil_div(number, kWindow) * pitch_of(cols) * sizeof(float) : 0;
+    // Keys of a window: few where there are few wavefronts, since a wavefront has eight rows under way at a time; many otherwise, since each window may leave two sums that are written and read
+    // once more.
+    s.window = kLeast;
+    while (s.window < kMost && number * cols / s.window > (size_t)8192 * 512) s.window *= 2;
+    s.sums = number > s.window ? 2 * ceil_div(number, s.window) * pitch_of(cols) * sizeof(float) : 0;
     s.bytes = (number > kRun ? 2 : 1) * s.keys + s.sums;
     return s;
 }
@@ -363,19 +389,19 @@ void launch_embedding_gradient(const Integers& tokens, size_t number, const Valu
     uint32_t log2 = 10, n = 1;
     for (uint64_t run = kRun; run < total; run *= kWays, log2 += 5) {
         now = part(n++);
-        launch_kernel(merge_runs_kernel, grid_of(total / kRun + now.last - now.first), dim3(kRun), st, static_cast<const uint64_t*>(keys), other, total, (uint32_t)run, log2,
+        launch_kernel(merge_runs_kernel, grid_of(total / kKeys + now.last - now.first), dim3(kRun), st, static_cast<const uint64_t*>(keys), other, total, (uint32_t)run, log2,
                       now);
         std::swap(keys, other);
     }
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
-        const Table s{(uint32_t)number, (uint32_t)cols, blocks, (uint32_t)pitch_of(cols), dy.stride, dtable.stride, scale};
-        const dim3 grid = grid_of(ceil_div(ceil_div(number, kWindow) * blocks, 4));
-        launch_kernel(accumulate ? add_windows_kernel<T, true> : add_windows_kernel<T, false>, grid, dim3(kBlock), st, static_cast<const uint64_t*>(keys),
+        const Table s{(uint32_t)number, (uint32_t)cols, blocks, (uint32_t)pitch_of(cols), space.window, dy.stride, dtable.stride, scale};
+        const uint64_t windows = ceil_div(number, space.window);
+        launch_kernel(accumulate ? add_windows_kernel<T, true> : add_windows_kernel<T, false>, grid_of(ceil_div(windows * blocks, 4)), dim3(kBlock), st, static_cast<const uint64_t*>(keys),
                       static_cast<const T*>(dy.data), s, sums, out);
-        if (number > kWindow)
-            launch_kernel(accumulate ? join_windows_kernel<T, true> : join_windows_kernel<T, false>, grid, dim3(kBlock), st, static_cast<const uint64_t*>(keys), s,
+        if (windows > 1)
+            launch_kernel(accumulate ? join_windows_kernel<T, true> : join_windows_kernel<T, false>, grid_of((windows - 1) * blocks), dim3(kBlock), st, static_cast<const uint64_t*>(keys), s,
                           static_cast<const float*>(sums), out);
     });
 }

@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kBlock) void add_vectors_kernel(const float* parts,
     f32x4 v = {};
     if (col < cols) {
         const float* from = parts + (uint64_t)vector * pitch + col;
-#pragma unroll 4
+#pragma unroll 16
         for (uint32_t n = turn; n < number; n += 32) {
             f32x4 t;
             memcpy(&t, from + (uint64_t)n * vectors * pitch, sizeof t);
