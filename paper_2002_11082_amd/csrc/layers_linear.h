@@ -40,6 +40,45 @@ struct Epilogue {
         }
         store_piece<false>(y + token * y_stride + out, valid, v);
     }
+
+    // The same for ROWS tokens, `apart` from one to the next, below `tokens`, of 16-bit types: what is loaded is under way together.  The bias comes from the caller.
+    template <int ROWS>
+    __device__ __forceinline__ void rows(uint32_t first, uint32_t apart, uint32_t tokens, uint32_t out, int valid, const float (&b)[8], float (&v)[ROWS][8]) const
+    {
+        static_assert(kPiece<T> == 8);
+        uint4 r[ROWS];
+        if (residual != nullptr) {
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n) r[n] = load_raw(residual + min(first + n * apart, tokens - 1) * residual_stride + out, valid);
+        }
+#pragma unroll
+        for (int n = 0; n < ROWS; ++n)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[n][i] += b[i];
+        if (before != nullptr) {
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n)
+                if (first + n * apart < tokens) store_piece<false>(before + (first + n * apart) * before_stride + out, valid, v[n]);
+        }
+        if (act != OGQ_IDENTITY) {
+            float a[ROWS * 8];
+#pragma unroll
+            for (int i = 0; i < ROWS * 8; ++i) a[i] = v[i / 8][i % 8];
+            each_of(act, a, [&](int i, float value, float) { v[i / 8][i % 8] = value; });
+        }
+        if (residual != nullptr) {
+#pragma unroll
+            for (int n = 0; n < ROWS; ++n) {
+                float add[8];
+                values_of<T>(r[n], add);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[n][i] += add[i];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < ROWS; ++n)
+            if (first + n * apart < tokens) store_piece<false>(y + (first + n * apart) * y_stride + out, valid, v[n]);
+    }
 };
 
 struct LinearShape {

@@ -78,7 +78,11 @@ struct Along {
     // How many whole steps from `first` on can be fetched without asking.
     __device__ __forceinline__ uint32_t readable(uint32_t first) const { return (last - first) / kDepth<T>; }
     __device__ __forceinline__ const T* at(uint32_t k, int u) const { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(data + k) + offset[u]); }
-    __device__ __forceinline__ void fetch_unit(uint32_t k, int u) { held[u].load(at(k, u)); }
+    __device__ __forceinline__ void fetch_unit(uint32_t k, int u)
+    {
+        if constexpr (NEAR) asm volatile("" : "+v"(offset[u]));  // (an address in scalar registers and 32 bits: the compiler makes 64 bits of these ahead of the loop)
+        held[u].load(at(k, u));
+    }
     __device__ __forceinline__ void fetch(uint32_t k)
     {
 #pragma unroll
@@ -349,22 +353,6 @@ __device__ __forceinline__ uint2 tile_of(uint32_t id, uint32_t tiles_out, uint32
     return make_uint2(panel * kWide + rest % width, rest / width);
 }
 
-// The order of instructions in a quarter of a step: behind its sixteen products, which the matrix core takes 32 cycles for each, reads of operands, writes to LDS and loads in turn.
-template <int READS, int WRITES, int LOADS>
-__device__ __forceinline__ void interleave()
-{
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
-        if (READS > 8 ? true : i % 2 == 0) {
-            if (i * READS / 16 < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
-        }
-        if (i % 2 == 1 && i / 2 < WRITES) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS write
-        if (i % 2 == 1 && i / 2 < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // memory read
-    }
-    __builtin_amdgcn_sched_barrier(0);
-}
-
 // Tiles of 256 x 256 sums of 16-bit products, 128 x 128 in each of four wavefronts, one to a SIMD, which has all of its registers: 256 hold the sums.  A step of 64 columns is multiplied in four
 // quarters; while one is, the next one's operands come from LDS.  Two stages of LDS: the step behind the next one goes where the last one was, and the one behind that sets off from
 // memory.  One barrier a step, in front of the last quarter, which reads the next step's first operands.
@@ -388,65 +376,58 @@ __global__ __launch_bounds__(256, 1) void large_linear_kernel(const T* x, const 
         s16x8 w[4], x[4];
     };
     uint32_t w_at = FeedW::operand(out_wave, lane), x_at = FeedX::operand(token_wave, lane);
-    const auto read = [&](Operands& r, uint32_t stage, int h) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[i] = FeedW::read_operand(lds, w_at, stage * kStage, i, h);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r.x[j] = FeedX::read_operand(lds, x_at, stage * kStage + FeedW::kPlane, j, h);
+    // Operand m of the eight, in the order in which they are needed first: w0, x0 ... x3, w1 ... w3.
+    const auto read = [&](Operands& r, uint32_t stage, int h, int m) __attribute__((always_inline)) {
+        if (m >= 1 && m < 5) r.x[m - 1] = FeedX::read_operand(lds, x_at, stage * kStage + FeedW::kPlane, m - 1, h);
+        else r.w[m == 0 ? 0 : m - 4] = FeedW::read_operand(lds, w_at, stage * kStage, m == 0 ? 0 : m - 4, h);
     };
-    const auto products = [&](const Operands& r, int from, int to) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = from; i < to; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum[i][j] = multiply_add<T>(r.w[i], r.x[j], sum[i][j]);
-    };
+    const auto product = [&](const Operands& r, int m) __attribute__((always_inline)) { sum[m / 4][m % 4] = multiply_add<T>(r.w[m / 4], r.x[m % 4], sum[m / 4][m % 4]); };
     // (one behind the last whole step is the last one again, and not used)
     const auto column = [&](uint32_t n) __attribute__((always_inline)) { return min(n, whole - 1) * kDepth<T>; };
-    // Units first ... of both factors' sixteen (two of W's to a unit of 32 bytes): to stage `stage`, and their places in step n set off.
-    const auto pass_on = [&](uint32_t stage, uint32_t n, int first, int last) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = first; u < last; ++u) {
-            if (u < 8) {
-                feed_x.bring_unit(stage * kStage, u);
-                feed_x.fetch_unit(column(n), u);
-            } else if (kW == 8 || (u & 1) == 0) {
-                feed_w.bring_unit(stage * kStage, (u - 8) * kW / 8);
-                feed_w.fetch_unit(column(n), (u - 8) * kW / 8);
-            }
+    // Unit u of both factors' sixteen (two of W's to a unit of 32 bytes): to stage `stage`, and its place in step n sets off.
+    const auto pass_on = [&](uint32_t stage, uint32_t n, int u) __attribute__((always_inline)) {
+        if (u < 8) {
+            feed_x.bring_unit(stage * kStage, u);
+            feed_x.fetch_unit(column(n), u);
+        } else if (kW == 8 || (u & 1) == 0) {
+            feed_w.bring_unit(stage * kStage, (u - 8) * kW / 8);
+            feed_w.fetch_unit(column(n), (u - 8) * kW / 8);
         }
     };
     Operands a, b;
-    constexpr int kReads = TRANSPOSED ? 12 : 8;
+    // A quarter of a step: sixteen products, which the matrix core takes 32 cycles for each.  Behind each of the first eight an operand of the next quarter is read, behind the others units
+    // first ... last are passed on.  The order is as written: the compiler's own has the reads waited for where they are issued (8192 x 8192 sums of 8192 products 904 us)
+    const auto quarter = [&](Operands& now, Operands& then, uint32_t stage, int h, uint32_t to, uint32_t n, int first, int last, bool meet) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 16; ++m) {
+            asm volatile("" : "+v"(now.x[m % 4]));  // (a product has no other order than that of what it takes)
+            product(now, m);
+            if (m < 8) read(then, stage, h, m);
+            else if (first + m - 8 < last) pass_on(to, n, first + m - 8);
+            __builtin_amdgcn_sched_barrier(0);
+            if (meet && m == 13) {
+                __syncthreads();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
     // Step n, of which `a` holds the first quarter's operands, in stage `here`; step n + 1 is in registers on its way to the other stage ...
     const auto step = [&](uint32_t n, uint32_t here) __attribute__((always_inline)) {
         const uint32_t next = here ^ 1;
         if constexpr (!TRANSPOSED) asm volatile("" : "+v"(w_at));  // (places are made again every step: there are no registers to hold all of them)
         asm volatile("" : "+v"(x_at));
-        read(b, here, 1);
-        pass_on(next, n + 2, 0, 6);
-        products(a, 0, 4);
-        interleave<kReads, 6, 6>();
-        read(a, here, 2);
-        pass_on(next, n + 2, 6, 12);
-        products(b, 0, 4);
-        interleave<kReads, 6, 6>();
-        read(b, here, 3);
-        pass_on(next, n + 2, 12, 16);
-        products(a, 0, 3);
-        __builtin_amdgcn_sched_barrier(0);
-        __syncthreads();
-        __builtin_amdgcn_sched_barrier(0);
-        products(a, 3, 4);
-        read(a, next, 0);
-        products(b, 0, 4);
-        __builtin_amdgcn_sched_barrier(0);
+        quarter(a, b, here, 1, next, n + 2, 0, 6, false);
+        quarter(b, a, here, 2, next, n + 2, 6, 12, false);
+        quarter(a, b, here, 3, next, n + 2, 12, 16, true);
+        quarter(b, a, next, 0, next, n + 2, 0, 0, false);
     };
     if (whole != 0) {
         feed_x.fetch(0), feed_w.fetch(0);
         feed_x.bring(0), feed_w.bring(0);
         feed_x.fetch(column(1)), feed_w.fetch(column(1));
         __syncthreads();
-        read(a, 0, 0);
+#pragma unroll
+        for (int m = 0; m < 8; ++m) read(a, 0, 0, m);
         uint32_t n = 0;
         for (; n + 2 <= whole; n += 2) {
             step(n, 0);
@@ -471,12 +452,177 @@ __global__ __launch_bounds__(256, 1) void large_linear_kernel(const T* x, const 
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            read(a, 0, h);
-            products(a, 0, 4);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) read(a, 0, h, m);
+#pragma unroll
+            for (int m = 0; m < 16; ++m) product(a, m);
         }
     }
     __syncthreads();
     finish_tile<T>(sum, out + out_wave, token + token_wave, lane, s, 0, e, lds + wave * kTurn<4>);
+}
+
+// The same tiles where the rows of both factors begin at multiples of 16 bytes: memory goes to LDS without a way through registers (16 bytes to a lane: lane n of a wavefront's load writes
+// bytes 16 n ... of 1 KB), in the places that Along and Across read.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds)
+{
+    // (in assembly because the compiler would have every read of LDS wait for all such loads; nothing is returned in registers.  One wait state between m0 and its use)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+
+// Units of 4 KB of a step of 256 rows along k, 32 rows each, or of 64 rows across k, 8 rows each.
+template <class T, bool ACROSS>
+struct Direct {
+    static constexpr int kUnits = 8, kRowPieces = ACROSS ? 32 : 8, kUnitRows = 256 / kRowPieces;
+    const T* data;
+    uint64_t stride;
+    uint32_t offset[ACROSS ? 1 : kUnits], lds;
+
+    Direct() = default;
+    // `at`: where the factor's plane of the first stage begins.
+    __device__ __forceinline__ Direct(const T* data_, uint64_t stride_, uint32_t first, uint32_t number, uint32_t thread, uint32_t at) : data(data_), stride(stride_)
+    {
+        const uint32_t row = thread / kRowPieces, piece = thread % kRowPieces;
+        lds = at + __builtin_amdgcn_readfirstlane(thread / 64) * 1024;
+        if constexpr (ACROSS) {
+            const uint32_t column = first + ((piece / 2) ^ Across<T, 256, true>::twist(row)) * 16 + piece % 2 * 8;
+            offset[0] = (row * (uint32_t)stride + (column < number ? column : first)) * sizeof(T);
+        } else {
+            data += first * stride;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) offset[u] = (min(row + u * kUnitRows, number - 1 - first) * (uint32_t)stride + (piece ^ (row / 2 & 7)) * 8) * sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void load(uint32_t k, uint32_t stage_bytes, int u)
+    {
+        if constexpr (ACROSS) load_to_lds(data + (uint64_t)(k + u * kUnitRows) * stride, offset[0], lds + stage_bytes + u * 4096);
+        else load_to_lds(data + k, offset[u], lds + stage_bytes + u * 4096);
+    }
+};
+
+// The sums of a wavefront, 128 outputs from `out` and 128 tokens from `token`, on their way out in eight parts of 64 by 32.  A lane holds four neighbouring outputs of a token; through LDS (8 KB of the
+// wavefront's own, 16 bytes of row r in place of those 16 (r % 16) bytes away, for the banks' sake) eight lanes get the 64 of one, so that whole lines are written.
+template <class T>
+__device__ __forceinline__ void finish_large(const f32x16 (&sum)[4][4], uint32_t out, uint32_t token, uint32_t lane, const LinearShape& s, const Epilogue<T>& e, char* space)
+{
+    const uint32_t column = lane % 8 * 8;
+    float bias[8];
+#pragma unroll 1
+    for (int part = 0; part < 8; ++part) {  // (one code for all parts: only what reads the sums' registers is there for each)
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            if (p == part) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const f32x16& v = sum[p / 4 * 2 + a][p % 4];
+                        *reinterpret_cast<f32x4*>(space + (lane & 31) * 256 + (((a * 8 + 2 * m + (lane >> 5)) ^ (lane & 15)) * 16)) = f32x4{v[4 * m], v[4 * m + 1], v[4 * m + 2], v[4 * m + 3]};
+                    }
+            }
+        wavefront_sync();
+        const uint32_t o = out + part / 4 * 64 + column;
+        const int valid = valid_of<T>(o, s.outs);
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t row = lane / 8 + 8 * i;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) memcpy(v[i] + 4 * h, __builtin_assume_aligned(space + row * 256 + (((lane % 8 * 2 + h) ^ (row & 15)) * 16), 16), 16);
+        }
+        wavefront_sync();
+        if (valid == 0) continue;
+        if (part % 4 == 0) load_vector<T>(e.bias == nullptr ? nullptr : e.bias + o, valid, 0.0f, bias);
+        const uint32_t first = token + part % 4 * 32 + lane / 8;
+        e.template rows<4>(first, 8, s.tokens, o, valid, bias, v);
+    }
+}
+
+// A step's four quarters, sixteen products each; behind a product an operand of the next quarter is read or a load to LDS sets off.  LDS holds five planes of 32 KB: the step's two, the next
+// one's, and one to which the next plane is on its way: x two steps ahead in the first two quarters, W in the last, when the step's own operands have been read by all: one barrier a step.  A workgroup
+// stays and takes tile after tile; the next one's first two steps come in while the last one's sums leave, through the plane that is free.
+template <class T, bool TRANSPOSED>
+__global__ __launch_bounds__(256, 1) void direct_linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
+{
+    using FeedW = std::conditional_t<TRANSPOSED, Across<T, 256, true>, Along<T, 256, true>>;
+    using FeedX = Along<T, 256, true>;
+    constexpr uint32_t kPlane = FeedX::kPlane;
+    static_assert(kPlanes<T> == 1 && FeedW::kPlane == 32768 && kPlane == 32768);
+    __shared__ __align__(256) char lds[5 * kPlane];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles = s.tiles_out * s.tiles_token, out_wave = (wave & 1) * 128, token_wave = (wave >> 1) * 128, steps = s.cols / kDepth<T>;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    // where loads are: the tile that is multiplied, or the next one
+    Direct<T, TRANSPOSED> load_w;
+    Direct<T, false> load_x;
+    const auto turn_to = [&](uint32_t id) __attribute__((always_inline)) {
+        const uint2 tile = tile_of(id < tiles ? id : blockIdx.x, s.tiles_out, s.tiles_token);  // (behind the last tile the first one again, which is not used)
+        load_w = Direct<T, TRANSPOSED>(weight, s.weight_stride, tile.x * 256, s.outs, threadIdx.x, base);
+        load_x = Direct<T, false>(x, s.x_stride, tile.y * 256, s.tokens, threadIdx.x, base);
+    };
+    f32x16 sum[4][4];
+    struct Operands {
+        s16x8 w[4], x[4];
+    };
+    uint32_t w_at = FeedW::operand(out_wave, lane), x_at = FeedX::operand(token_wave, lane);
+    // Operand m of the eight, in the order in which they are needed first: w0, x0 ... x3, w1 ... w3.
+    const auto read = [&](Operands& r, uint32_t x_plane, uint32_t w_plane, int h, int m) __attribute__((always_inline)) {
+        if (m >= 1 && m < 5) r.x[m - 1] = FeedX::read_operand(lds, x_at, x_plane, m - 1, h);
+        else r.w[m == 0 ? 0 : m - 4] = FeedW::read_operand(lds, w_at, w_plane, m == 0 ? 0 : m - 4, h);
+    };
+    // The planes, by where they begin: this step's, the next one's, and the one that is free.
+    uint32_t x_here = 0, w_here = kPlane, x_next = 2 * kPlane, w_next = 3 * kPlane, free = 4 * kPlane;
+    Operands a, b;
+    turn_to(blockIdx.x);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) load_x.load(0, x_here, u), load_w.load(0, w_here, u);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) load_x.load(kDepth<T>, x_next, u), load_w.load(kDepth<T>, w_next, u);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < 8; ++m) read(a, x_here, w_here, 0, m);
+    for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[i][j] = f32x16{};
+        for (uint32_t n = 0; n < steps; ++n) {
+            if (n + 2 == steps) turn_to(id + gridDim.x);
+            const uint32_t k = (n + 2 < steps ? n + 2 : n + 2 - steps) * kDepth<T>;
+            if constexpr (!TRANSPOSED) asm volatile("" : "+v"(w_at));  // (places are made again every step: there are no registers to hold all of them)
+            asm volatile("" : "+v"(x_at));
+            const auto quarter = [&](int q, Operands& now, Operands& then, uint32_t x_plane, uint32_t w_plane) __attribute__((always_inline)) {
+#pragma unroll
+                for (int m = 0; m < 16; ++m) {
+                    asm volatile("" : "+v"(now.x[m % 4]));  // (a product has no other order than that of what it takes)
+                    sum[m / 4][m % 4] = multiply_add<T>(now.w[m / 4], now.x[m % 4], sum[m / 4][m % 4]);
+                    if (q == 2 ? m < 8 : m % 2 == 0) read(then, x_plane, w_plane, (q + 1) % 4, q == 2 ? m : m / 2);
+                    if (q < 2 && m % 4 == 1) load_x.load(k, free, q * 4 + m / 4);
+                    if (q == 3 && m % 2 == 1) load_w.load(k, x_here, m / 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (q == 2 && m == 13) {
+                        // this wavefront's share of the next step has arrived, all but the eight loads of the one behind it (stores of the last tile may be among what is under way, in any order)
+                        if (n == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                        else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                        __syncthreads();
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+            quarter(0, a, b, x_here, w_here);
+            quarter(1, b, a, x_here, w_here);
+            quarter(2, a, b, x_here, w_here);
+            quarter(3, b, a, x_next, w_next);
+            const uint32_t w_last = w_here, x_last = x_here;
+            x_here = x_next, w_here = w_next, x_next = free, w_next = x_last, free = w_last;
+        }
+        const uint2 tile = tile_of(id, s.tiles_out, s.tiles_token);
+        finish_large<T>(sum, tile.x * 256 + out_wave, tile.y * 256 + token_wave, lane, s, e, lds + free + wave * (kPlane / 4));
+        __syncthreads();
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way to LDS that is no longer this workgroup's)
+    __syncthreads();
 }
 
 // The parts' sums of a piece of a token's outputs.
@@ -575,7 +721,15 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
         auto kernel = transposed ? linear_kernel<T, 128, 128, true> : linear_kernel<T, 128, 128, false>;
         if (plan.tile_token == 64) kernel = transposed ? linear_kernel<T, 128, 64, true> : linear_kernel<T, 128, 64, false>;
         if constexpr (sizeof(T) == 2)
-            if (plan.tile_out == 256) kernel = transposed ? large_linear_kernel<T, true> : large_linear_kernel<T, false>;
+            if (plan.tile_out == 256) {
+                const bool whole = cols % 64 == 0 && ((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(w) | x.stride * 2 | weight.stride * 2) & 15) == 0 && (!transposed || outs % 8 == 0);
+                if (whole) {
+                    launch_kernel(transposed ? direct_linear_kernel<T, true> : direct_linear_kernel<T, false>, dim3(s.tiles_out * s.tiles_token < 256 ? s.tiles_out * s.tiles_token : 256),
+                                  dim3(256), st, from, w, s, e);
+                    return;
+                }
+                kernel = transposed ? large_linear_kernel<T, true> : large_linear_kernel<T, false>;
+            }
         launch_kernel(kernel, dim3(s.tiles_out * s.tiles_token * s.parts), dim3(256), st, from, w, s, e);
         if (s.sums != nullptr) launch_join_parts(s, e, st);
     });

@@ -148,6 +148,27 @@ def test_linear_of_whole_numbers_is_exact(tokens, outs, cols, transposed, dtype)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols,shift", [(2600, 4200, 576, 0), (1300, 14000, 512, 0), (2600, 4200, 576, 3), (2590, 4100, 601, 0)])
+def test_large_linear(tokens, outs, cols, shift, transposed, dtype):
+    """More tiles than fit the chip at once, the last ones partly filled; rows that begin anywhere."""
+    print("[layers] linear, large", tokens, outs, cols, shift, transposed, dtype, flush=True)
+    x = values(tokens, cols, dtype, 1, pad=shift, shift=shift)
+    w = values(cols if transposed else outs, outs if transposed else cols, dtype, 2, pad=shift, factor=1.0 / math.sqrt(cols))
+    bias, residual = vector(outs, 3), values(tokens, outs, dtype, 4, pad=shift, shift=shift)
+    for act, b, r in ((None, None, None), ("gelu", bias, residual)):
+        (y, bound), (z, z_bound) = ref.linear(x, w, b, act, r, transposed)
+        got, before = ogq.ogq_linear(x, w, b, ACTS[act], r, transposed, keep=True)
+        ref.close(got, y, ref.rounded(bound, y, dtype), f"y {act}")
+        ref.close(before, z, ref.rounded(z_bound, z, dtype), f"before {act}")
+        wide = torch.full((tokens, outs + 8), 55.0, dtype=dtype, device=DEV)
+        out = wide[:, :outs]
+        out.copy_(values(tokens, outs, dtype, 4) if r is None else r)
+        ogq.ogq_linear(x, w, b, ACTS[act], None if r is None else out, transposed, y=out)
+        assert torch.equal(out, got) and (wide[:, outs:] == 55).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tokens", [2, 40, 200])
 def test_linear_of_infinities_and_nan(tokens, dtype):
     x, w = whole(tokens, 90, dtype, 1) + 4, whole(150, 90, dtype, 2) + 4  # no zeros
