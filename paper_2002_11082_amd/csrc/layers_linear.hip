@@ -582,6 +582,7 @@ __global__ __launch_bounds__(256, 1) void direct_linear_kernel(const T* x, const
     __syncthreads();
 #pragma unroll
     for (int m = 0; m < 8; ++m) read(a, x_here, w_here, 0, m);
+    uint32_t stores = 0;  // of the last tile, at least, that may be under way
     for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -602,9 +603,12 @@ __global__ __launch_bounds__(256, 1) void direct_linear_kernel(const T* x, const
                     if (q == 3 && m % 2 == 1) load_w.load(k, x_here, m / 2);
                     __builtin_amdgcn_sched_barrier(0);
                     if (q == 2 && m == 13) {
-                        // this wavefront's share of the next step has arrived, all but the eight loads of the one behind it (stores of the last tile may be among what is under way, in any order)
-                        if (n == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                        else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                        // This wavefront's share of the next step has arrived, all but the eight loads of the one behind it.  (In front of these, in a tile's first step, the last tile's stores:
+                        // 32 of a tile that is full, or twice as many.  They complete in the order in which they were issued.)
+                        if (n != 0) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                        else if (stores == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                        else if (stores == 32) asm volatile("s_waitcnt vmcnt(40)" ::: "memory");
+                        else asm volatile("s_waitcnt vmcnt(63)" ::: "memory");
                         __syncthreads();
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -619,6 +623,7 @@ __global__ __launch_bounds__(256, 1) void direct_linear_kernel(const T* x, const
         }
         const uint2 tile = tile_of(id, s.tiles_out, s.tiles_token);
         finish_large<T>(sum, tile.x * 256 + out_wave, tile.y * 256 + token_wave, lane, s, e, lds + free + wave * (kPlane / 4));
+        stores = (tile.x + 1) * 256 <= s.outs && (tile.y + 1) * 256 <= s.tokens ? (e.before != nullptr ? 64 : 32) : 0;
         __syncthreads();
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way to LDS that is no longer this workgroup's)
