@@ -91,10 +91,12 @@ int ogq_embedding_gradient(const void* d_tokens, uint32_t integer, size_t tokens
  * any value is the cross entropy of a label.  Rows without a place, or whose values are all -infinity, have loss 0 and gradient 0; so have rows of row_weight 0, and what they hold is
  * not looked at.  d_row_weight: [rows], NULL for 1 everywhere.  A logit of -infinity has q = 0, and the loss is infinite where p is not 0 there.  A row in which a logit or a value is NaN or +infinity
  * has NaN for both.  d_loss: fp32 [rows]; for the gradient it may be NULL.  top is at most 1024.  d_dlogits may be d_logits with the same stride. */
+size_t ogq_distill_workspace(size_t rows, size_t cols, uint32_t dtype, size_t top);
 int ogq_distill_loss(const void* d_logits, size_t stride, size_t rows, size_t cols, uint32_t dtype, const void* d_places, uint32_t integer, const float* d_values, size_t top,
-                     float temperature, const float* d_row_weight, float* d_loss, void* hip_stream);
+                     float temperature, const float* d_row_weight, float* d_loss, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 int ogq_distill_gradient(const void* d_logits, size_t stride, size_t rows, size_t cols, uint32_t dtype, const void* d_places, uint32_t integer, const float* d_values, size_t top,
-                         float temperature, const float* d_row_weight, float* d_loss, void* d_dlogits, size_t dlogits_stride, void* hip_stream);
+                         float temperature, const float* d_row_weight, float* d_loss, void* d_dlogits, size_t dlogits_stride, void* d_workspace, size_t workspace_bytes,
+                         void* hip_stream);
 
 /* Text for a status code, those of ogq.h and ogq_groups.h included (static storage, never NULL). */
 const char* ogq_layers_strerror(int status);

@@ -13,7 +13,7 @@ from .groups import (BF16, FP16, FP32, GELU, GELU_TANH, RELU, SILU, GroupParams,
                      ogq_activation_forward, ogq_group_codes_bytes, ogq_group_dequantize, ogq_group_exponents_count,
                      ogq_group_matvec, ogq_group_matvec_workspace, ogq_group_quantize, ogq_groups_strerror, ogq_weight_gradient,
                      ogq_weight_gradient_workspace)
-from .layers import (IDENTITY, INT32, INT64, layers_lib, ogq_distill_gradient, ogq_distill_loss, ogq_embedding_forward,
+from .layers import (IDENTITY, INT32, INT64, layers_lib, ogq_distill_gradient, ogq_distill_loss, ogq_distill_workspace, ogq_embedding_forward,
                      ogq_embedding_gradient, ogq_embedding_gradient_workspace, ogq_layer_norm_backward, ogq_layer_norm_backward_workspace,
                      ogq_layer_norm_forward, ogq_layers_strerror, ogq_linear, ogq_linear_backward, ogq_linear_backward_workspace,
                      ogq_linear_workspace)
@@ -25,7 +25,7 @@ __all__ = [
     "FP32", "BF16", "FP16", "RELU", "GELU", "GELU_TANH", "SILU", "GroupParams", "groups_lib", "make_group_params", "ogq_activation_backward",
     "ogq_activation_forward", "ogq_group_codes_bytes", "ogq_group_dequantize", "ogq_group_exponents_count", "ogq_group_matvec",
     "ogq_group_matvec_workspace", "ogq_group_quantize", "ogq_groups_strerror", "ogq_weight_gradient", "ogq_weight_gradient_workspace",
-    "IDENTITY", "INT32", "INT64", "layers_lib", "ogq_distill_gradient", "ogq_distill_loss", "ogq_embedding_forward",
+    "IDENTITY", "INT32", "INT64", "layers_lib", "ogq_distill_gradient", "ogq_distill_loss", "ogq_distill_workspace", "ogq_embedding_forward",
     "ogq_embedding_gradient", "ogq_embedding_gradient_workspace", "ogq_layer_norm_backward", "ogq_layer_norm_backward_workspace",
     "ogq_layer_norm_forward", "ogq_layers_strerror", "ogq_linear", "ogq_linear_backward", "ogq_linear_backward_workspace",
     "ogq_linear_workspace",

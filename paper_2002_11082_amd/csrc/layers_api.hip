@@ -247,33 +247,43 @@ int ogq_embedding_gradient(const void* d_tokens, uint32_t integer, size_t tokens
     return finish_launches();
 }
 
+size_t ogq_distill_workspace(size_t rows, size_t cols, uint32_t dtype, size_t top)
+{
+    if (check_distill(rows, cols, dtype, OGQ_INT32, top, 1.0f) != OGQ_OK || rows == 0 || cols == 0) return 0;
+    return ogq::distill_workspace(rows, cols, dtype, top);
+}
+
 int ogq_distill_loss(const void* d_logits, size_t stride, size_t rows, size_t cols, uint32_t dtype, const void* d_places, uint32_t integer, const float* d_values, size_t top,
-                     float temperature, const float* d_row_weight, float* d_loss, void* hip_stream)
+                     float temperature, const float* d_row_weight, float* d_loss, void* d_workspace, size_t workspace_bytes, void* hip_stream)
 {
     int rc = check_distill(rows, cols, dtype, integer, top, temperature);
     if (rc != OGQ_OK) return rc;
     if (rows == 0) return OGQ_OK;
     rc = first_of({check_vector(d_loss), check_optional(d_row_weight), cols != 0 ? check_values(d_logits, stride, rows, dtype) : OGQ_OK,
-                   top != 0 ? first_of({check_integers(d_places, integer), check_vector(d_values)}) : OGQ_OK});
+                   top != 0 ? first_of({check_integers(d_places, integer), check_vector(d_values)}) : OGQ_OK,
+                   check_workspace(d_workspace, workspace_bytes, cols != 0 ? ogq::distill_workspace(rows, cols, dtype, top) : 0)});
     if (rc != OGQ_OK) return rc;
     begin_launches();
-    ogq::launch_distill({d_logits, stride}, rows, cols, dtype, {d_places, integer}, d_values, top, temperature, d_row_weight, d_loss, {nullptr, 0}, stream(hip_stream));
+    ogq::launch_distill({d_logits, stride}, rows, cols, dtype, {d_places, integer}, d_values, top, temperature, d_row_weight, d_loss, {nullptr, 0}, d_workspace,
+                        stream(hip_stream));
     return finish_launches();
 }
 
 int ogq_distill_gradient(const void* d_logits, size_t stride, size_t rows, size_t cols, uint32_t dtype, const void* d_places, uint32_t integer, const float* d_values, size_t top,
-                         float temperature, const float* d_row_weight, float* d_loss, void* d_dlogits, size_t dlogits_stride, void* hip_stream)
+                         float temperature, const float* d_row_weight, float* d_loss, void* d_dlogits, size_t dlogits_stride, void* d_workspace, size_t workspace_bytes,
+                         void* hip_stream)
 {
     int rc = check_distill(rows, cols, dtype, integer, top, temperature);
     if (rc != OGQ_OK) return rc;
     if (rows == 0 || (cols == 0 && !d_loss)) return OGQ_OK;
     rc = first_of({check_optional(d_loss), check_optional(d_row_weight), cols != 0 ? check_values(d_logits, stride, rows, dtype) : OGQ_OK,
                    cols != 0 ? check_result(d_dlogits, dlogits_stride, rows, cols, dtype) : OGQ_OK,
-                   top != 0 ? first_of({check_integers(d_places, integer), check_vector(d_values)}) : OGQ_OK});
+                   top != 0 ? first_of({check_integers(d_places, integer), check_vector(d_values)}) : OGQ_OK,
+                   check_workspace(d_workspace, workspace_bytes, cols != 0 ? ogq::distill_workspace(rows, cols, dtype, top) : 0)});
     if (rc != OGQ_OK) return rc;
     begin_launches();
     ogq::launch_distill({d_logits, stride}, rows, cols, dtype, {d_places, integer}, d_values, top, temperature, d_row_weight, d_loss, {d_dlogits, dlogits_stride},
-                        stream(hip_stream));
+                        d_workspace, stream(hip_stream));
     return finish_launches();
 }
 

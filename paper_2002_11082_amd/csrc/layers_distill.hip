@@ -16,38 +16,76 @@ struct Distill {
     const void* places;
     const float *values, *row_weight;
     float* loss;
+    uint32_t slices;                // of a row, where several workgroups share it
+    float2* parts;                  // [rows][slices]: a slice's largest logit over the temperature and the sum of its exponentials
+    float* logits_there;            // [rows][top]: the logits at the teacher's places
 };
 
-// exp(x - most), x and most over the temperature: in fp32 to a few roundings of 32 bits, for 16-bit results to 2^-19 of it.
+// exp((x - most) / temperature), most being over the temperature already: in fp32 to a few roundings of 32 bits, for 16-bit results to 2^-17 of it.
 template <class T>
-__device__ __forceinline__ float exp_below(float x, float most)
-{
-    if constexpr (sizeof(T) == 4) {
-        const float d = x - most;
-        // (-infinity has no fraction, NaN none either: the instruction takes both)
-        return d < -200.0f ? 0.0f : exp_of(d, 0.0f);
-    } else {
-        return __builtin_amdgcn_exp2f((x - most) * kLog2e);
+struct ExpBelow {
+    float factor, most;
+    __device__ __forceinline__ ExpBelow(float per_temperature, float most_)
+    {
+        factor = sizeof(T) == 4 ? per_temperature : per_temperature * kLog2e;
+        most = sizeof(T) == 4 ? most_ : most_ * kLog2e;
     }
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            const float d = x * factor - most;
+            // (-infinity has no fraction, NaN none either: the instruction takes both)
+            return d < -200.0f ? 0.0f : exp_of(d, 0.0f);
+        } else {
+            return __builtin_amdgcn_exp2f(__builtin_fmaf(x, factor, -most));
+        }
+    }
+};
+
+__device__ __forceinline__ float exp_of_share(float d) { return d < -200.0f ? 0.0f : exp_of(d, 0.0f); }
+
+// Place n of a row, -1 where it stands for none.
+__device__ __forceinline__ int64_t place_at(const Distill& s, uint64_t n)
+{
+    const int64_t c = s.wide ? static_cast<const int64_t*>(s.places)[n] : (int64_t)static_cast<const int32_t*>(s.places)[n];
+    return c >= 0 && c < (int64_t)s.cols ? c : -1;
 }
 
-// A workgroup of THREADS to a row, P pieces to each, or P = 0: the row, of any length, is read for each of its passes.  The teacher's places are shared out over the threads, and are in
-// LDS for the places that are the same.
-template <class T, int THREADS, int P, bool GRADIENT>
+// What a row's workgroup is to do.
+//   kLoss      the loss
+//   kGradient  the loss and the gradient
+//   kPart      of rows that several workgroups share: largest logit and sum of exponentials of a slice; the first slice's also puts the logits at the teacher's places aside
+//   kRest      and then the loss and, where it is wanted, a slice of the gradient
+enum class Pass { kLoss, kGradient, kPart, kRest };
+
+// A workgroup of THREADS to a row (or a slice of it), P pieces to each, or P = 0: the row, of any length, is read for each of its passes.  The teacher's places are shared out over the threads, and
+// are in LDS for the places that are the same.
+template <class T, int THREADS, int P, Pass PASS>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Distill s, T* dlogits)
 {
     constexpr int N = kPiece<T>, kWaves = THREADS / 64, kMostTop = 1024, kSlots = kMostTop / THREADS, kHeld = P == 0 ? 1 : P;
+    constexpr bool kSliced = PASS == Pass::kPart || PASS == Pass::kRest, kGradient = PASS == Pass::kGradient || PASS == Pass::kRest;
+    static_assert(!kSliced || P != 0);
     __shared__ float2 space[2][kWaves];
     // a row's places and what the teacher has there: exp(value - largest)
-    __shared__ uint32_t place_of[GRADIENT ? kMostTop : 1];
-    __shared__ float weight_of[GRADIENT ? kMostTop : 1];
+    __shared__ uint32_t place_of[kGradient ? kMostTop : 1];
+    __shared__ float weight_of[kGradient ? kMostTop : 1];
     BlockSums<kWaves> sums{space};
     const uint32_t thread = threadIdx.x;
-    const uint64_t row = this_block();
+    const uint64_t row = kSliced ? this_block() / s.slices : this_block();
     if (row >= s.rows) return;
+    const uint32_t slice = kSliced ? (uint32_t)(this_block() - row * s.slices) : 0;
+    if (PASS == Pass::kRest && dlogits == nullptr && slice != 0) return;
+    // the slice's first column, and one behind its last
+    const uint32_t first = slice * (uint32_t)(THREADS * P * N), last = kSliced ? min(s.cols, first + (uint32_t)(THREADS * P * N)) : s.cols;
     const T* from = logits + row * s.stride;
-    T* to = GRADIENT ? dlogits + row * s.out_stride : nullptr;
+    T* to = kGradient ? dlogits + row * s.out_stride : nullptr;
     const float row_weight = s.row_weight == nullptr ? 1.0f : s.row_weight[row];
+    const auto at = [&](int p, uint32_t t) __attribute__((always_inline)) {
+        // (the last piece of the row's last slice ends with the row)
+        if constexpr (kSliced) return PieceAt<T>(first + (p * THREADS + t) * N, s.cols);
+        else return piece_at<T, THREADS, P == 0 ? 1 : P>(p, t, s.cols);
+    };
     uint4 held[kHeld];
     // f(values, i -> whether value i counts) for all pieces of the thread, which it may change; STORE: and they go to the gradient
     const auto each_piece = [&](auto store, auto f) __attribute__((always_inline)) {
@@ -59,11 +97,19 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
                 asm volatile("" : "+v"(t));
                 // (the values are made again from what is held, piece after piece: otherwise the compiler keeps them from one pass to the next, in registers that there are not)
                 asm volatile("" : "+v"(held[p].x), "+v"(held[p].y), "+v"(held[p].z), "+v"(held[p].w));
-                const PieceAt<T> at = piece_at<T, THREADS, P>(p, t, s.cols);
+                const PieceAt<T> piece = at(p, t);
                 values_of<T>(held[p], v);
-                f(v, [&](int i) { return at.counts(i); });
-                if constexpr (decltype(store)::value)
-                    if (at.there) store_piece<false>(to + at.col, N, v);
+                f(v, [&](int i) { return piece.counts(i); });
+                if constexpr (decltype(store)::value) {
+                    if (!piece.there) continue;
+                    if (!kSliced || piece.again == 0) {
+                        store_piece<false>(to + piece.col, N, v);
+                    } else {  // (what the last piece has of the one before it may be another workgroup's)
+#pragma unroll
+                        for (int i = 0; i < N; ++i)
+                            if (piece.counts(i)) to[piece.col + i] = (T)v[i];
+                    }
+                }
             }
         } else {
             for (uint32_t col = thread * N; col < s.cols; col += THREADS * N) {
@@ -77,10 +123,12 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
     constexpr std::true_type kStore{};
     constexpr std::false_type kOnly{};
     const auto finish_without = [&]() __attribute__((always_inline)) {
-        if (thread == 0 && s.loss != nullptr) s.loss[row] = 0.0f;
-        if constexpr (GRADIENT) {
+        if (PASS == Pass::kPart) return;
+        if (thread == 0 && slice == 0 && s.loss != nullptr) s.loss[row] = 0.0f;
+        if constexpr (kGradient) {
+            if (dlogits == nullptr) return;
             float v[N] = {};
-            for (uint32_t col = thread * N; col < s.cols; col += THREADS * N) store_piece<false>(to + col, valid_of<T>(col, s.cols), v);
+            for (uint32_t col = first + thread * N; col < last; col += THREADS * N) store_piece<false>(to + col, valid_of<T>(col, last), v);
         }
     };
     if (row_weight == 0.0f) {
@@ -89,87 +137,110 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
     }
     if constexpr (P != 0) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) held[p] = load_whole(from + piece_at<T, THREADS, P>(p, thread, s.cols).col);
+        for (int p = 0; p < P; ++p) held[p] = load_whole(from + at(p, thread).col);
     }
     // The teacher's places of this thread, their values and the student's logits there.
     uint32_t place[kSlots];
     float value[kSlots], logit[kSlots];
-    float most_value = -INFINITY, most = -INFINITY;
+    float most_value = -INFINITY, most = -INFINITY, total = 0.0f, teacher = 0.0f;
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
         const uint32_t slot = k * THREADS + thread;
         place[k] = 0xFFFFFFFFu, value[k] = -INFINITY, logit[k] = 0.0f;
-        if (slot < s.top) {
-            const uint64_t at = row * s.top + slot;
-            const int64_t c = s.wide ? static_cast<const int64_t*>(s.places)[at] : (int64_t)static_cast<const int32_t*>(s.places)[at];
-            if (c >= 0 && c < (int64_t)s.cols) {
+        if (slot < s.top && !(PASS == Pass::kPart && slice != 0)) {
+            const uint64_t n = row * s.top + slot;
+            const int64_t c = place_at(s, n);
+            if (c >= 0) {
                 place[k] = (uint32_t)c;
-                value[k] = s.values[at] * s.per_temperature;
-                logit[k] = (float)from[c] * s.per_temperature;
+                value[k] = s.values[n] * s.per_temperature;
+                logit[k] = PASS == Pass::kRest ? s.logits_there[n] : (float)from[c];
                 most_value = fmaxf(most_value, value[k]);
+                if (PASS == Pass::kPart) s.logits_there[n] = logit[k];
             }
         }
     }
-    each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
+    if constexpr (PASS == Pass::kRest) {
+        // the slices' parts, a few to a lane: all of them scaled to the largest
+        const float2* parts = s.parts + row * s.slices;
+        for (uint32_t n = thread; n < s.slices; n += THREADS) most = fmaxf(most, parts[n].x);
+        const float2 t = sums.largest(most, most_value);
+        most = t.x, most_value = t.y;
+        for (uint32_t n = thread; n < s.slices; n += THREADS) total += parts[n].y * exp_of_share(parts[n].x - most);
+    } else {
+        each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) most = fmaxf(most, P != 0 || counts(i) ? v[i] : -INFINITY);  // (twice is no harm)
-    });
-    {
+            for (int i = 0; i < N; ++i) most = fmaxf(most, P != 0 || counts(i) ? v[i] : -INFINITY);  // (twice is no harm)
+        });
         const float2 t = sums.largest(most * s.per_temperature, most_value);
         most = t.x, most_value = t.y;
-    }
-    float total = 0.0f, teacher = 0.0f;
-    each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
-        float t = 0.0f;
+        const ExpBelow<T> exp_below(s.per_temperature, most);
+        if (PASS == Pass::kPart && most == -INFINITY) {  // nothing but -infinities, of which the row may have others, and NaN
+            each_piece(kOnly, [&](const float(&v)[N], auto) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) t += counts(i) ? exp_below<T>(v[i] * s.per_temperature, most) : 0.0f;
-        total += t;
-    });
+                for (int i = 0; i < N; ++i) total += v[i] != v[i] ? v[i] : 0.0f;
+            });
+        } else {
+            each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
+                float t = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) t += counts(i) ? exp_below(v[i]) : 0.0f;
+                total += t;
+            });
+        }
+    }
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
         const bool there = place[k] != 0xFFFFFFFFu;
         // (the largest of values that are all -infinity or NaN is -infinity: of the first the row has none, the second are NaN)
         value[k] = there && value[k] != -INFINITY ? value[k] - most_value : -INFINITY;
-        const float e = there ? exp_below<float>(value[k], 0.0f) : 0.0f;
+        const float e = there ? exp_of_share(value[k]) : 0.0f;
         teacher += e;
-        if constexpr (GRADIENT) {
+        if constexpr (kGradient) {
             const uint32_t slot = k * THREADS + thread;
-            if (slot < s.top) place_of[slot] = place[k], weight_of[slot] = e;
+            if (slot < (s.top + 7) / 8 * 8) place_of[slot] = place[k], weight_of[slot] = e;  // (behind the last place: none)
         }
     }
     {
         const float2 t = sums(total, teacher);
         total = t.x, teacher = t.y;
     }
+    if constexpr (PASS == Pass::kPart) {
+        if (thread == 0) s.parts[row * s.slices + slice] = make_float2(most, total);
+        return;
+    }
     if (teacher == 0.0f) {  // no place, or none with a value
         finish_without();
         return;
     }
+    const ExpBelow<T> exp_below(s.per_temperature, most);
     const float per_teacher = 1.0f / teacher, log_teacher = logf(teacher), log_total = logf(total);
     float divergence = 0.0f;
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
-        const float p = place[k] != 0xFFFFFFFFu ? exp_below<float>(value[k], 0.0f) * per_teacher : 0.0f;
+        const float p = place[k] != 0xFFFFFFFFu ? exp_of_share(value[k]) * per_teacher : 0.0f;
         // (not equal to 0: a NaN stays)
-        if (p != 0.0f) divergence += p * ((value[k] - log_teacher) - ((logit[k] - most) - log_total));
+        if (p != 0.0f) divergence += p * ((value[k] - log_teacher) - ((logit[k] * s.per_temperature - most) - log_total));
     }
     const float2 sum = sums(divergence, 0.0f);
-    if (thread == 0 && s.loss != nullptr) s.loss[row] = row_weight * s.temperature * s.temperature * sum.x;
-    if constexpr (GRADIENT) {
-        // (a NaN of the teacher's is everywhere, one of the student's is in `total`)
-        const float factor = row_weight * s.temperature, per_total = 1.0f / total, scale = factor * per_total, none = teacher != teacher ? teacher : 0.0f;
+    if (thread == 0 && slice == 0 && s.loss != nullptr) s.loss[row] = row_weight * s.temperature * s.temperature * sum.x;
+    if constexpr (kGradient) {
+        // (a NaN of the teacher's is in `teacher`, one of the student's in `total`)
+        if (PASS == Pass::kRest && dlogits == nullptr) return;
+        const float factor = row_weight * s.temperature, per_total = 1.0f / total, scale = teacher != teacher ? teacher : factor * per_total;
         each_piece(kStore, [&](float(&v)[N], auto) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = exp_below<T>(v[i] * s.per_temperature, most) * scale + none;
+            for (int i = 0; i < N; ++i) v[i] = exp_below(v[i]) * scale;
         });
         // Behind the row's other values: the places, each with the shares of all that are the same.
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kSlots; ++k) {
-            if (place[k] == 0xFFFFFFFFu) continue;
+            if (place[k] < first || place[k] >= last) continue;  // (none is above all)
             float p = 0.0f;
-            for (uint32_t n = 0; n < s.top; ++n) p += place_of[n] == place[k] ? weight_of[n] : 0.0f;
-            to[place[k]] = (T)(factor * (exp_below<T>(logit[k], most) * per_total - p * per_teacher));
+            for (uint32_t n = 0; n < s.top; n += 8)
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) p += place_of[n + i] == place[k] ? weight_of[n + i] : 0.0f;
+            to[place[k]] = (T)(factor * (exp_below(logit[k]) * per_total - p * per_teacher));
         }
     }
 }
@@ -189,37 +260,64 @@ RowShape shape_of(size_t cols, uint32_t dtype)
     return {1024, 0};
 }
 
-template <class T, bool GRADIENT, int THREADS>
+template <class T, Pass PASS, int THREADS>
 auto kernel_of(int pieces)
 {
     if constexpr (THREADS == 256) {
-        return pieces == 1 ? distill_kernel<T, 256, 1, GRADIENT> : pieces == 2 ? distill_kernel<T, 256, 2, GRADIENT> : distill_kernel<T, 256, 4, GRADIENT>;
+        return pieces == 1 ? distill_kernel<T, 256, 1, PASS> : pieces == 2 ? distill_kernel<T, 256, 2, PASS> : distill_kernel<T, 256, 4, PASS>;
     } else {
-        return pieces == 2   ? distill_kernel<T, 1024, 2, GRADIENT>
-               : pieces == 4 ? distill_kernel<T, 1024, 4, GRADIENT>
-               : pieces == 8 ? distill_kernel<T, 1024, 8, GRADIENT>
-               : pieces == 16 ? distill_kernel<T, 1024, 16, GRADIENT>
-                              : distill_kernel<T, 1024, 0, GRADIENT>;
+        return pieces == 2   ? distill_kernel<T, 1024, 2, PASS>
+               : pieces == 4 ? distill_kernel<T, 1024, 4, PASS>
+               : pieces == 8 ? distill_kernel<T, 1024, 8, PASS>
+               : pieces == 16 ? distill_kernel<T, 1024, 16, PASS>
+                              : distill_kernel<T, 1024, 0, PASS>;
     }
+}
+
+// Several workgroups to a row, of 256 threads with four pieces each, where rows of four such slices or more leave CUs without work: a second launch and reading the row again cost less than what one
+// CU takes for the row's exponentials.  1: none.
+constexpr uint32_t kSliceThreads = 256, kSlicePieces = 4;
+uint32_t slices_of(size_t rows, size_t cols, uint32_t dtype)
+{
+    const uint64_t slices = ceil_div(cols, (uint64_t)kSliceThreads * kSlicePieces * (dtype == OGQ_FP32 ? 4 : 8));
+    return rows <= 128 && slices >= 4 ? (uint32_t)slices : 1;
 }
 
 }  // namespace
 
-void launch_distill(const Values& logits, size_t rows, size_t cols, uint32_t dtype, const Integers& places, const float* values, size_t top, float temperature,
-                    const float* row_weight, float* loss, const Result& dlogits, hipStream_t st)
+size_t distill_workspace(size_t rows, size_t cols, uint32_t dtype, size_t top)
 {
-    const Distill s{(uint32_t)rows, (uint32_t)cols, (uint32_t)top, places.type == OGQ_INT64, 1.0f / temperature, temperature, logits.stride, dlogits.stride,
-                    places.data,    values,         row_weight,    loss};
+    const uint32_t slices = slices_of(rows, cols, dtype);
+    return slices > 1 ? rows * (slices * sizeof(float2) + top * sizeof(float)) : 0;
+}
+
+void launch_distill(const Values& logits, size_t rows, size_t cols, uint32_t dtype, const Integers& places, const float* values, size_t top, float temperature,
+                    const float* row_weight, float* loss, const Result& dlogits, void* workspace, hipStream_t st)
+{
+    Distill s{};
+    s.rows = (uint32_t)rows, s.cols = (uint32_t)cols, s.top = (uint32_t)top, s.wide = places.type == OGQ_INT64;
+    s.per_temperature = 1.0f / temperature, s.temperature = temperature, s.stride = logits.stride, s.out_stride = dlogits.stride;
+    s.places = places.data, s.values = values, s.row_weight = row_weight, s.loss = loss;
+    s.slices = slices_of(rows, cols, dtype);
+    s.parts = static_cast<float2*>(workspace), s.logits_there = reinterpret_cast<float*>(s.parts + rows * s.slices);
     const RowShape shape = shape_of(cols, dtype);
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const auto go = [&](auto gradient) {
-            constexpr bool kGradient = decltype(gradient)::value;
-            const auto kernel = shape.threads == 256 ? kernel_of<T, kGradient, 256>(shape.pieces) : kernel_of<T, kGradient, 1024>(shape.pieces);
-            launch_kernel(kernel, grid_of(rows), dim3(shape.threads), st, static_cast<const T*>(logits.data), s, static_cast<T*>(dlogits.data));
+        const auto from = static_cast<const T*>(logits.data);
+        const auto to = static_cast<T*>(dlogits.data);
+        if (s.slices > 1) {
+            const dim3 grid = grid_of((uint64_t)rows * s.slices), block(kSliceThreads);
+            launch_kernel(distill_kernel<T, kSliceThreads, kSlicePieces, Pass::kPart>, grid, block, st, from, s, to);
+            launch_kernel(distill_kernel<T, kSliceThreads, kSlicePieces, Pass::kRest>, grid, block, st, from, s, to);
+            return;
+        }
+        const auto go = [&](auto pass) {
+            constexpr Pass kPass = decltype(pass)::value;
+            const auto kernel = shape.threads == 256 ? kernel_of<T, kPass, 256>(shape.pieces) : kernel_of<T, kPass, 1024>(shape.pieces);
+            launch_kernel(kernel, grid_of(rows), dim3(shape.threads), st, from, s, to);
         };
-        if (dlogits.data != nullptr) go(std::true_type{});
-        else go(std::false_type{});
+        if (to != nullptr) go(std::integral_constant<Pass, Pass::kGradient>{});
+        else go(std::integral_constant<Pass, Pass::kLoss>{});
     });
 }
 

@@ -38,8 +38,9 @@ void launch_embedding_gradient(const Integers& tokens, size_t number, const Valu
                                const Result& dtable, void* workspace, hipStream_t st);
 
 // layers_distill.hip; without a gradient dlogits.data is null
+size_t distill_workspace(size_t rows, size_t cols, uint32_t dtype, size_t top);
 void launch_distill(const Values& logits, size_t rows, size_t cols, uint32_t dtype, const Integers& places, const float* values, size_t top, float temperature,
-                    const float* row_weight, float* loss, const Result& dlogits, hipStream_t st);
+                    const float* row_weight, float* loss, const Result& dlogits, void* workspace, hipStream_t st);
 
 }  // namespace ogq
 #endif  // OGQ_LAYERS_LAUNCH_H

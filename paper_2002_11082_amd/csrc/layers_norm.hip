@@ -338,28 +338,31 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
     }
 }
 
-// The parts' sums: 32 neighbouring columns (a line) to a workgroup, eight lanes with four columns each, and 32 threads to them that take the parts in turn.
-__global__ __launch_bounds__(kBlock) void add_vectors_kernel(const float* parts, uint32_t number, uint32_t cols, uint32_t pitch, uint32_t vectors, uint32_t blocks, float* first,
-                                                           float* second, bool accumulate)
+// The parts' sums: 32 neighbouring columns (a line) to a workgroup, eight lanes with four columns each, and 128 threads to them that take the parts in turn, whose sums are then added two by two.
+__global__ __launch_bounds__(1024) void add_vectors_kernel(const float* parts, uint32_t number, uint32_t cols, uint32_t pitch, uint32_t vectors, uint32_t blocks, float* first,
+                                                         float* second, bool accumulate)
 {
-    __shared__ f32x4 shared[32][8];
+    constexpr uint32_t kTurns = 128;
+    __shared__ f32x4 shared[kTurns / 2][8];
     const uint32_t lane = threadIdx.x & 7, turn = threadIdx.x >> 3, vector = this_block() / blocks, col = (this_block() % blocks * 8 + lane) * 4;
     if (vector >= vectors) return;
     f32x4 v = {};
     if (col < cols) {
         const float* from = parts + (uint64_t)vector * pitch + col;
-#pragma unroll 16
-        for (uint32_t n = turn; n < number; n += 32) {
+#pragma unroll 8
+        for (uint32_t n = turn; n < number; n += kTurns) {
             f32x4 t;
             memcpy(&t, from + (uint64_t)n * vectors * pitch, sizeof t);
             v += t;
         }
     }
-    shared[turn][lane] = v;
-    __syncthreads();
+    for (uint32_t half = kTurns / 2; half != 0; half /= 2) {
+        if (turn >= half && turn < 2 * half) shared[turn - half][lane] = v;
+        __syncthreads();
+        if (turn < half) v += shared[turn][lane];
+        __syncthreads();
+    }
     if (turn != 0 || col >= cols) return;
-#pragma unroll
-    for (int n = 1; n < 32; ++n) v += shared[n][lane];
     float* out = (vector == 0 ? first : second) + col;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -404,7 +407,7 @@ Cut rows_cut(size_t rows, uint32_t most, uint32_t multiple)
     return {part, (uint32_t)ceil_div(rows, part)};
 }
 
-Cut backward_cut(size_t rows, const RowShape& shape) { return shape.threads == 64 ? rows_cut(rows, 512, 4) : rows_cut(rows, 512, 1); }
+Cut backward_cut(size_t rows, const RowShape& shape) { return shape.threads == 64 ? rows_cut(rows, 512, 4) : rows_cut(rows, rows >= 6144 ? 768 : 512, 1); }
 
 // Columns' blocks and rows' parts of columns_kernel.
 Cut columns_cut(size_t rows, size_t cols, uint32_t dtype)
@@ -428,7 +431,7 @@ void launch_columns(const Values& dy, const Values& x, size_t rows, size_t cols,
 void launch_add_vectors(const float* parts, uint32_t number, size_t cols, size_t pitch, float* first, float* second, bool accumulate, hipStream_t st)
 {
     const uint32_t blocks = (uint32_t)ceil_div(cols, 32), vectors = second != nullptr ? 2 : 1;
-    launch_kernel(add_vectors_kernel, grid_of((uint64_t)blocks * vectors), dim3(kBlock), st, parts, number, (uint32_t)cols, (uint32_t)pitch, vectors, blocks, first, second, accumulate);
+    launch_kernel(add_vectors_kernel, grid_of((uint64_t)blocks * vectors), dim3(1024), st, parts, number, (uint32_t)cols, (uint32_t)pitch, vectors, blocks, first, second, accumulate);
 }
 
 void launch_layer_norm_forward(const Values& x, size_t rows, size_t cols, uint32_t dtype, const float* weight, const float* bias, float eps, const Result& y, float* mean,

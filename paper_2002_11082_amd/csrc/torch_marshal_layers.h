@@ -13,6 +13,7 @@ struct BoundLayers {
     decltype(&ogq_embedding_forward) embedding_forward = nullptr;
     decltype(&ogq_embedding_gradient_workspace) embedding_workspace = nullptr;
     decltype(&ogq_embedding_gradient) embedding_gradient = nullptr;
+    decltype(&ogq_distill_workspace) distill_workspace = nullptr;
     decltype(&ogq_distill_loss) distill_loss = nullptr;
     decltype(&ogq_distill_gradient) distill_gradient = nullptr;
     PyObject* check = nullptr;  // callable: raises OgqError for a status other than 0
@@ -290,53 +291,60 @@ struct Divergence {
         temperature = float_of(args[3]);
         row_weight = Vector(args[4], logits.rows, logits.t, "row_weight");
     }
+    at::Tensor workspace(PyObject* given) const { return workspace_of(given, bound_layers.distill_workspace(logits.rows, logits.cols, logits.dtype, top), logits.t); }
     const float* values_in() const { return static_cast<const float*>(values.const_data_ptr()); }
 };
 
-// distill_loss(logits, places, values, temperature, row_weight or None, loss or None) -> loss
+// distill_loss(logits, places, values, temperature, row_weight or None, loss or None, workspace or None) -> loss
 PyObject* distill_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
-    if (!argument_count(nargs, 6)) return nullptr;
+    if (!argument_count(nargs, 7)) return nullptr;
     return guarded_layers([&]() -> PyObject* {
         const Divergence d(args);
         const Vector loss = vector_result(args[5], d.logits.rows, d.logits.t, "loss");
+        const at::Tensor space = d.workspace(args[6]);
+        void* workspace = space.defined() ? space.data_ptr() : nullptr;
+        const size_t bytes = space.defined() ? space.nbytes() : 0;
         const void *from = d.logits.in(), *places = d.places.const_data_ptr();
         float* to = loss.out();
         call_layers(d.logits.t, [&](void* st) {
             return bound_layers.distill_loss(from, d.logits.stride, d.logits.rows, d.logits.cols, d.logits.dtype, places, d.integer, d.values_in(), d.top, d.temperature,
-                                             d.row_weight.in(), to, st);
+                                             d.row_weight.in(), to, workspace, bytes, st);
         });
         written(args[5], loss.t);
         return THPVariable_Wrap(loss.t);
     });
 }
 
-// distill_gradient(logits, places, values, temperature, row_weight or None, dlogits or None, loss or None) -> (loss, dlogits)
+// distill_gradient(logits, places, values, temperature, row_weight or None, dlogits or None, loss or None, workspace or None) -> (loss, dlogits)
 PyObject* distill_gradient(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
-    if (!argument_count(nargs, 7)) return nullptr;
+    if (!argument_count(nargs, 8)) return nullptr;
     return guarded_layers([&]() -> PyObject* {
         const Divergence d(args);
         const Matrix dlogits = result(args[5], d.logits.rows, d.logits.cols, d.logits.t.scalar_type(), d.logits.t, "dlogits");
         const Vector loss = vector_result(args[6], d.logits.rows, d.logits.t, "loss");
+        const at::Tensor space = d.workspace(args[7]);
+        void* workspace = space.defined() ? space.data_ptr() : nullptr;
+        const size_t bytes = space.defined() ? space.nbytes() : 0;
         const void *from = d.logits.in(), *places = d.places.const_data_ptr();
         void* to = dlogits.out();
         float* to_loss = loss.out();
         call_layers(d.logits.t, [&](void* st) {
             return bound_layers.distill_gradient(from, d.logits.stride, d.logits.rows, d.logits.cols, d.logits.dtype, places, d.integer, d.values_in(), d.top, d.temperature,
-                                                 d.row_weight.in(), to_loss, to, dlogits.stride, st);
+                                                 d.row_weight.in(), to_loss, to, dlogits.stride, workspace, bytes, st);
         });
         written(args[5], dlogits.t), written(args[6], loss.t);
         return pack({loss.t, dlogits.t});
     });
 }
 
-// bind_layers(addresses of the twelve functions in the order of BoundLayers, check)
+// bind_layers(addresses of the thirteen functions in the order of BoundLayers, check)
 PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
-    if (!argument_count(nargs, 13)) return nullptr;
-    void* address[12];
-    for (int i = 0; i < 12; ++i) {
+    if (!argument_count(nargs, 14)) return nullptr;
+    void* address[13];
+    for (int i = 0; i < 13; ++i) {
         address[i] = PyLong_AsVoidPtr(args[i]);
         if (!address[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "address 0");
@@ -354,10 +362,11 @@ PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     b.embedding_forward = reinterpret_cast<decltype(b.embedding_forward)>(address[7]);
     b.embedding_workspace = reinterpret_cast<decltype(b.embedding_workspace)>(address[8]);
     b.embedding_gradient = reinterpret_cast<decltype(b.embedding_gradient)>(address[9]);
-    b.distill_loss = reinterpret_cast<decltype(b.distill_loss)>(address[10]);
-    b.distill_gradient = reinterpret_cast<decltype(b.distill_gradient)>(address[11]);
-    Py_INCREF(args[12]);
+    b.distill_workspace = reinterpret_cast<decltype(b.distill_workspace)>(address[10]);
+    b.distill_loss = reinterpret_cast<decltype(b.distill_loss)>(address[11]);
+    b.distill_gradient = reinterpret_cast<decltype(b.distill_gradient)>(address[12]);
+    Py_INCREF(args[13]);
     Py_XDECREF(b.check);
-    b.check = args[12];
+    b.check = args[13];
     Py_RETURN_NONE;
 }

@@ -43,8 +43,9 @@ def layers_lib() -> ctypes.CDLL:
                 ("ogq_embedding_forward", i32, [vp, u32, sz, vp, sz, sz, sz, u32, f32, vp, sz, vp]),
                 ("ogq_embedding_gradient_workspace", sz, [sz, sz, sz]),
                 ("ogq_embedding_gradient", i32, [vp, u32, sz, vp, sz, sz, sz, u32, f32, i32, vp, sz, vp, sz, vp]),
-                ("ogq_distill_loss", i32, [vp, sz, sz, sz, u32, vp, u32, vp, sz, f32, vp, vp, vp]),
-                ("ogq_distill_gradient", i32, [vp, sz, sz, sz, u32, vp, u32, vp, sz, f32, vp, vp, vp, sz, vp]),
+                ("ogq_distill_workspace", sz, [sz, sz, u32, sz]),
+                ("ogq_distill_loss", i32, [vp, sz, sz, sz, u32, vp, u32, vp, sz, f32, vp, vp, vp, sz, vp]),
+                ("ogq_distill_gradient", i32, [vp, sz, sz, sz, u32, vp, u32, vp, sz, f32, vp, vp, vp, sz, vp, sz, vp]),
                 ("ogq_layers_strerror", ctypes.c_char_p, [i32]),
                 ("ogq_layers_last_hip_error", i32, [])):
             f = getattr(L, name)
@@ -81,6 +82,11 @@ def ogq_embedding_gradient_workspace(tokens: int, vocab: int, cols: int) -> int:
     return layers_lib().ogq_embedding_gradient_workspace(tokens, vocab, cols)
 
 
+def ogq_distill_workspace(rows: int, cols: int, dtype: int, top: int) -> int:
+    """dtype: FP32, BF16 or FP16."""
+    return layers_lib().ogq_distill_workspace(rows, cols, dtype, top)
+
+
 _marshal = None
 
 
@@ -91,7 +97,7 @@ def _load_marshal():
     addresses = [ctypes.cast(f, ctypes.c_void_p).value
                  for f in (L.ogq_layer_norm_forward, L.ogq_layer_norm_backward_workspace, L.ogq_layer_norm_backward, L.ogq_linear_workspace, L.ogq_linear,
                            L.ogq_linear_backward_workspace, L.ogq_linear_backward, L.ogq_embedding_forward, L.ogq_embedding_gradient_workspace,
-                           L.ogq_embedding_gradient, L.ogq_distill_loss, L.ogq_distill_gradient)]
+                           L.ogq_embedding_gradient, L.ogq_distill_workspace, L.ogq_distill_loss, L.ogq_distill_gradient)]
     module.bind_layers(*addresses, _check)
     _marshal = module
     return module
@@ -131,12 +137,12 @@ def ogq_embedding_gradient(tokens, dy, vocab: int, scale: float = 1.0, dtable=No
     return (_marshal or _load_marshal()).embedding_gradient(tokens, dy, vocab, scale, dtable, accumulate, workspace)
 
 
-def ogq_distill_loss(logits, places, values, temperature: float = 1.0, row_weight=None, loss=None):
+def ogq_distill_loss(logits, places, values, temperature: float = 1.0, row_weight=None, loss=None, workspace=None):
     """The divergence [rows] of softmax(logits / temperature) from the teacher's distribution over `places` [rows, top], softmax(values / temperature), times temperature^2 and the row's
     weight.  A place that is not in the row stands for none."""
-    return (_marshal or _load_marshal()).distill_loss(logits, places, values, temperature, row_weight, loss)
+    return (_marshal or _load_marshal()).distill_loss(logits, places, values, temperature, row_weight, loss, workspace)
 
 
-def ogq_distill_gradient(logits, places, values, temperature: float = 1.0, row_weight=None, dlogits=None, loss=None):
+def ogq_distill_gradient(logits, places, values, temperature: float = 1.0, row_weight=None, dlogits=None, loss=None, workspace=None):
     """(loss, dlogits): the same and the gradient of its sum, in one pass over the logits.  dlogits may be logits."""
-    return (_marshal or _load_marshal()).distill_gradient(logits, places, values, temperature, row_weight, dlogits, loss)
+    return (_marshal or _load_marshal()).distill_gradient(logits, places, values, temperature, row_weight, dlogits, loss, workspace)

@@ -284,7 +284,8 @@ def teacher(rows, cols, top, seed, ids=torch.int64):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,top,pad", [(1, 1, 1, 0), (3, 5, 4, 1), (2, 8, 8, 0), (4, 100, 3, 0), (3, 1000, 1024, 0), (5, 1025, 20, 2), (2, 2048, 1, 0), (3, 4099, 64, 0), (2, 8192, 300, 0),
-                                               (2, 8200, 5, 3), (2, 20000, 64, 0), (2, 32769, 100, 1), (2, 65536, 64, 0), (1, 100003, 10, 0), (1, 131072, 64, 0), (1, 140001, 64, 0), (300, 300, 7, 0)])
+                                               (2, 8200, 5, 3), (2, 20000, 64, 0), (2, 32769, 100, 1), (2, 65536, 64, 0), (1, 100003, 10, 0), (1, 131072, 64, 0), (1, 140001, 64, 0), (300, 300, 7, 0),
+                                               (128, 33001, 9, 0), (129, 33001, 9, 1), (70, 49153, 200, 3)])
 def test_distill(rows, cols, top, pad, dtype):
     print("[layers] distill", rows, cols, top, pad, dtype, flush=True)
     logits = values(rows, cols, dtype, 1, pad, shift=pad % 2, factor=3.0)
@@ -300,7 +301,7 @@ def test_distill(rows, cols, top, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("cols", [6, 700, 9000, 140000])
+@pytest.mark.parametrize("cols", [6, 700, 9000, 40000, 140000])
 def test_distill_of_rows_that_are_empty_or_bad(cols, dtype):
     rows = 12
     logits = values(rows, cols, dtype, 1)
@@ -319,6 +320,7 @@ def test_distill_of_rows_that_are_empty_or_bad(cols, dtype):
     weight[9], logits[9, 3] = 0.0, math.nan  # a row that is not looked at
     places[10] = 3                      # one place five times
     logits[11] = -60000.0
+    logits[2, 100:] = -math.inf         # all but the row's first logits masked
     (loss, b), (d, bd) = ref.distill(logits, places, v, 1.0, weight)
     got, dlogits = ogq.ogq_distill_gradient(logits, places, v, 1.0, weight)
     assert (got[[0, 1, 9]] == 0).all() and (dlogits[[0, 1, 9]] == 0).all()
