@@ -68,8 +68,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
     static_assert(!kSliced || P != 0);
     __shared__ float2 space[2][kWaves];
     // a row's places and what the teacher has there: exp(value - largest)
-    __shared__ uint32_t place_of[kGradient ? kMostTop : 1];
-    __shared__ float weight_of[kGradient ? kMostTop : 1];
+    __shared__ __align__(16) uint32_t place_of[kGradient ? kMostTop : 1];
+    __shared__ __align__(16) float weight_of[kGradient ? kMostTop : 1];
     BlockSums<kWaves> sums{space};
     const uint32_t thread = threadIdx.x;
     const uint64_t row = kSliced ? this_block() / s.slices : this_block();
@@ -237,9 +237,12 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
         for (int k = 0; k < kSlots; ++k) {
             if (place[k] < first || place[k] >= last) continue;  // (none is above all)
             float p = 0.0f;
-            for (uint32_t n = 0; n < s.top; n += 8)
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) p += place_of[n + i] == place[k] ? weight_of[n + i] : 0.0f;
+            for (uint32_t n = 0; n < s.top; n += 8) {
+                const uint4 a = *reinterpret_cast<const uint4*>(place_of + n), b = *reinterpret_cast<const uint4*>(place_of + n + 4);
+                const float4 c = *reinterpret_cast<const float4*>(weight_of + n), d = *reinterpret_cast<const float4*>(weight_of + n + 4);
+                p += a.x == place[k] ? c.x : 0.0f, p += a.y == place[k] ? c.y : 0.0f, p += a.z == place[k] ? c.z : 0.0f, p += a.w == place[k] ? c.w : 0.0f;
+                p += b.x == place[k] ? d.x : 0.0f, p += b.y == place[k] ? d.y : 0.0f, p += b.z == place[k] ? d.z : 0.0f, p += b.w == place[k] ? d.w : 0.0f;
+            }
             to[place[k]] = (T)(factor * (exp_below(logit[k]) * per_total - p * per_teacher));
         }
     }
