@@ -280,25 +280,15 @@ __device__ __forceinline__ void mend_sums(const float* x, const float* weight, c
         }
 }
 
-// The pairs of pieces whose products count: all but those below 2^-24 of the largest.
-template <class T, class F>
-__device__ __forceinline__ void each_pair(F f)
-{
-    if constexpr (kPlanes<T> == 1) {
-        f(0, 0);
-    } else {
-        f(2, 0), f(0, 2), f(1, 1), f(1, 0), f(0, 1), f(0, 0);
-    }
-}
-
-// Tiles of OUT outputs by TOKENS tokens, a quarter in each of four wavefronts.
+// Tiles of OUT outputs by TOKENS tokens, a quarter in each of four wavefronts.  In 16 bits two stages of LDS and one barrier a step: while one step is multiplied the next one waits in registers,
+// goes to LDS behind the products, and the one behind it sets off.  fp32, whose three pieces fill LDS, has one stage and two barriers, and more workgroups to a CU.
 template <class T, int OUT, int TOKENS, bool TRANSPOSED>
 __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
 {
     using FeedW = std::conditional_t<TRANSPOSED, Across<T, OUT, false>, Along<T, OUT, false>>;
     using FeedX = Along<T, TOKENS, false>;
-    constexpr int kBytesW = kPlanes<T> * FeedW::kPlane, kStage = kBytesW + kPlanes<T> * FeedX::kPlane, NO = OUT / 64, NT = TOKENS / 64;
-    constexpr int kBytes = kStage > 4 * kTurn<NO> ? kStage : 4 * kTurn<NO>;
+    constexpr int kBytesW = kPlanes<T> * FeedW::kPlane, kStage = kBytesW + kPlanes<T> * FeedX::kPlane, NO = OUT / 64, NT = TOKENS / 64, kStages = sizeof(T) == 2 ? 2 : 1, D = kDepth<T>;
+    constexpr int kBytes = kStages * kStage > 4 * kTurn<NO> ? kStages * kStage : 4 * kTurn<NO>;
     __shared__ __align__(16) char lds[kBytes];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t tiles = s.tiles_out * s.tiles_token, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
@@ -317,26 +307,60 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
             feed_x.fetch_asking(k);
         }
     };
+    const auto bring = [&](uint32_t stage) __attribute__((always_inline)) {
+        feed_w.bring(stage * kStage);
+        feed_x.bring(stage * kStage);
+    };
+    // The pairs of pieces of a step's slices of 16, one behind the other; the operands of one are read while the one before it is multiplied.
+    constexpr int kPairs = kPlanes<T> == 1 ? 1 : 6, kSlices = D / 16;
+    struct Operands {
+        s16x8 w[NO], x[NT];
+    };
+    const auto read = [&](Operands& r, const char* at, int n) __attribute__((always_inline)) {
+        constexpr int kW[6] = {2, 0, 1, 1, 0, 0}, kX[6] = {0, 2, 1, 0, 1, 0};  // (all but those below 2^-24 of the largest, the smallest first)
+        const int h = n / kPairs, p = kPairs == 1 ? 0 : kW[n % 6], q = kPairs == 1 ? 0 : kX[n % 6];
+#pragma unroll
+        for (int i = 0; i < NO; ++i) r.w[i] = FeedW::read(at + p * FeedW::kPlane, out_wave + 32 * i, h, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) r.x[j] = FeedX::read(at + kBytesW + q * FeedX::kPlane, token_wave + 32 * j, h, lane);
+    };
+    const auto products = [&](uint32_t stage) __attribute__((always_inline)) {
+        const char* at = lds + stage * kStage;
+        Operands r[2];
+        read(r[0], at, 0);
+#pragma unroll
+        for (int n = 0; n < kSlices * kPairs; ++n) {
+            if (n + 1 < kSlices * kPairs) read(r[(n + 1) & 1], at, n + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                asm volatile("" : "+v"(r[n & 1].x[j]));  // (a product has no other order than that of what it takes)
+#pragma unroll
+                for (int i = 0; i < NO; ++i) sum[i][j] = multiply_add<T>(r[n & 1].w[i], r[n & 1].x[j], sum[i][j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     fetch(first);
-    for (uint32_t k = first; k < last; k += kDepth<T>) {
-        __syncthreads();
-        feed_w.bring(0);
-        feed_x.bring(0);
-        __syncthreads();
-        fetch(k + kDepth<T>);
-#pragma unroll
-        for (int h = 0; h < kDepth<T> / 16; ++h)
-            each_pair<T>([&](int p, int q) __attribute__((always_inline)) {
-                s16x8 a[NO], b[NT];
-#pragma unroll
-                for (int i = 0; i < NO; ++i) a[i] = FeedW::read(lds + p * FeedW::kPlane, out_wave + 32 * i, h, lane);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) b[j] = FeedX::read(lds + kBytesW + q * FeedX::kPlane, token_wave + 32 * j, h, lane);
-#pragma unroll
-                for (int i = 0; i < NO; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) sum[i][j] = multiply_add<T>(a[i], b[j], sum[i][j]);
-            });
+    if constexpr (kStages == 2) {
+        if (first < last) bring(0);
+        fetch(first + kDepth<T>);
+        uint32_t stage = 0;
+        for (uint32_t k = first; k < last; k += kDepth<T>) {
+            __syncthreads();
+            products(stage);
+            stage ^= 1;
+            if (k + kDepth<T> < last) bring(stage);
+            fetch(k + 2 * kDepth<T>);
+        }
+    } else {
+        for (uint32_t k = first; k < last; k += kDepth<T>) {
+            __syncthreads();
+            bring(0);
+            __syncthreads();
+            fetch(k + kDepth<T>);
+            products(0);
+        }
     }
     __syncthreads();
     if constexpr (sizeof(T) == 4) mend_sums<TRANSPOSED>(x, weight, s, out + out_wave, token + token_wave, first, last, lane, sum);
@@ -655,28 +679,45 @@ struct Plan {
     uint32_t tile_out, tile_token, tiles_out, tiles_token, part, parts;
 };
 
+// Which tiles, and into how many parts a sum is cut: what takes least by this account, in us.  With c workgroups on a CU a step (64 columns in 16 bits, 32 in fp32) takes a + b c, of which
+// a CU holds up to `most`; parts cost a launch of 3.5 us, 0.3 us each, and 8 bytes for each of their sums, written and read, at 4 TB/s.
+//   16 bits: 64 x 64 0.28 + 0.17 c, 128 x 64 0.27 + 0.26 c, 128 x 128 0.52 + 0.26 c, 256 x 256 (no parts) 1.6 and 10 a tile;  fp32: 128 x 64 0.5 + 0.63 c, 128 x 128 1.0 + 0.8 c.
+// Measured for x [tokens, cols] to outs (fp16; by tile and parts): 1000 x 1000 to 1000: 64 x 64 9.0 in one part, 14.8 in two, 128 x 128 16.9; 128 x 4096 to 4096: 64 x 64 29.3 in one, 16.5 in 4, 18.7 in 8,
+// 128 x 128 50.7 in one, 19.4 in 6; 256 x 25088 to 4096: 128 x 128 148 in 2, 74.9 in 8, 92.4 in 12, 64 x 64 98.8 in 2; 2000 x 2048 to 2048: 64 x 64 33.5, 128 x 64 28.3, 128 x 128 30.4, in two parts 36.8; 4096
+// x 512 to 512: 64 x 64 7.8, 128 x 128 11.3.  fp32: 128 x 4096 to 4096: 128 x 64 148 in one, 46.3 in 4, 38.5 in 8, 128 x 128 38.6 in 16; 256 x 25088 to 4096: 128 x 128 301 in 8, 297 in 12, 128 x 64 341 in 8; 2000 x
+// 2048 to 2048: 128 x 128 123 in one, 106 in 2.
 // near: whether a tile's rows of both factors lie within 2^32 bytes.
+struct Tile {
+    uint32_t out, token, most;
+    double a, b;
+};
+
 Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool near)
 {
-    Plan p;
-    const uint32_t depth = dtype == OGQ_FP32 ? 32 : 64;
-    p.tiles_out = (uint32_t)ceil_div(outs, 256), p.tiles_token = (uint32_t)ceil_div(tokens, 256);
-    if (dtype != OGQ_FP32 && near && tokens > 128 && (uint64_t)p.tiles_out * p.tiles_token >= 160 && cols >= 512) {
-        p.tile_out = p.tile_token = 256, p.part = (uint32_t)cols, p.parts = 1;
-        return p;
+    static constexpr Tile kHalf[] = {{64, 64, 5, 0.28, 0.17}, {128, 64, 3, 0.27, 0.26}, {128, 128, 2, 0.52, 0.26}}, kFull[] = {{128, 64, 4, 0.5, 0.63}, {128, 128, 3, 1.0, 0.8}};
+    const bool fp32 = dtype == OGQ_FP32;
+    const uint32_t depth = fp32 ? 32 : 64, kinds = fp32 ? 2 : 3;
+    const uint64_t steps = ceil_div(cols, depth);
+    Plan p{};
+    double least = 1e300;
+    if (!fp32 && near && cols >= 512 && tokens > 128 && outs > 128) {
+        const uint64_t tiles = ceil_div(outs, 256) * ceil_div(tokens, 256);
+        least = (double)ceil_div(tiles, 256) * ((double)steps * 1.6 + 10.0);
+        p = {256, 256, (uint32_t)ceil_div(outs, 256), (uint32_t)ceil_div(tokens, 256), (uint32_t)cols, 1};
     }
-    p.tile_out = 128;
-    p.tile_token = tokens <= 64 ? 64 : 128;
-    p.tiles_out = (uint32_t)ceil_div(outs, p.tile_out), p.tiles_token = (uint32_t)ceil_div(tokens, p.tile_token);
-    const uint64_t tiles = (uint64_t)p.tiles_out * p.tiles_token, steps = ceil_div(cols, depth);
-    uint64_t parts = 1;
-    if (tiles < 512) {
-        parts = 512 / tiles;
-        if (parts > steps / 4) parts = steps / 4;
-        if (parts < 1) parts = 1;
+    for (uint32_t n = 0; n < kinds; ++n) {
+        const Tile& t = fp32 ? kFull[n] : kHalf[n];
+        const uint64_t tiles = ceil_div(outs, t.out) * ceil_div(tokens, t.token);
+        for (uint64_t parts = 1; parts <= 32 && (parts == 1 || (parts <= steps / 2 && tiles * parts <= 1024)); ++parts) {
+            const uint64_t each = ceil_div(steps, parts), slots = 256 * t.most, full = tiles * parts / slots, rest = tiles * parts % slots;
+            const double step = (double)full * (t.a + t.b * (double)t.most) + (rest != 0 ? t.a + t.b * (double)ceil_div(rest, 256) : 0.0);
+            const double join = parts > 1 ? 3.5 + 0.3 * (double)parts + 2e-6 * (double)parts * (double)tokens * (double)outs : 0.0, cost = step * (double)each + join;
+            if (cost >= least) continue;
+            least = cost;
+            p = {t.out, t.token, (uint32_t)ceil_div(outs, t.out), (uint32_t)ceil_div(tokens, t.token), steps == 0 ? depth : (uint32_t)(each * depth), 1};
+            p.parts = steps == 0 ? 1 : (uint32_t)ceil_div(cols, p.part);
+        }
     }
-    p.part = steps == 0 ? depth : (uint32_t)(ceil_div(steps, parts) * depth);
-    p.parts = steps == 0 ? 1 : (uint32_t)ceil_div(cols, p.part);
     return p;
 }
 
@@ -718,13 +759,19 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
             launch_few(plan, from, w, transposed, s, e, st);
             return;
         }
-        // (more parts where they are not near there are not: the large tiles are enough for the chip, and the small ones are more)
+        // (with rows that are not near, what takes large tiles elsewhere takes others in one part: the workspace is what the sizes say)
         const bool near = x.stride < ((size_t)1 << 23) && weight.stride < ((size_t)1 << 23) && outs < ((size_t)1 << 30);
-        const Plan plan = plan_of(tokens, outs, cols, dtype, near);
+        Plan plan = plan_of(tokens, outs, cols, dtype, true);
+        if (plan.tile_out == 256 && !near) {
+            plan = plan_of(tokens, outs, cols, dtype, false);
+            plan.part = (uint32_t)cols, plan.parts = 1;
+        }
         s.tiles_out = plan.tiles_out, s.tiles_token = plan.tiles_token, s.part = plan.part, s.parts = plan.parts;
         s.sums = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
         auto kernel = transposed ? linear_kernel<T, 128, 128, true> : linear_kernel<T, 128, 128, false>;
         if (plan.tile_token == 64) kernel = transposed ? linear_kernel<T, 128, 64, true> : linear_kernel<T, 128, 64, false>;
+        if constexpr (sizeof(T) == 2)
+            if (plan.tile_out == 64) kernel = transposed ? linear_kernel<T, 64, 64, true> : linear_kernel<T, 64, 64, false>;
         if constexpr (sizeof(T) == 2)
             if (plan.tile_out == 256) {
                 const bool whole = cols % 64 == 0 && ((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(w) | x.stride * 2 | weight.stride * 2) & 15) == 0 && (!transposed || outs % 8 == 0);

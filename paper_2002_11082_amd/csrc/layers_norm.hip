@@ -119,8 +119,19 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* 
 struct RowParts {
     uint32_t rows, cols, part, pitch;
     float per_col;
-    float* parts;  // null: no sums
+    float* parts;  // null: no sums, or those of the only part
+    float *first, *second;  // where these go: weight and bias, or the one vector there is, in `first`
+    bool accumulate;
 };
+
+// Sums of an only part: one or two vectors, of which a thread has these values.
+template <int N, class F>
+__device__ __forceinline__ void store_only(float* to, bool accumulate, const float (&v)[N], F counts)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (counts(i)) to[i] = accumulate ? to[i] + v[i] : v[i];
+}
 
 // The backward pass of rows that THREADS threads hold, P pieces each.  A row's values set off while the one before is worked on.  64 threads to a row: the four wavefronts of a workgroup
 // take its rows in turn, and add their sums over the rows in LDS in the end.
@@ -186,8 +197,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
             store_piece<false>(to + at(p).col, N, g[p]);
         }
     }
-    if (s.parts == nullptr) return;
-    float* out = s.parts + (uint64_t)this_block() * 2 * s.pitch;
+    if (s.parts == nullptr && s.first == nullptr) return;
     if constexpr (THREADS == 64) {
         __shared__ float shared[2][64 * P * N];
         // wavefront after wavefront, in their order
@@ -217,6 +227,12 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         if (!at(p).there) continue;
+        if (s.parts == nullptr) {
+            store_only(s.first + at(p).col, s.accumulate, dw[p], [&](int i) { return at(p).counts(i); });
+            store_only(s.second + at(p).col, s.accumulate, db[p], [&](int i) { return at(p).counts(i); });
+            continue;
+        }
+        float* out = s.parts + (uint64_t)this_block() * 2 * s.pitch;
         memcpy(out + at(p).col, dw[p], sizeof dw[p]);
         memcpy(out + s.pitch + at(p).col, db[p], sizeof db[p]);
     }
@@ -318,7 +334,7 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
             }
         }
     }
-    if (s.parts == nullptr) return;
+    if (s.parts == nullptr && s.first == nullptr) return;
     __shared__ float shared[kVectors][N][3][64];
     if (wave != 0) {
 #pragma unroll
@@ -334,7 +350,8 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int w = 0; w < 3; ++w) sum[k][i] += shared[k][i][w][lane];
-        memcpy(s.parts + ((uint64_t)part * kVectors + k) * s.pitch + col, sum[k], sizeof sum[k]);
+        if (s.parts == nullptr) store_only((k == 0 ? s.first : s.second) + col, s.accumulate, sum[k], [&](int i) { return i < valid; });
+        else memcpy(s.parts + ((uint64_t)part * kVectors + k) * s.pitch + col, sum[k], sizeof sum[k]);
     }
 }
 
@@ -417,11 +434,9 @@ Cut columns_cut(size_t rows, size_t cols, uint32_t dtype)
 }
 
 template <class T, Columns WHAT>
-void launch_columns(const Values& dy, const Values& x, size_t rows, size_t cols, const Cut& cut, float* parts, const float* mean, const float* rstd, uint32_t act, const Result& dz,
-                    hipStream_t st)
+void launch_columns(const Values& dy, const Values& x, const RowParts& s, const Cut& cut, const float* mean, const float* rstd, uint32_t act, const Result& dz, hipStream_t st)
 {
-    const RowParts s{(uint32_t)rows, (uint32_t)cols, cut.part, pitch_of(cols), 0.0f, parts};
-    const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
+    const uint32_t blocks = (uint32_t)ceil_div(s.cols, 64 * kPiece<T>);
     launch_kernel(columns_kernel<T, WHAT>, grid_of((uint64_t)blocks * cut.parts), dim3(kBlock), st, static_cast<const T*>(dy.data), dy.stride,
                   static_cast<const T*>(x.data), x.stride, s, blocks, mean, rstd, act, static_cast<T*>(dz.data), dz.stride);
 }
@@ -463,7 +478,13 @@ size_t layer_norm_backward_workspace(size_t rows, size_t cols, uint32_t dtype)
 {
     const RowShape shape = shape_of(cols, dtype, 2);
     const Cut cut = shape.threads != 0 ? backward_cut(rows, shape) : columns_cut(rows, cols, dtype);
-    return (size_t)cut.parts * 2 * pitch_of(cols) * sizeof(float);
+    return cut.parts > 1 ? (size_t)cut.parts * 2 * pitch_of(cols) * sizeof(float) : 0;
+}
+
+// The sums of a call's parts: to the workspace, and from there added up, or those of the only part straight to where they belong.
+RowParts parts_of(size_t rows, size_t cols, const Cut& cut, float per_col, void* workspace, float* first, float* second, bool accumulate)
+{
+    return {(uint32_t)rows, (uint32_t)cols, cut.part, pitch_of(cols), per_col, first != nullptr && cut.parts > 1 ? static_cast<float*>(workspace) : nullptr, first, second, accumulate};
 }
 
 void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, size_t cols, uint32_t dtype, const float* weight, const float* mean, const float* rstd,
@@ -475,18 +496,17 @@ void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, 
     }
     const RowShape shape = shape_of(cols, dtype, 2);
     const float per_col = (float)(1.0 / (double)cols);
-    float* parts = dweight != nullptr ? static_cast<float*>(workspace) : nullptr;
-    Cut cut = shape.threads != 0 ? backward_cut(rows, shape) : columns_cut(rows, cols, dtype);
+    const Cut cut = shape.threads != 0 ? backward_cut(rows, shape) : columns_cut(rows, cols, dtype);
+    const RowParts s = parts_of(rows, cols, cut, per_col, workspace, dweight, dbias, accumulate);
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         if (shape.threads == 0) {
             // (the sums first: dx may lie where dy is)
-            if (parts != nullptr) launch_columns<T, Columns::kNorm>(dy, x, rows, cols, cut, parts, mean, rstd, 0, {nullptr, 0}, st);
+            if (dweight != nullptr) launch_columns<T, Columns::kNorm>(dy, x, s, cut, mean, rstd, 0, {nullptr, 0}, st);
             launch_kernel(layer_norm_backward_long_kernel<T>, grid_of(rows), dim3(1024), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data),
                           x.stride, (uint32_t)rows, (uint32_t)cols, per_col, weight, mean, rstd, static_cast<T*>(dx.data), dx.stride);
             return;
         }
-        const RowParts s{(uint32_t)rows, (uint32_t)cols, cut.part, pitch_of(cols), per_col, parts};
         const auto pick = [&](auto n) {
             constexpr int kThreads = decltype(n)::value;
             if (shape.threads != kThreads) return;
@@ -496,10 +516,14 @@ void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, 
         };
         pick(std::integral_constant<int, 64>{}), pick(std::integral_constant<int, 256>{}), pick(std::integral_constant<int, 1024>{});
     });
-    if (parts != nullptr) launch_add_vectors(parts, cut.parts, cols, pitch_of(cols), dweight, dbias, accumulate, st);
+    if (s.parts != nullptr) launch_add_vectors(s.parts, cut.parts, cols, s.pitch, dweight, dbias, accumulate, st);
 }
 
-size_t linear_backward_workspace(size_t tokens, size_t outs, uint32_t dtype) { return (size_t)columns_cut(tokens, outs, dtype).parts * pitch_of(outs) * sizeof(float); }
+size_t linear_backward_workspace(size_t tokens, size_t outs, uint32_t dtype)
+{
+    const uint32_t parts = columns_cut(tokens, outs, dtype).parts;
+    return parts > 1 ? (size_t)parts * pitch_of(outs) * sizeof(float) : 0;
+}
 
 void launch_linear_backward(const Values& dy, size_t tokens, size_t outs, uint32_t dtype, uint32_t act, const Values& before, const Result& dz, float* dbias, bool accumulate,
                             void* workspace, hipStream_t st)
@@ -509,13 +533,13 @@ void launch_linear_backward(const Values& dy, size_t tokens, size_t outs, uint32
         return;
     }
     const Cut cut = columns_cut(tokens, outs, dtype);
-    float* parts = dbias != nullptr ? static_cast<float*>(workspace) : nullptr;
+    const RowParts s = parts_of(tokens, outs, cut, 0.0f, workspace, dbias, nullptr, accumulate);
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (act == OGQ_IDENTITY) launch_columns<T, Columns::kSums>(dy, before, tokens, outs, cut, parts, nullptr, nullptr, act, dz, st);
-        else launch_columns<T, Columns::kActivation>(dy, before, tokens, outs, cut, parts, nullptr, nullptr, act, dz, st);
+        if (act == OGQ_IDENTITY) launch_columns<T, Columns::kSums>(dy, before, s, cut, nullptr, nullptr, act, dz, st);
+        else launch_columns<T, Columns::kActivation>(dy, before, s, cut, nullptr, nullptr, act, dz, st);
     });
-    if (parts != nullptr) launch_add_vectors(parts, cut.parts, outs, pitch_of(outs), dbias, nullptr, accumulate, st);
+    if (s.parts != nullptr) launch_add_vectors(s.parts, cut.parts, outs, s.pitch, dbias, nullptr, accumulate, st);
 }
 
 }  // namespace ogq
