@@ -291,7 +291,8 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
     constexpr int kBytes = kStages * kStage > 4 * kTurn<NO> ? kStages * kStage : 4 * kTurn<NO>;
     __shared__ __align__(16) char lds[kBytes];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tiles = s.tiles_out * s.tiles_token, tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
+    const uint32_t tiles = s.tiles_out * s.tiles_token, tile = this_block() % tiles, part = this_block() / tiles;
+    if (part >= s.parts) return;  // (behind the last tile, in the last row of a large grid)
     const uint32_t out = tile % s.tiles_out * OUT, token = tile / s.tiles_out * TOKENS, out_wave = (wave & 1) * (OUT / 2), token_wave = (wave >> 1) * (TOKENS / 2);
     const uint32_t first = part * s.part, last = min(s.cols, first + s.part);
     FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, last, threadIdx.x, lds);
@@ -782,7 +783,7 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
                 }
                 kernel = transposed ? large_linear_kernel<T, true> : large_linear_kernel<T, false>;
             }
-        launch_kernel(kernel, dim3(s.tiles_out * s.tiles_token * s.parts), dim3(256), st, from, w, s, e);
+        launch_kernel(kernel, grid_of((uint64_t)s.tiles_out * s.tiles_token * s.parts), dim3(256), st, from, w, s, e);
         if (s.sums != nullptr) launch_join_parts(s, e, st);
     });
 }

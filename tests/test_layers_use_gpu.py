@@ -1,0 +1,258 @@
+"""libogq_layers on the GPU as programs use it: a whole training step of all operators together, captured graphs, other streams, autograd's versions, tensors whose offsets pass 32 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2002_11082_amd as ogq
+from tests import layers_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+GROUP = ogq.make_group_params(32, 8)
+
+
+class Model:
+    """Tokens through a table, blocks of norm, two linear layers and what goes around them, a norm, and the table's shape again for logits; parameters are views of one flat fp32 tensor."""
+
+    def __init__(self, vocab, width, hidden, blocks, seed):
+        self.vocab, self.width, self.hidden, self.blocks = vocab, width, hidden, blocks
+        self.shapes = {"table": (vocab, width), "head": (vocab, width), "norm_w": (width,), "norm_b": (width,)}
+        for n in range(blocks):
+            self.shapes.update({f"{n}.norm_w": (width,), f"{n}.norm_b": (width,), f"{n}.up": (hidden, width), f"{n}.up_b": (hidden,), f"{n}.down": (width, hidden), f"{n}.down_b": (width,)})
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.flat = torch.empty(sum(math.prod(s) for s in self.shapes.values()), device=DEV)
+        for name, w in self.views(self.flat).items():
+            if name.endswith("norm_w"):
+                w.copy_(1.0 + 0.1 * torch.randn(w.shape, generator=gen, device=DEV))
+            else:
+                w.copy_(torch.randn(w.shape, generator=gen, device=DEV) * (0.1 if w.dim() == 1 else 1.0 / math.sqrt(w.shape[1])))
+
+    def views(self, flat):
+        parts = flat.split([math.prod(s) for s in self.shapes.values()])
+        return {name: part.view(shape) for (name, shape), part in zip(self.shapes.items(), parts)}
+
+
+def step(model, flat, gradient, tokens, places, values, dtype):
+    """One step's loss, its parameters' gradients into `gradient` (which is added to): the package's operators alone."""
+    p, g = model.views(flat), model.views(gradient)
+    held = {name: w.to(dtype) for name, w in p.items() if w.dim() == 2}
+    rows = tokens.numel()
+    x = ogq.ogq_embedding_forward(tokens, held["table"], 2.0)
+    kept = []
+    for n in range(model.blocks):
+        y, mean, rstd = ogq.ogq_layer_norm_forward(x, p[f"{n}.norm_w"], p[f"{n}.norm_b"])
+        h, before = ogq.ogq_linear(y, held[f"{n}.up"], p[f"{n}.up_b"], ogq.GELU, keep=True)
+        out = ogq.ogq_linear(h, held[f"{n}.down"], p[f"{n}.down_b"], None, x)
+        kept.append((x, mean, rstd, ogq.ogq_group_quantize(y, GROUP), before, ogq.ogq_group_quantize(h, GROUP)))
+        x = out
+    y, mean, rstd = ogq.ogq_layer_norm_forward(x, p["norm_w"], p["norm_b"])
+    y_held = ogq.ogq_group_quantize(y, GROUP)
+    logits = ogq.ogq_linear(y, held["head"])
+    weight = torch.full((rows,), 1.0 / rows, device=DEV)
+    loss, dlogits = ogq.ogq_distill_gradient(logits, places, values, 1.5, weight, dlogits=logits)
+    ogq.ogq_weight_gradient(dlogits, *y_held, model.width, GROUP, g["head"], accumulate=True)
+    dx, _, _ = ogq.ogq_layer_norm_backward(ogq.ogq_linear(dlogits, held["head"], transposed=True), x, mean, rstd, p["norm_w"], dweight=g["norm_w"], dbias=g["norm_b"], accumulate=True)
+    for n in reversed(range(model.blocks)):
+        x, mean, rstd, y_held, before, h_held = kept[n]
+        ogq.ogq_linear_backward(dx, dbias=g[f"{n}.down_b"], accumulate=True)
+        ogq.ogq_weight_gradient(dx, *h_held, model.hidden, GROUP, g[f"{n}.down"], accumulate=True)
+        dh = ogq.ogq_linear(dx, held[f"{n}.down"], transposed=True)
+        dz, _ = ogq.ogq_linear_backward(dh, ogq.GELU, before, dz=dh, dbias=g[f"{n}.up_b"], accumulate=True)
+        ogq.ogq_weight_gradient(dz, *y_held, model.width, GROUP, g[f"{n}.up"], accumulate=True)
+        back, _, _ = ogq.ogq_layer_norm_backward(ogq.ogq_linear(dz, held[f"{n}.up"], transposed=True), x, mean, rstd, p[f"{n}.norm_w"], dweight=g[f"{n}.norm_w"],
+                                                 dbias=g[f"{n}.norm_b"], accumulate=True)
+        dx = dx + back
+    ogq.ogq_embedding_gradient(tokens, dx, model.vocab, 2.0, dtable=g["table"], accumulate=True)
+    return loss.sum()
+
+
+def exact_loss(model, flat, tokens, places, values, seen=None):
+    """The same in 64 bits, for autograd.  seen: what goes into each product with weights that has a gradient, and what comes out."""
+    p = model.views(flat)
+
+    def product(x, name):
+        z = x @ p[name].t()
+        if seen is not None:
+            z.retain_grad()
+            seen[name] = (x.detach(), z)
+        return z
+
+    def norm(x, w, b):
+        return torch.nn.functional.layer_norm(x, (model.width,), p[w], p[b], 1e-5)
+
+    x = p["table"][tokens] * 2.0
+    for n in range(model.blocks):
+        z = product(norm(x, f"{n}.norm_w", f"{n}.norm_b"), f"{n}.up") + p[f"{n}.up_b"]
+        x = x + product(0.5 * z * torch.erfc(-z / math.sqrt(2.0)), f"{n}.down") + p[f"{n}.down_b"]
+    log_q = torch.log_softmax(product(norm(x, "norm_w", "norm_b"), "head") / 1.5, 1)
+    log_p = torch.log_softmax(values.double() / 1.5, 1)
+    return 1.5 ** 2 / tokens.numel() * (log_p.exp() * (log_p - log_q.gather(1, places))).sum()
+
+
+def batch(model, rows, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    tokens = torch.randint(0, model.vocab, (rows,), generator=gen, device=DEV)
+    places = torch.stack([torch.randperm(model.vocab, generator=gen, device=DEV)[:8] for _ in range(rows)])
+    return tokens, places, 2.0 * torch.randn(rows, 8, generator=gen, device=DEV)
+
+
+def test_gradients_of_a_whole_model():
+    """In fp32 all roundings but those of the 8-bit checkpoints are below 1e-5: parameters whose gradients do not go through them agree that far with autograd's in 64 bits.  A checkpoint's step is less than a
+    63.5th of the group's largest value m (the next smaller power of two would not hold 127 steps), and a value is off by at most half of it, m / 127: a weight gradient by at most the sum over
+    the rows of |dz| m / 127."""
+    model = Model(211, 96, 160, 2, 1)
+    tokens, places, values = batch(model, 50, 2)
+    gradient = torch.zeros_like(model.flat)
+    loss = float(step(model, model.flat, gradient, tokens, places, values, torch.float32))
+    flat, seen = model.flat.double().requires_grad_(), {}
+    exact = exact_loss(model, flat, tokens, places, values, seen)
+    exact.backward()
+    assert abs(loss - float(exact.detach())) < 1e-5 * abs(float(exact.detach()))
+    want = model.views(flat.grad)
+    for name, g in model.views(gradient).items():
+        off, size = (g.double() - want[name]).abs(), float(want[name].norm())
+        if name in seen:
+            x, z = seen[name]
+            largest = x.abs().view(x.shape[0], -1, 32).amax(2, keepdim=True).expand(-1, -1, 32).reshape(x.shape)
+            assert bool((off <= z.grad.abs().t() @ largest / 127 + 1e-5 * size).all()), name
+        else:
+            assert float(off.norm()) < 1e-5 * size, (name, float(off.norm()) / size)
+    # against differences: the exact loss along the gradient that the operators made
+    direction = gradient.double() / gradient.double().norm()
+    e = 1e-5
+    with torch.no_grad():
+        slope = (exact_loss(model, flat + e * direction, tokens, places, values) - exact_loss(model, flat - e * direction, tokens, places, values)) / (2 * e)
+    assert abs(float(slope) - float((gradient.double() * direction).sum())) < 1e-4 * abs(float(slope))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_captured_step_of_a_whole_model(dtype):
+    """The step in a graph, replayed with other tokens, with eager steps between the replays, is the eager step; two graphs do not share a workspace."""
+    model = Model(300, 64, 96, 1, 3)
+    static = [t.clone() for t in batch(model, 37, 4)]
+    gradients = [torch.zeros_like(model.flat) for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step(model, model.flat, gradients[0], *static, dtype)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, losses = [], []
+    for n in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            gradients[n].zero_()
+            losses.append(step(model, model.flat, gradients[n], *static, dtype))
+        graphs.append(graph)
+    for n in range(6):
+        for to, new in zip(static, batch(model, 37, 10 + n)):
+            to.copy_(new)
+        graphs[n % 2].replay()
+        eager = torch.zeros_like(model.flat)
+        loss = step(model, model.flat, eager, *static, dtype)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, gradients[n % 2]) and torch.equal(loss, losses[n % 2]), n
+
+
+def test_streams():
+    """Work goes to the current stream: on another one, behind a long run of its own, results are those of the default stream."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(300, 512, generator=gen, device=DEV).bfloat16()
+    w = torch.randn(512, 512, generator=gen, device=DEV).bfloat16()
+    tokens = torch.randint(0, 90, (300,), generator=gen, device=DEV)
+
+    def all_of(x):
+        y, mean, rstd = ogq.ogq_layer_norm_forward(x)
+        z = ogq.ogq_linear(y, w, None, ogq.SILU)
+        t = ogq.ogq_embedding_gradient(tokens, z, 90)
+        return y, z, t, ogq.ogq_distill_gradient(z, tokens.view(300, 1) % 512, z[:, :1].float().contiguous())[1]
+
+    want = all_of(x + 1)
+    side = torch.cuda.Stream()
+    late = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(50):
+            late.add_(0.0)
+        late.copy_(x + 1)
+        got = all_of(late)
+    side.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_outputs_of_the_caller_get_a_new_version():
+    x = torch.randn(6, 64, device=DEV)
+    leaf = torch.randn(6, 64, device=DEV, requires_grad=True)
+    for write in (lambda t: ogq.ogq_layer_norm_forward(x, y=t), lambda t: ogq.ogq_linear(x, torch.randn(64, 64, device=DEV), y=t), lambda t: ogq.ogq_linear_backward(x, ogq.RELU, x, dz=t),
+                  lambda t: ogq.ogq_embedding_forward(torch.arange(6, device=DEV), x, y=t), lambda t: ogq.ogq_embedding_gradient(torch.arange(6, device=DEV), x, 6, dtable=t),
+                  lambda t: ogq.ogq_distill_gradient(x, torch.zeros(6, 1, dtype=torch.int64, device=DEV), x[:, :1].contiguous(), dlogits=t)):
+        kept = torch.randn(6, 64, device=DEV)
+        product = (leaf * kept).sum()
+        write(kept)
+        with pytest.raises(RuntimeError):
+            product.backward()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of more than 2^32 bytes in all, and more than 2^32 values: their first and last ones are those of a small tensor."""
+    rows, cols = (1 << 21) + 3, 2064
+    print("[layers] large tensors", flush=True)
+    small = torch.randn(64, cols, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    x = small.repeat(rows // 64 + 1, 1)[:rows]
+    assert x.numel() > 1 << 32
+    order = torch.arange(rows, device=DEV) % 64
+    ends = torch.cat([torch.arange(300, device=DEV), torch.arange(rows - 300, rows, device=DEV)])
+    weight, bias = torch.randn(cols, device=DEV), torch.randn(cols, device=DEV)
+    y, mean, rstd = ogq.ogq_layer_norm_forward(x, weight, bias)
+    want = ogq.ogq_layer_norm_forward(small, weight, bias)
+    assert torch.equal(y[ends], want[0][order[ends]]) and torch.equal(mean, want[1][order])
+    dx = ogq.ogq_layer_norm_backward(x, x, mean, rstd, weight, dx=y)[0]
+    assert torch.equal(dx[ends], ogq.ogq_layer_norm_backward(small, small, want[1], want[2], weight)[0][order[ends]])
+    # rows of a large table, and their gradients
+    tokens = torch.tensor([rows - 1, 5, rows - 1, 0, rows - 64], device=DEV)
+    assert torch.equal(ogq.ogq_embedding_forward(tokens, x), x[tokens])
+    del y, dx
+    # as tokens of a linear layer with few outputs; and as logits
+    w = torch.randn(24, cols, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    z = ogq.ogq_linear(x, w, None, ogq.RELU)
+    exact, bound = ref.linear(small, w, None, "relu", None, False)[0]
+    ref.close(z[ends], exact[order[ends]], ref.rounded(bound, exact, torch.bfloat16)[order[ends]], "z")
+    places = (order % cols).view(rows, 1).int()
+    loss, d = ogq.ogq_distill_gradient(x, places, torch.ones(rows, 1, device=DEV), dlogits=x)
+    want, wd = ogq.ogq_distill_gradient(small, places[:64].contiguous(), torch.ones(64, 1, device=DEV), row_weight=torch.ones(64, device=DEV))
+    assert torch.equal(d[ends], wd[order[ends]]) and torch.equal(loss[ends], want[order[ends]])
+
+
+def test_a_table_gradient_beyond_32_bits():
+    vocab, cols = (1 << 20) + 7, 4112
+    print("[layers] large table", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    tokens = torch.cat([torch.tensor([vocab - 1, 0, vocab - 1], device=DEV), torch.randint(vocab - 50, vocab, (2000,), generator=gen, device=DEV)])
+    dy = torch.randint(-3, 4, (tokens.numel(), cols), generator=gen, device=DEV).bfloat16()
+    got = ogq.ogq_embedding_gradient(tokens, dy, vocab)
+    exact = torch.zeros(51, cols, device=DEV).index_add_(0, torch.where(tokens == 0, 50, tokens - (vocab - 50)), dy.float())
+    assert torch.equal(got[-50:], exact[:50]) and torch.equal(got[0], exact[50])
+    for at in range(1, vocab - 50, 1 << 18):
+        assert not bool(got[at:min(at + (1 << 18), vocab - 50)].any())
+
+
+def test_strides_of_inputs():
+    """Inputs whose rows are the same, or lie 2^25 values apart."""
+    x = torch.randn(1, 600, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).half()
+    w = torch.randn(700, 600, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).half()
+    for tokens in (5, 90, 2000):
+        y = ogq.ogq_linear(x.expand(tokens, 600), w)
+        far = torch.empty(1 << 25, dtype=torch.half, device=DEV).as_strided((2, 600), (1 << 24, 1))
+        far.copy_(x.expand(2, 600))
+        assert torch.equal(y, y[:1].expand(tokens, 700))
+        assert torch.equal(ogq.ogq_linear(x.expand(tokens, 600), w[:1].expand(700, 600)), y[:, :1].expand(tokens, 700))
+        assert torch.equal(ogq.ogq_linear(far, w), ogq.ogq_linear(x.expand(2, 600), w))
+    # a large product whose rows are too far apart for 32 bits of a tile's bytes
+    wide = torch.empty(400 * (1 << 23) + 640, dtype=torch.half, device=DEV)
+    w = torch.randint(-3, 4, (40000, 640), device=DEV).half()
+    x = torch.randint(-3, 4, (300, 640), device=DEV).half()
+    far = wide.as_strided((300, 640), (1 << 23, 1))
+    far.copy_(x)
+    assert torch.equal(ogq.ogq_linear(far, w), ogq.ogq_linear(x, w))
