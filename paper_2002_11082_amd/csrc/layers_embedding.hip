@@ -199,7 +199,7 @@ struct Piece {
 };
 
 struct Table {
-    uint32_t number, cols, blocks, pitch, window;  // blocks: of 64 pieces, along a row; window: keys of one
+    uint32_t number, cols, blocks, pitch, window;  // blocks: of 64 pieces, along a row; window: keys of one (or rows of the table)
     uint64_t dy_stride, dtable_stride;
     float scale;
 };
@@ -308,6 +308,68 @@ __global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* ke
     piece.template store<ACCUMULATE>(dtable + (uint64_t)token * s.dtable_stride, s.scale, sum);
 }
 
+// Up to kFew tokens in one launch: a wavefront has up to 16 rows of the table's gradient (s.window), 64 pieces of each, and all of the tokens, four to a lane.  Rows that none of them names are zeros; the others
+// take the rows of their tokens in their order, eight at a time.
+constexpr uint32_t kFew = 256;
+template <class T, bool ACCUMULATE>
+__global__ __launch_bounds__(kBlock) void few_tokens_gradient_kernel(const void* tokens, bool wide, uint32_t vocab, const T* dy, Table s, float* dtable)
+{
+    constexpr int N = kPiece<T>, kAhead = 8;
+    const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = unit / s.blocks;
+    const uint64_t first = group * s.window;
+    if (first >= vocab) return;
+    const uint32_t lane = threadIdx.x & 63, rows = (uint32_t)min((uint64_t)s.window, vocab - first);
+    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * N, s.cols);
+    uint32_t row[kFew / 64];  // of this wavefront's that a token names, kNone for others
+    uint32_t named = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kFew / 64; ++k) {
+        const uint32_t at = k * 64 + lane, token = at < s.number ? token_of(tokens, wide, at, vocab) : kNone;
+        row[k] = token != kNone && token - (uint32_t)first < rows && token >= first ? token - (uint32_t)first : kNone;
+        named |= __builtin_amdgcn_ballot_w64(row[k] != kNone) != 0 ? 1u : 0u;
+    }
+    float* out = dtable + first * s.dtable_stride;
+    if (named == 0) {
+        if (ACCUMULATE) return;
+        const float zero[N] = {};
+        for (uint32_t r = 0; r < rows; ++r) piece.template store<false>(out + r * s.dtable_stride, 0.0f, zero);
+        return;
+    }
+    for (uint32_t r = 0; r < rows; ++r) {
+        float sum[N] = {};
+        bool any = false;
+#pragma unroll 1
+        for (uint32_t k = 0; k < kFew / 64; ++k) {
+            uint32_t mine = kNone;
+#pragma unroll
+            for (uint32_t i = 0; i < kFew / 64; ++i)
+                if (i == k) mine = row[i];
+            uint64_t which = __builtin_amdgcn_ballot_w64(mine == r);
+            while (which != 0) {
+                any = true;
+                const uint32_t count = __builtin_popcountll(which);
+                uint4 v[kAhead];
+#pragma unroll
+                for (uint32_t n = 0; n < kAhead; ++n) {  // (behind the last one it is loaded again, and not used)
+                    v[n] = piece.load(dy + (uint64_t)(k * 64 + __builtin_ctzll(which)) * s.dy_stride);
+                    if (n + 1 < count) which &= which - 1;
+                }
+                if (count <= kAhead) which = 0;
+#pragma unroll
+                for (uint32_t n = 0; n < kAhead; ++n) {
+                    float a[N];
+                    values_of<T>(v[n], a);
+                    if (n < count) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) sum[i] += a[i];
+                    }
+                }
+            }
+        }
+        if (any || !ACCUMULATE) piece.template store<ACCUMULATE>(out + r * s.dtable_stride, s.scale, sum);
+    }
+}
+
 // The gradient of no tokens.
 __global__ __launch_bounds__(kRun) void fill_kernel(Fill fill)
 {
@@ -324,7 +386,8 @@ size_t pitch_of(size_t cols) { return (cols + 7) / 8 * 8; }
 
 Space space_of(size_t number, size_t cols)
 {
-    Space s;
+    Space s{};
+    if (number <= kFew) return s;
     s.keys = ceil_div(number, kRun) * kRun * sizeof(uint64_t);
     // Keys of a window: few where there are few wavefronts, since a wavefront has eight rows under way at a time; many otherwise, since each window may leave two sums that are written and read
     // once more.
@@ -368,6 +431,19 @@ void launch_embedding_gradient(const Integers& tokens, size_t number, const Valu
     const Fill fill = fill_of(dtable, vocab, cols);
     if (number == 0) {
         launch_kernel(fill_kernel, grid_of(fill.last), dim3(kRun), st, fill);
+        return;
+    }
+    if (number <= kFew) {
+        with_type(dtype, [&](auto* t) {
+            using T = std::remove_pointer_t<decltype(t)>;
+            const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
+            // rows of a wavefront: many only where there are many, since it takes the rows of its tokens one behind the other
+            const uint64_t all = (uint64_t)vocab * blocks;
+            const uint32_t rows = all >= 65536 ? 16 : all >= 16384 ? 4 : 1;
+            const Table s{(uint32_t)number, (uint32_t)cols, blocks, 0, rows, dy.stride, dtable.stride, scale};
+            launch_kernel(accumulate ? few_tokens_gradient_kernel<T, true> : few_tokens_gradient_kernel<T, false>, grid_of(ceil_div(ceil_div(vocab, rows) * blocks, 4)), dim3(kBlock),
+                          st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)vocab, static_cast<const T*>(dy.data), s, out);
+        });
         return;
     }
     const Space space = space_of(number, cols);

@@ -282,21 +282,25 @@ __device__ __forceinline__ void mend_sums(const float* x, const float* weight, c
 
 // Tiles of OUT outputs by TOKENS tokens, a quarter in each of four wavefronts.  In 16 bits two stages of LDS and one barrier a step: while one step is multiplied the next one waits in registers,
 // goes to LDS behind the products, and the one behind it sets off.  fp32, whose three pieces fill LDS, has one stage and two barriers, and more workgroups to a CU.
-template <class T, int OUT, int TOKENS, bool TRANSPOSED>
-__global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
+// Where there are too few tiles for the chip, two teams of four wavefronts take a tile's steps in turn and add what they have in LDS.
+template <class T, int OUT, int TOKENS, bool TRANSPOSED, int TEAMS = 1>
+__global__ __launch_bounds__(256 * TEAMS) void linear_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
 {
     using FeedW = std::conditional_t<TRANSPOSED, Across<T, OUT, false>, Along<T, OUT, false>>;
     using FeedX = Along<T, TOKENS, false>;
     constexpr int kBytesW = kPlanes<T> * FeedW::kPlane, kStage = kBytesW + kPlanes<T> * FeedX::kPlane, NO = OUT / 64, NT = TOKENS / 64, kStages = sizeof(T) == 2 ? 2 : 1, D = kDepth<T>;
     constexpr int kBytes = kStages * kStage > 4 * kTurn<NO> ? kStages * kStage : 4 * kTurn<NO>;
-    __shared__ __align__(16) char lds[kBytes];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(TEAMS == 1 || (TEAMS == 2 && kStages == 2 && kBytes >= 1024 * NO * NT * 16));
+    __shared__ __align__(16) char all_lds[TEAMS * kBytes];
+    const uint32_t lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all_waves & 3, team = TEAMS == 1 ? 0 : all_waves >> 2;
+    const uint32_t thread = TEAMS == 1 ? threadIdx.x : threadIdx.x & 255;
+    char* lds = all_lds + team * kBytes;
     const uint32_t tiles = s.tiles_out * s.tiles_token, tile = this_block() % tiles, part = this_block() / tiles;
     if (part >= s.parts) return;  // (behind the last tile, in the last row of a large grid)
     const uint32_t out = tile % s.tiles_out * OUT, token = tile / s.tiles_out * TOKENS, out_wave = (wave & 1) * (OUT / 2), token_wave = (wave >> 1) * (TOKENS / 2);
     const uint32_t first = part * s.part, last = min(s.cols, first + s.part);
-    FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, last, threadIdx.x, lds);
-    FeedX feed_x(x, s.x_stride, token, s.tokens, s.cols, last, threadIdx.x, lds + kBytesW);
+    FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, last, thread, lds);
+    FeedX feed_x(x, s.x_stride, token, s.tokens, s.cols, last, thread, lds + kBytesW);
     f32x16 sum[NO][NT] = {};
     const uint32_t whole = first + (first < last ? feed_w.readable(first) : 0) * kDepth<T>;  // the first column of a step that asks
     const auto fetch = [&](uint32_t k) __attribute__((always_inline)) {
@@ -342,17 +346,19 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    fetch(first);
+    const uint32_t begin = first + team * D;
+    fetch(begin);
     if constexpr (kStages == 2) {
-        if (first < last) bring(0);
-        fetch(first + kDepth<T>);
+        if (begin < last) bring(0);
+        fetch(begin + TEAMS * D);
         uint32_t stage = 0;
-        for (uint32_t k = first; k < last; k += kDepth<T>) {
+        // (the teams meet at the same barriers: the last step may be one team's alone)
+        for (uint32_t k = begin; k < last + team * D; k += TEAMS * D) {
             __syncthreads();
-            products(stage);
+            if (TEAMS == 1 || k < last) products(stage);
             stage ^= 1;
-            if (k + kDepth<T> < last) bring(stage);
-            fetch(k + 2 * kDepth<T>);
+            if (k + TEAMS * D < last) bring(stage);
+            fetch(k + 2 * TEAMS * D);
         }
     } else {
         for (uint32_t k = first; k < last; k += kDepth<T>) {
@@ -365,6 +371,31 @@ __global__ __launch_bounds__(256) void linear_kernel(const T* x, const T* weight
     }
     __syncthreads();
     if constexpr (sizeof(T) == 4) mend_sums<TRANSPOSED>(x, weight, s, out + out_wave, token + token_wave, first, last, lane, sum);
+    if constexpr (TEAMS == 2) {
+        // the second team's sums, 16 bytes of a lane at a time
+        f32x4* const exchange = reinterpret_cast<f32x4*>(all_lds + kBytes) + wave * (NO * NT * 256) + lane;
+#pragma unroll
+        for (int a = 0; a < NO; ++a)
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    f32x4& place = exchange[((a * NT + b) * 4 + m) * 64];
+                    if (team == 1) place = f32x4{sum[a][b][4 * m], sum[a][b][4 * m + 1], sum[a][b][4 * m + 2], sum[a][b][4 * m + 3]};
+                }
+        __syncthreads();
+        if (team == 1) return;
+#pragma unroll
+        for (int a = 0; a < NO; ++a)
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const f32x4 v = exchange[((a * NT + b) * 4 + m) * 64];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[a][b][4 * m + i] += v[i];
+                }
+    }
     finish_tile<T>(sum, out + out_wave, token + token_wave, lane, s, part, e, lds + wave * kTurn<NO>);
 }
 
@@ -677,11 +708,12 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(LinearShape s, Epilo
 }
 
 struct Plan {
-    uint32_t tile_out, tile_token, tiles_out, tiles_token, part, parts;
+    uint32_t tile_out, tile_token, tiles_out, tiles_token, part, parts, teams;
 };
 
 // Which tiles, and into how many parts a sum is cut: what takes least by this account, in us.  With c workgroups on a CU a step (64 columns in 16 bits, 32 in fp32) takes a + b c, of which
-// a CU holds up to `most`; parts cost a launch of 3.5 us, 0.3 us each, and 8 bytes for each of their sums, written and read, at 4 TB/s.
+// a CU holds up to `most`; parts cost a launch of 3.5 us, 0.3 us each, and 8 bytes for each of their sums, written and read, at 4 TB/s.  Where there is up
+// to one workgroup to a CU, the tiles of 64 tokens have two teams in 16 bits, and a step takes 0.7 of the time (64 x 4096 to 16384 27.6 us without, 24.3 with; 128 x 128 are no faster with them: 1733 x 1216 to 1249 19.7 without, 20.5 with).
 //   16 bits: 64 x 64 0.28 + 0.17 c, 128 x 64 0.27 + 0.26 c, 128 x 128 0.52 + 0.26 c, 256 x 256 (no parts) 1.6 and 10 a tile;  fp32: 128 x 64 0.5 + 0.63 c, 128 x 128 1.0 + 0.8 c.
 // Measured for x [tokens, cols] to outs (fp16; by tile and parts): 1000 x 1000 to 1000: 64 x 64 9.0 in one part, 14.8 in two, 128 x 128 16.9; 128 x 4096 to 4096: 64 x 64 29.3 in one, 16.5 in 4, 18.7 in 8,
 // 128 x 128 50.7 in one, 19.4 in 6; 256 x 25088 to 4096: 128 x 128 148 in 2, 74.9 in 8, 92.4 in 12, 64 x 64 98.8 in 2; 2000 x 2048 to 2048: 64 x 64 33.5, 128 x 64 28.3, 128 x 128 30.4, in two parts 36.8; 4096
@@ -704,18 +736,19 @@ Plan plan_of(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool near)
     if (!fp32 && near && cols >= 512 && tokens > 128 && outs > 128) {
         const uint64_t tiles = ceil_div(outs, 256) * ceil_div(tokens, 256);
         least = (double)ceil_div(tiles, 256) * ((double)steps * 1.6 + 10.0);
-        p = {256, 256, (uint32_t)ceil_div(outs, 256), (uint32_t)ceil_div(tokens, 256), (uint32_t)cols, 1};
+        p = {256, 256, (uint32_t)ceil_div(outs, 256), (uint32_t)ceil_div(tokens, 256), (uint32_t)cols, 1, 1};
     }
     for (uint32_t n = 0; n < kinds; ++n) {
         const Tile& t = fp32 ? kFull[n] : kHalf[n];
         const uint64_t tiles = ceil_div(outs, t.out) * ceil_div(tokens, t.token);
         for (uint64_t parts = 1; parts <= 32 && (parts == 1 || (parts <= steps / 2 && tiles * parts <= 1024)); ++parts) {
             const uint64_t each = ceil_div(steps, parts), slots = 256 * t.most, full = tiles * parts / slots, rest = tiles * parts % slots;
-            const double step = (double)full * (t.a + t.b * (double)t.most) + (rest != 0 ? t.a + t.b * (double)ceil_div(rest, 256) : 0.0);
+            const bool teams = !fp32 && t.token == 64 && tiles * parts <= 256 && each >= 4;
+            const double step = ((double)full * (t.a + t.b * (double)t.most) + (rest != 0 ? t.a + t.b * (double)ceil_div(rest, 256) : 0.0)) * (teams ? 0.7 : 1.0);
             const double join = parts > 1 ? 3.5 + 0.3 * (double)parts + 2e-6 * (double)parts * (double)tokens * (double)outs : 0.0, cost = step * (double)each + join;
             if (cost >= least) continue;
             least = cost;
-            p = {t.out, t.token, (uint32_t)ceil_div(outs, t.out), (uint32_t)ceil_div(tokens, t.token), steps == 0 ? depth : (uint32_t)(each * depth), 1};
+            p = {t.out, t.token, (uint32_t)ceil_div(outs, t.out), (uint32_t)ceil_div(tokens, t.token), steps == 0 ? depth : (uint32_t)(each * depth), 1, teams ? 2u : 1u};
             p.parts = steps == 0 ? 1 : (uint32_t)ceil_div(cols, p.part);
         }
     }
@@ -783,7 +816,13 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
                 }
                 kernel = transposed ? large_linear_kernel<T, true> : large_linear_kernel<T, false>;
             }
-        launch_kernel(kernel, grid_of((uint64_t)s.tiles_out * s.tiles_token * s.parts), dim3(256), st, from, w, s, e);
+        if constexpr (sizeof(T) == 2) {
+            if (plan.teams == 2) {
+                kernel = transposed ? linear_kernel<T, 128, 64, true, 2> : linear_kernel<T, 128, 64, false, 2>;
+                if (plan.tile_out == 64) kernel = transposed ? linear_kernel<T, 64, 64, true, 2> : linear_kernel<T, 64, 64, false, 2>;
+            }
+        }
+        launch_kernel(kernel, grid_of((uint64_t)s.tiles_out * s.tiles_token * s.parts), dim3(256 * plan.teams), st, from, w, s, e);
         if (s.sums != nullptr) launch_join_parts(s, e, st);
     });
 }

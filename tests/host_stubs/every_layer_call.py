@@ -40,7 +40,7 @@ def main():
                 call(f"sums {at}", 1, 2, lib.ogq_linear_backward, A, cols, rows, cols, dtype, 4, None, 0, None, 0, A, 0, A, BIG, None)
                 call(f"embedding {at}", 1, 1, lib.ogq_embedding_forward, A, 0, rows, A, cols, 1000, cols, dtype, 1.0, A, cols, None)
                 for accumulate in (0, 1):
-                    call(f"embedding gradient {at}", 2, 5, lib.ogq_embedding_gradient, A, 1, rows, A, cols, 1000, cols, dtype, 1.0, accumulate, A, cols, A, BIG, None)
+                    call(f"embedding gradient {at}", 1 if rows <= 256 else 2, 1 if rows <= 256 else 5, lib.ogq_embedding_gradient, A, 1, rows, A, cols, 1000, cols, dtype, 1.0, accumulate, A, cols, A, BIG, None)
                 call(f"distill {at}", 1, 2, lib.ogq_distill_loss, A, cols, rows, cols, dtype, A, 0, A, 10, 1.0, None, A, A, BIG, None)
                 call(f"distill gradient {at}", 1, 2, lib.ogq_distill_gradient, A, cols, rows, cols, dtype, A, 0, A, 10, 1.0, None, A, A, cols, A, BIG, None)
         for tokens in (1, 2, 3, 4, 5, 6, 7, 8, 9, 16, 33, 64, 65, 100, 300, 1000, 5000, 20000):

@@ -34,6 +34,7 @@ def main():
             call(f"linear backward {at}", 1, lib.ogq_linear_backward, A, cols, rows, cols, dtype, 1, A, cols, A, cols, A, 1, A, BIG, None)
             call(f"embedding {at}", rows, lib.ogq_embedding_forward, A, 0, rows, A, cols, 100, cols, dtype, 1.0, A, cols, None)
             call(f"embedding gradient {at}", 64, lib.ogq_embedding_gradient, A, 1, 100, A, cols, rows, cols, dtype, 1.0, 0, A, cols, A, BIG, None)
+            call(f"embedding gradient, sorted, {at}", 64, lib.ogq_embedding_gradient, A, 1, 300, A, cols, rows, cols, dtype, 1.0, 0, A, cols, A, BIG, None)
             call(f"embedding of nothing {at}", rows * cols // 16, lib.ogq_embedding_gradient, None, 1, 0, None, cols, rows, cols, dtype, 1.0, 0, A, cols, None, 0, None)
             call(f"distill {at}", rows * 256, lib.ogq_distill_gradient, A, cols, rows, cols, dtype, A, 0, A, 10, 1.0, None, A, A, cols, A, BIG, None)
         for number, cols in (((1 << 30) - 1, 1), ((1 << 30) - 1, 800), (1 << 29, 1900)):

@@ -88,11 +88,11 @@ def test_refusals_of_embedding(lib):
     assert forward(integer=2) == -30 and forward(dtype=3) == -22 and forward(scale=INF) == -31 and forward(stride=7) == -24 and forward(number=1 << 31) == -9
     assert forward(number=0, tokens=0) == 0 and forward(cols=0) == 0
 
-    def gradient(tokens=A, integer=0, number=4, dy=A, vocab=10, cols=8, dtype=0, scale=1.0, accumulate=0, out=A, stride=8, space=A, size=1 << 20):
+    def gradient(tokens=A, integer=0, number=400, dy=A, vocab=10, cols=8, dtype=0, scale=1.0, accumulate=0, out=A, stride=8, space=A, size=1 << 20):
         return lib.ogq_embedding_gradient(tokens, integer, number, dy, 8, vocab, cols, dtype, scale, accumulate, out, stride, space, size, None)
 
-    need = ogq.ogq_embedding_gradient_workspace(4, 10, 8)
-    assert need > 0 and ogq.ogq_embedding_gradient_workspace(1 << 30, 10, 1) == 0
+    need = ogq.ogq_embedding_gradient_workspace(400, 10, 8)
+    assert need > 0 and ogq.ogq_embedding_gradient_workspace(1 << 30, 10, 1) == 0 and ogq.ogq_embedding_gradient_workspace(200, 10, 8) == 0
     assert gradient(tokens=0) == -1 and gradient(dy=0) == -1 and gradient(out=0) == -1 and gradient(space=None) == -1 and gradient(size=need - 1) == -25 and gradient(space=A + 8) == -6
     assert gradient(integer=2) == -30 and gradient(dtype=3) == -22 and gradient(scale=float("nan")) == -31 and gradient(stride=7) == -24 and gradient(number=1 << 30) == -9
     assert gradient(vocab=0) == 0 and gradient(number=0, accumulate=1, tokens=0, dy=0, space=None, size=0) == 0

@@ -227,7 +227,7 @@ def test_linear_backward(tokens, outs, pad, dtype):
 # ----------------------------------------------------------------------------------------------------------- embedding
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("ids", [torch.int32, torch.int64])
-@pytest.mark.parametrize("number,vocab,cols,pad", [(1, 1, 1, 0), (5, 3, 7, 2), (64, 10, 8, 0), (127, 2, 33, 0), (128, 1, 100, 1), (200, 1000, 333, 0), (1024, 50, 64, 0), (1025, 7, 520, 3),
+@pytest.mark.parametrize("number,vocab,cols,pad", [(1, 1, 1, 0), (5, 3, 7, 2), (64, 10, 8, 0), (127, 2, 33, 0), (128, 1, 100, 1), (200, 1000, 333, 0), (256, 5, 40, 0), (256, 1, 1030, 1), (257, 5, 40, 0), (1024, 50, 64, 0), (1025, 7, 520, 3),
                                                    (3000, 5000, 40, 0), (5000, 3, 24, 0), (40000, 300, 12, 0)])
 def test_embedding(number, vocab, cols, pad, ids, dtype):
     print("[layers] embedding", number, vocab, cols, pad, ids, dtype, flush=True)
@@ -245,7 +245,7 @@ def test_embedding(number, vocab, cols, pad, ids, dtype):
     assert torch.equal(more, got + 4.0) and (wide[:, 0] == 4).all() and (wide[:, 1 + cols:] == 4).all()
 
 
-@pytest.mark.parametrize("number", [100, 2000, 70000])
+@pytest.mark.parametrize("number", [100, 256, 2000, 70000])
 def test_embedding_gradient_of_whole_numbers_is_exact(number):
     """Few tokens that are frequent, many that are not, some that name no row; int64 beyond 32 bits."""
     gen = torch.Generator(device=DEV).manual_seed(3)
