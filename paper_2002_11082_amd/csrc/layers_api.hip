@@ -84,7 +84,7 @@ int check_linear(size_t tokens, size_t outs, size_t cols, uint32_t dtype)
 {
     const int rc = first_of({check_dtype(dtype), check_size(tokens, cols), check_size(tokens, outs), check_size(outs, cols), check_size(cols, outs)});
     if (rc != OGQ_OK) return rc;
-    // workgroups of 256 threads in one dimension, one to a tile: 2^32 threads are too many for a launch
+    // tiles, and parts of their sums, are counted in 32 bits
     return (tokens + 127) / 128 * ((outs + 127) / 128) < ((size_t)1 << 24) ? OGQ_OK : OGQ_ERR_SIZE;
 }
 

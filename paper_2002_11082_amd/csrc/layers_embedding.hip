@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kBlock) void few_tokens_gradient_kernel(const void*
                 }
             }
         }
-        if (any || !ACCUMULATE) piece.template store<ACCUMULATE>(out + r * s.dtable_stride, s.scale, sum);
+        if (any || !ACCUMULATE) piece.template store<ACCUMULATE>(out + r * s.dtable_stride, any ? s.scale : 0.0f, sum);
     }
 }
 

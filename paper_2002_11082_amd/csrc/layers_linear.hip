@@ -422,7 +422,8 @@ __global__ __launch_bounds__(256, 1) void large_linear_kernel(const T* x, const 
     static_assert(kX == 8 && (kW == 8 || kW == 4) && 2 * kStage >= 4 * kTurn<4>);
     __shared__ __align__(256) char lds[2 * kStage];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint2 tile = tile_of(blockIdx.x, s.tiles_out, s.tiles_token);
+    if (this_block() >= s.tiles_out * s.tiles_token) return;  // (in the last row of a large grid)
+    const uint2 tile = tile_of(this_block(), s.tiles_out, s.tiles_token);
     const uint32_t out = tile.x * 256, token = tile.y * 256, out_wave = (wave & 1) * 128, token_wave = (wave >> 1) * 128;
     FeedW feed_w(weight, s.weight_stride, out, s.outs, s.cols, s.cols, threadIdx.x, lds);
     FeedX feed_x(x, s.x_stride, token, s.tokens, s.cols, s.cols, threadIdx.x, lds + FeedW::kPlane);

@@ -238,6 +238,24 @@ def test_a_table_gradient_beyond_32_bits():
         assert not bool(got[at:min(at + (1 << 18), vocab - 50)].any())
 
 
+@pytest.mark.parametrize("cols", (521, 576))
+def test_more_tiles_than_a_row_of_workgroups(cols):
+    """More than 2^20 tiles of 256 x 256, of rows that begin anywhere and of aligned ones: small whole numbers, so that sums are exact and each tile is a copy of the first ones."""
+    torch.cuda.empty_cache()
+    tokens, outs = (1 << 18) + 512, 1 << 18
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("less than 160 GiB of memory free")
+    print("[layers] many tiles", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    small, w = (torch.randint(-3, 4, (512, cols), generator=gen, device=DEV).bfloat16() for _ in range(2))
+    y = ogq.ogq_linear(small.repeat(tokens // 512, 1), w.repeat(outs // 512, 1))
+    want = (small.double() @ w.double().T).bfloat16().repeat(1, outs // 512)
+    for at in range(0, tokens, 512):
+        assert torch.equal(y[at:at + 512], want), at
+    del y
+    torch.cuda.empty_cache()
+
+
 def test_strides_of_inputs():
     """Inputs whose rows are the same, or lie 2^25 values apart."""
     x = torch.randn(1, 600, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).half()
