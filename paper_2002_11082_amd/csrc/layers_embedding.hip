@@ -308,65 +308,77 @@ __global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* ke
     piece.template store<ACCUMULATE>(dtable + (uint64_t)token * s.dtable_stride, s.scale, sum);
 }
 
-// Up to kFew tokens in one launch: a wavefront has up to 16 rows of the table's gradient (s.window), 64 pieces of each, and all of the tokens, four to a lane.  Rows that none of them names are zeros; the others
-// take the rows of their tokens in their order, eight at a time.
+// Up to kFew tokens in one launch: a workgroup has s.window rows of the table's gradient, 64 pieces of each; all of its wavefronts look at all of the tokens, four to a lane, and each adds the rows of
+// its own 64 of them, in their order, 8 under way together.  Rows that only one wavefront's tokens name are stored by it, those of several are added in LDS, in the wavefronts' order; others are zeros.
 constexpr uint32_t kFew = 256;
 template <class T, bool ACCUMULATE>
 __global__ __launch_bounds__(kBlock) void few_tokens_gradient_kernel(const void* tokens, bool wide, uint32_t vocab, const T* dy, Table s, float* dtable)
 {
-    constexpr int N = kPiece<T>, kAhead = 8;
-    const uint64_t unit = (uint64_t)this_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = unit / s.blocks;
-    const uint64_t first = group * s.window;
+    constexpr int N = kPiece<T>, kAhead = 8, kWaves = kFew / 64;
+    __shared__ float shared[2][kWaves][N][64];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t first = (uint64_t)(this_block() / s.blocks) * s.window;
     if (first >= vocab) return;
-    const uint32_t lane = threadIdx.x & 63, rows = (uint32_t)min((uint64_t)s.window, vocab - first);
-    const Piece<T> piece((uint32_t)(unit % s.blocks * 64 + lane) * N, s.cols);
-    uint32_t row[kFew / 64];  // of this wavefront's that a token names, kNone for others
-    uint32_t named = 0;
+    const uint32_t rows = (uint32_t)min((uint64_t)s.window, vocab - first);
+    const Piece<T> piece((this_block() % s.blocks * 64 + lane) * N, s.cols);
+    uint32_t row[kWaves];  // of this workgroup's that a token names, kNone for others
 #pragma unroll
-    for (uint32_t k = 0; k < kFew / 64; ++k) {
+    for (int k = 0; k < kWaves; ++k) {
         const uint32_t at = k * 64 + lane, token = at < s.number ? token_of(tokens, wide, at, vocab) : kNone;
-        row[k] = token != kNone && token - (uint32_t)first < rows && token >= first ? token - (uint32_t)first : kNone;
-        named |= __builtin_amdgcn_ballot_w64(row[k] != kNone) != 0 ? 1u : 0u;
+        row[k] = token != kNone && token >= first && token - (uint32_t)first < rows ? token - (uint32_t)first : kNone;
     }
     float* out = dtable + first * s.dtable_stride;
-    if (named == 0) {
-        if (ACCUMULATE) return;
-        const float zero[N] = {};
-        for (uint32_t r = 0; r < rows; ++r) piece.template store<false>(out + r * s.dtable_stride, 0.0f, zero);
-        return;
-    }
-    for (uint32_t r = 0; r < rows; ++r) {
+    uint32_t side = 0;
+    for (uint32_t r = 0; r < rows; ++r, out += s.dtable_stride) {
+        uint32_t having = 0;  // the wavefronts whose tokens name this row
+        uint64_t which = 0;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const uint64_t all = __builtin_amdgcn_ballot_w64(row[k] == r);
+            having |= all != 0 ? 1u << k : 0u;
+            which = k == wave ? all : which;
+        }
         float sum[N] = {};
-        bool any = false;
-#pragma unroll 1
-        for (uint32_t k = 0; k < kFew / 64; ++k) {
-            uint32_t mine = kNone;
+        if (having == 0) {
+            if (!ACCUMULATE && r % kWaves == wave) piece.template store<false>(out, 0.0f, sum);
+            continue;
+        }
+        while (which != 0) {
+            const uint32_t count = __builtin_popcountll(which);
+            uint4 v[kAhead];
 #pragma unroll
-            for (uint32_t i = 0; i < kFew / 64; ++i)
-                if (i == k) mine = row[i];
-            uint64_t which = __builtin_amdgcn_ballot_w64(mine == r);
-            while (which != 0) {
-                any = true;
-                const uint32_t count = __builtin_popcountll(which);
-                uint4 v[kAhead];
+            for (uint32_t n = 0; n < kAhead; ++n) {  // (behind the last one it is loaded again, and not used)
+                v[n] = piece.load(dy + (uint64_t)(wave * 64 + __builtin_ctzll(which)) * s.dy_stride);
+                if (n + 1 < count) which &= which - 1;
+            }
+            if (count <= kAhead) which = 0;
 #pragma unroll
-                for (uint32_t n = 0; n < kAhead; ++n) {  // (behind the last one it is loaded again, and not used)
-                    v[n] = piece.load(dy + (uint64_t)(k * 64 + __builtin_ctzll(which)) * s.dy_stride);
-                    if (n + 1 < count) which &= which - 1;
-                }
-                if (count <= kAhead) which = 0;
+            for (uint32_t n = 0; n < kAhead; ++n) {
+                float a[N];
+                values_of<T>(v[n], a);
+                if (n < count) {
 #pragma unroll
-                for (uint32_t n = 0; n < kAhead; ++n) {
-                    float a[N];
-                    values_of<T>(v[n], a);
-                    if (n < count) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) sum[i] += a[i];
-                    }
+                    for (int i = 0; i < N; ++i) sum[i] += a[i];
                 }
             }
         }
-        if (any || !ACCUMULATE) piece.template store<ACCUMULATE>(out + r * s.dtable_stride, any ? s.scale : 0.0f, sum);
+        if ((having & (having - 1)) == 0) {
+            if (having >> wave & 1) piece.template store<ACCUMULATE>(out, s.scale, sum);
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) shared[side][wave][i][lane] = sum[i];
+        __syncthreads();
+        if (wave == r % kWaves) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                sum[i] = shared[side][0][i][lane];
+#pragma unroll
+                for (int k = 1; k < kWaves; ++k) sum[i] += shared[side][k][i][lane];
+            }
+            piece.template store<ACCUMULATE>(out, s.scale, sum);
+        }
+        side ^= 1;  // (a side is written again behind the next barrier, which its reader reaches when it has read)
     }
 }
 
@@ -437,11 +449,11 @@ void launch_embedding_gradient(const Integers& tokens, size_t number, const Valu
         with_type(dtype, [&](auto* t) {
             using T = std::remove_pointer_t<decltype(t)>;
             const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
-            // rows of a wavefront: many only where there are many, since it takes the rows of its tokens one behind the other
+            // rows of a workgroup: many only where there are many, since a wavefront takes the rows of its tokens one behind the other
             const uint64_t all = (uint64_t)vocab * blocks;
-            const uint32_t rows = all >= 65536 ? 16 : all >= 16384 ? 4 : 1;
+            const uint32_t rows = all >= 65536 ? 32 : all >= 16384 ? 16 : 4;
             const Table s{(uint32_t)number, (uint32_t)cols, blocks, 0, rows, dy.stride, dtable.stride, scale};
-            launch_kernel(accumulate ? few_tokens_gradient_kernel<T, true> : few_tokens_gradient_kernel<T, false>, grid_of(ceil_div(ceil_div(vocab, rows) * blocks, 4)), dim3(kBlock),
+            launch_kernel(accumulate ? few_tokens_gradient_kernel<T, true> : few_tokens_gradient_kernel<T, false>, grid_of(ceil_div(vocab, rows) * blocks), dim3(kBlock),
                           st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)vocab, static_cast<const T*>(dy.data), s, out);
         });
         return;

@@ -258,6 +258,21 @@ def test_embedding_gradient_of_whole_numbers_is_exact(number):
     assert torch.equal(ogq.ogq_embedding_gradient(tokens, dy, 900).double(), exact)
 
 
+@pytest.mark.parametrize("vocab,cols", [(20001, 72), (70003, 40), (9000, 1030)])
+@pytest.mark.parametrize("number", [1, 64, 65, 256])
+def test_embedding_gradient_of_few_tokens_in_a_large_table(number, vocab, cols):
+    """One token that stands everywhere but at three places, at the table's end; equal tokens far apart."""
+    for dtype in (torch.float32, torch.bfloat16):
+        tokens = torch.full((number,), vocab - 1, device=DEV)
+        tokens[number // 2], tokens[number // 3], tokens[-1] = 0, vocab // 2, vocab // 2
+        dy = whole(number, cols, dtype, 5)
+        exact = torch.zeros(vocab, cols, dtype=torch.float64, device=DEV).index_add_(0, tokens, dy.double())
+        got = ogq.ogq_embedding_gradient(tokens, dy, vocab)
+        assert torch.equal(got.double(), exact)
+        ogq.ogq_embedding_gradient(tokens.int(), dy, vocab, -2.0, dtable=got, accumulate=True)
+        assert torch.equal(got.double(), -exact)
+
+
 def test_embedding_over_nothing():
     table = values(5, 6, torch.float32, 1)
     none = torch.empty(0, dtype=torch.int64, device=DEV)
