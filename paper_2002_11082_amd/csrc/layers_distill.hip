@@ -277,13 +277,14 @@ auto kernel_of(int pieces)
     }
 }
 
-// Several workgroups to a row, of 256 threads with four pieces each, where rows of four such slices or more leave CUs without work: a second launch and reading the row again cost less than what one
-// CU takes for the row's exponentials.  1: none.
+// Several workgroups to a row, of 256 threads with four pieces each, where rows of eight such slices or more leave CUs without work: a second launch and reading the row again cost less than what one
+// CU takes for the row's exponentials.  fp16, a gradient of one workgroup to a row and of several: 16 rows x 32768 8.3 us and 9.2, 16 x 65536 12.1 and 9.0, 64 x 65536 12.9 and 11.4, 64 x 131072 21.6 and
+// 15.3, 128 x 131072 25.8 and 25.3, 192 x 131072 28.2 and 36.6.  1: none.
 constexpr uint32_t kSliceThreads = 256, kSlicePieces = 4;
 uint32_t slices_of(size_t rows, size_t cols, uint32_t dtype)
 {
     const uint64_t slices = ceil_div(cols, (uint64_t)kSliceThreads * kSlicePieces * (dtype == OGQ_FP32 ? 4 : 8));
-    return rows <= 128 && slices >= 4 ? (uint32_t)slices : 1;
+    return rows <= 96 && slices >= 8 ? (uint32_t)slices : 1;
 }
 
 }  // namespace

@@ -11,7 +11,7 @@ namespace {
 
 constexpr uint32_t kRun = 1024;   // keys that a workgroup sorts
 constexpr uint32_t kWays = 32;    // sorted runs that a launch makes one of
-constexpr uint32_t kLeast = 8, kMost = 64;  // neighbouring keys whose rows a wavefront adds, a window: a power of two
+constexpr uint32_t kLeast = 8, kMost = 32;  // neighbouring keys whose rows a wavefront adds, a window: a power of two
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // Token n, or kNone where it names no row.
@@ -402,9 +402,10 @@ Space space_of(size_t number, size_t cols)
     if (number <= kFew) return s;
     s.keys = ceil_div(number, kRun) * kRun * sizeof(uint64_t);
     // Keys of a window: few where there are few wavefronts, since a wavefront has eight rows under way at a time; many otherwise, since each window may leave two sums that are written and read
-    // once more.
+    // once more.  bf16, all launches, windows of 8, 16, 32, 64 keys: 300 tokens x 512 16.4, 19.2, 24.6, 36.4 us; 4096 x 1024 34.5, 38.4, 46.9, 64.9; 32768 x 1024 67.4, 59.7, 58.8, 68.7;
+    // 16384 x 4096 192.5, 185.8, 180.8, 193.0.
     s.window = kLeast;
-    while (s.window < kMost && number * cols / s.window > (size_t)8192 * 512) s.window *= 2;
+    while (s.window < kMost && number * cols / s.window > (size_t)2048 * 512) s.window *= 2;
     s.sums = number > s.window ? 2 * ceil_div(number, s.window) * pitch_of(cols) * sizeof(float) : 0;
     s.bytes = (number > kRun ? 2 : 1) * s.keys + s.sums;
     return s;
@@ -449,9 +450,10 @@ void launch_embedding_gradient(const Integers& tokens, size_t number, const Valu
         with_type(dtype, [&](auto* t) {
             using T = std::remove_pointer_t<decltype(t)>;
             const uint32_t blocks = (uint32_t)ceil_div(cols, 64 * kPiece<T>);
-            // rows of a workgroup: many only where there are many, since a wavefront takes the rows of its tokens one behind the other
+            // Rows of a workgroup: many only where there are many, since a wavefront takes the rows of its tokens one behind the other.  256 tokens, bf16, 1, 4, 16, 32 rows: 1000 x 512 4.3, 5.3, 9.5,
+            // 13.2 us (sorted 15.9); 32768 x 1024 69.0, 32.0, 26.3, 32.6 (25.6).
             const uint64_t all = (uint64_t)vocab * blocks;
-            const uint32_t rows = all >= 65536 ? 32 : all >= 16384 ? 16 : 4;
+            const uint32_t rows = all >= 16384 ? 16 : all >= 4096 ? 4 : 1;
             const Table s{(uint32_t)number, (uint32_t)cols, blocks, 0, rows, dy.stride, dtable.stride, scale};
             launch_kernel(accumulate ? few_tokens_gradient_kernel<T, true> : few_tokens_gradient_kernel<T, false>, grid_of(ceil_div(vocab, rows) * blocks), dim3(kBlock),
                           st, tokens.data, tokens.type == OGQ_INT64, (uint32_t)vocab, static_cast<const T*>(dy.data), s, out);

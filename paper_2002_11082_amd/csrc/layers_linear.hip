@@ -773,7 +773,7 @@ template void launch_join_parts<_Float16>(const LinearShape&, const Epilogue<_Fl
 
 size_t linear_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed)
 {
-    const uint32_t parts = tokens <= kFewTokens ? few_plan(tokens, outs, cols, dtype, transposed).parts : plan_of(tokens, outs, cols, dtype, true).parts;
+    const uint32_t parts = few_tokens(tokens, outs, cols, dtype, transposed) ? few_plan(tokens, outs, cols, dtype, transposed).parts : plan_of(tokens, outs, cols, dtype, true).parts;
     return parts > 1 ? (size_t)parts * tokens * pitch_of(outs) * sizeof(float) : 0;
 }
 
@@ -787,7 +787,7 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
         const Epilogue<T> e{bias,          static_cast<const T*>(residual.data), static_cast<T*>(y.data), static_cast<T*>(before.data), residual.stride, y.stride,
                             before.stride, s.outs,                               act};
         const auto from = static_cast<const T*>(x.data), w = static_cast<const T*>(weight.data);
-        if (tokens <= kFewTokens) {
+        if (few_tokens(tokens, outs, cols, dtype, transposed)) {
             const FewPlan plan = few_plan(tokens, outs, cols, dtype, transposed);
             s.tiles_out = (uint32_t)ceil_div(outs, 64 * kPiece<T>), s.part = plan.part, s.parts = plan.parts;
             s.sums = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
