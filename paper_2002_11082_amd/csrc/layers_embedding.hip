@@ -1,8 +1,9 @@
 // libogq_layers: rows of a table by tokens, and the table's gradient.
 //
 // The gradient's rows are sums over equal tokens.  The tokens are sorted with their positions first, so that a sum has its rows one behind the other, in their order, whatever the
-// order in which workgroups come: keys of 64 bits, the token above the position, no two of them alike.  A wavefront then adds the rows of 64 neighbouring keys, so that a frequent token
-// is as much work as many rare ones.  Bound by memory: the table's gradient is written once, most of it zeros, behind which the sorting hides.
+// order in which workgroups come: keys of 64 bits, the token above the position, no two of them alike.  A wavefront then adds the rows of a window of neighbouring keys, so that a frequent token
+// is as much work as many rare ones.  Bound by memory: the table's gradient is written once, most of it zeros, behind which the sorting hides; rows that tokens name twice.  16384 tokens of
+// 32768 x 4096 bf16: the rows 40 us, sorting and zeros 33 + 46 (537 MB, 6.8 TB/s), the windows' sums 70 to 80, those of several windows 13.
 #include "layers_common.h"
 
 namespace ogq {
@@ -21,7 +22,7 @@ __device__ __forceinline__ uint32_t token_of(const void* tokens, bool wide, uint
     return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : kNone;
 }
 
-// 2^log2 threads to a row, which take its pieces in turn.  Bound by memory.
+// 2^log2 threads to a row, which take its pieces in turn.  Bound by memory: 16384 rows of 4096 bf16 40 us, 134 MB written at 3.4 TB/s while 84 MB of rows are gathered.
 template <class T>
 __global__ __launch_bounds__(kBlock) void embedding_kernel(const void* tokens, bool wide, uint32_t number, const T* table, uint64_t table_stride, uint32_t vocab, uint32_t cols,
                                                          uint32_t threads_log2, float scale, T* y, uint64_t y_stride)
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(kRun) void sort_runs_kernel(const void* tokens, boo
 }
 
 // Runs of `run` sorted keys into runs of kWays times as many: a key's place is its own and what the other runs have below it.  Eight lanes to a key, each of which searches four runs, side by
-// side: first among every 128th part of a run, which is in LDS, then in memory.  `total` is a multiple of kRun.  The workgroups behind those that the keys need fill.
+// side: first among 128 samples of each run, which are in LDS, then in memory: in runs of 1024 three loads that wait for one another, in place of ten.  `total` is a multiple of kRun.  The workgroups behind those that the keys need fill.
 constexpr uint32_t kKeys = kRun / 8;  // of a workgroup
 __global__ __launch_bounds__(kRun) void merge_runs_kernel(const uint64_t* from, uint64_t* to, uint32_t total, uint32_t run, uint32_t run_log2, Fill fill)
 {
@@ -309,7 +310,8 @@ __global__ __launch_bounds__(kBlock) void join_windows_kernel(const uint64_t* ke
 }
 
 // Up to kFew tokens in one launch: a workgroup has s.window rows of the table's gradient, 64 pieces of each; all of its wavefronts look at all of the tokens, four to a lane, and each adds the rows of
-// its own 64 of them, in their order, 8 under way together.  Rows that only one wavefront's tokens name are stored by it, those of several are added in LDS, in the wavefronts' order; others are zeros.
+// its own 64 of them, in their order, 8 under way together.  Rows that only one wavefront's tokens name are stored by it, those of several are added in LDS, in the wavefronts' order; others are zeros.  Bound by latency: 256 tokens in
+// a table of 1000 x 512 bf16 4.3 us (sorted 15.9); 256 x 4096 of one token 16 us.
 constexpr uint32_t kFew = 256;
 template <class T, bool ACCUMULATE>
 __global__ __launch_bounds__(kBlock) void few_tokens_gradient_kernel(const void* tokens, bool wide, uint32_t vocab, const T* dy, Table s, float* dtable)

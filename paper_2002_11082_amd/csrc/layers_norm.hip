@@ -17,7 +17,7 @@ __device__ __forceinline__ uint64_t first_row()
 }
 
 // P pieces of a row to each of THREADS threads.  `off`, the differences from the mean as it came out of fp32 sums, are summed too: what is left of the mean's rounding is taken off
-// again, so that an offset of the whole row costs nothing but the rounding of x.
+// again, so that an offset of the whole row costs nothing but the rounding of x.  Bound by memory: 8192 x 4096 bf16 24.6 us, 5.5 TB/s read and written; one row of 4096 2.8 us, latency.
 template <class T, int THREADS, int P>
 __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_forward_kernel(const T* x, uint64_t x_stride, uint32_t rows, uint32_t cols, const float* weight, const float* bias,
                                                                              float eps, float per_col, T* y, uint64_t y_stride, float* mean, float* rstd)
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_forward_kernel(c
     }
 }
 
-// Rows of any length, read three times, by a workgroup each.
+// Rows of any length, read three times (twice from the caches), by a workgroup each.
 template <class T>
 __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* x, uint64_t x_stride, uint32_t rows, uint32_t cols, const float* weight, const float* bias, float eps,
                                                                      float per_col, T* y, uint64_t y_stride, float* mean, float* rstd)
@@ -134,7 +134,7 @@ __device__ __forceinline__ void store_only(float* to, bool accumulate, const flo
 }
 
 // The backward pass of rows that THREADS threads hold, P pieces each.  A row's values set off while the one before is worked on.  64 threads to a row: the four wavefronts of a workgroup
-// take its rows in turn, and add their sums over the rows in LDS in the end.
+// take its rows in turn, and add their sums over the rows in LDS in the end.  Bound by memory: 8192 x 4096 bf16 41 us, 5.3 TB/s with the parts' sums; 1237 x 1001 fp32 5.6 us, latency.
 template <class T, int THREADS, int P>
 __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, const float* weight,
                                                                               const float* mean, const float* rstd, T* dx, uint64_t dx_stride)
@@ -285,6 +285,7 @@ enum class Columns { kNorm, kActivation, kSums };
 //   kNorm        dy * u and dy, of rows that no workgroup holds whole
 //   kActivation  dz = dy * act'(z), stored, and the sums of dz (s.parts may be null)
 //   kSums        the sums of dy
+// Bound by memory: kActivation (gelu by tanh) of 4096 x 4096 bf16 27 us with what the caches hold, 3.7 TB/s.
 template <class T, Columns WHAT>
 __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, uint32_t blocks, const float* mean,
                                                        const float* rstd, uint32_t act, T* dz, uint64_t dz_stride)
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
     }
 }
 
-// The parts' sums: 32 neighbouring columns (a line) to a workgroup, eight lanes with four columns each, and 128 threads to them that take the parts in turn, whose sums are then added two by two.
+// The parts' sums: 32 neighbouring columns (a line) to a workgroup, eight lanes with four columns each, and 128 threads to them that take the parts in turn, whose sums are then added two by two.  Bound by latency: 512 parts of 4096 columns, two vectors, about 5 us, a launch of which is 2.
 __global__ __launch_bounds__(1024) void add_vectors_kernel(const float* parts, uint32_t number, uint32_t cols, uint32_t pitch, uint32_t vectors, uint32_t blocks, float* first,
                                                          float* second, bool accumulate)
 {
