@@ -107,6 +107,8 @@ def test_layer_norm_over_nothing():
 # -------------------------------------------------------------------------------------------------------------- linear
 LINEARS = [(1, 1, 1), (1, 5, 3), (2, 8, 16), (3, 100, 33), (4, 300, 600), (5, 17, 1000), (6, 2100, 130), (7, 64, 2050), (8, 513, 777), (1, 9000, 40), (9, 1, 1), (9, 130, 65), (16, 128, 64),
            (33, 200, 31), (64, 129, 127), (65, 128, 128), (100, 300, 257), (129, 127, 320), (200, 1000, 96), (300, 40, 3000), (12, 16, 5000)]
+# few tokens: a wavefront's four rows of weights, a workgroup's, and what goes to the matrix cores
+LINEARS += [(tokens, 8197, 70) for tokens in range(1, 9)] + [(tokens, 2051, 300) for tokens in range(1, 9)] + [(tokens, 8197, 2056) for tokens in (1, 4, 5)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -300,7 +302,7 @@ def teacher(rows, cols, top, seed, ids=torch.int64):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,top,pad", [(1, 1, 1, 0), (3, 5, 4, 1), (2, 8, 8, 0), (4, 100, 3, 0), (3, 1000, 1024, 0), (5, 1025, 20, 2), (2, 2048, 1, 0), (3, 4099, 64, 0), (2, 8192, 300, 0),
                                                (2, 8200, 5, 3), (2, 20000, 64, 0), (2, 32769, 100, 1), (2, 65536, 64, 0), (1, 100003, 10, 0), (1, 131072, 64, 0), (1, 140001, 64, 0), (300, 300, 7, 0),
-                                               (128, 33001, 9, 0), (129, 33001, 9, 1), (70, 49153, 200, 3)])
+                                               (128, 33001, 9, 0), (129, 33001, 9, 1), (70, 49153, 200, 3), (97, 70001, 30, 1), (97, 131075, 30, 0)])
 def test_distill(rows, cols, top, pad, dtype):
     print("[layers] distill", rows, cols, top, pad, dtype, flush=True)
     logits = values(rows, cols, dtype, 1, pad, shift=pad % 2, factor=3.0)
@@ -316,8 +318,9 @@ def test_distill(rows, cols, top, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("cols", [6, 700, 9000, 40000, 140000])
-def test_distill_of_rows_that_are_empty_or_bad(cols, dtype):
+@pytest.mark.parametrize("cols,times", [(6, 1), (700, 1), (9000, 1), (40000, 1), (140000, 1), (40000, 9), (70001, 9), (140000, 9)])
+def test_distill_of_rows_that_are_empty_or_bad(cols, times, dtype):
+    """times: the same rows again and again, so many that a row is one workgroup's."""
     rows = 12
     logits = values(rows, cols, dtype, 1)
     places, v = teacher(rows, cols, 5, 2)
@@ -337,14 +340,19 @@ def test_distill_of_rows_that_are_empty_or_bad(cols, dtype):
     logits[11] = -60000.0
     logits[2, 100:] = -math.inf         # all but the row's first logits masked
     (loss, b), (d, bd) = ref.distill(logits, places, v, 1.0, weight)
+    logits, places, v, weight = logits.repeat(times, 1), places.repeat(times, 1), v.repeat(times, 1), weight.repeat(times)
     got, dlogits = ogq.ogq_distill_gradient(logits, places, v, 1.0, weight)
+    assert torch.equal(ogq.ogq_distill_loss(logits, places, v, 1.0, weight).nan_to_num(), got.nan_to_num())
+    for n in range(1, times):
+        assert torch.equal(got[n * rows:(n + 1) * rows].nan_to_num(), got[:rows].nan_to_num())
+        assert torch.equal(dlogits[n * rows:(n + 1) * rows].nan_to_num(), dlogits[:rows].nan_to_num())
+    got, dlogits = got[:rows], dlogits[:rows]
     assert (got[[0, 1, 9]] == 0).all() and (dlogits[[0, 1, 9]] == 0).all()
     for row in (3, 4, 5, 6):
         assert torch.isnan(got[row]) and torch.isnan(dlogits[row]).all(), row
     assert got[8] == math.inf and torch.isfinite(dlogits[8].float()).all() and dlogits[7, 1] == 0
     ref.close(got, loss, ref.rounded(b, loss, torch.float32), "loss")
     ref.close(dlogits, d, ref.rounded(bd, d, dtype), "dlogits")
-    assert torch.equal(ogq.ogq_distill_loss(logits, places, v, 1.0, weight).nan_to_num(), got.nan_to_num())
 
 
 def test_distill_over_nothing():
