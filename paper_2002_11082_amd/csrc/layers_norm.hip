@@ -16,6 +16,36 @@ __device__ __forceinline__ uint64_t first_row()
     return THREADS == 64 ? (uint64_t)this_block() * 4 + (threadIdx.x >> 6) : this_block();
 }
 
+constexpr float kDown = 0x1p-32f, kUp = 0x1p32f, kLargest = 0x1.fffffep127f;
+
+// A row's mean; sum_of(factor) is the sum of its values times a factor.  Where the sum is beyond fp32 though the values are not, it is taken of 2^-32 times the values.
+template <class F>
+__device__ __forceinline__ float mean_of(F sum_of, float per_col)
+{
+    const float m = sum_of(1.0f) * per_col;
+    if (fabsf(m) < INFINITY) return m;  // (NaN where parts of the sum are infinite)
+    const float sum = sum_of(kDown);
+    // (the mean of the largest values may be rounded beyond them)
+    return !(fabsf(sum) < INFINITY) ? sum : fminf(fmaxf(sum * per_col, -kLargest * kDown), kLargest * kDown) * kUp;
+}
+
+// What is left of the mean's rounding, and 1 / deviation, from the sums of the differences from the mean and of their squares; squares_of(factor) is the sum of squares of the differences times a factor, for
+// sums that are beyond fp32 where the variance is not.  rstd is 0 where the variance is beyond fp32, NaN where a value is NaN or infinite.
+struct Spread {
+    float rest, rstd;
+};
+
+template <class F>
+__device__ __forceinline__ Spread spread_of(float2 sums, float per_col, float eps, F squares_of)
+{
+    const float rest = sums.x * per_col;
+    float variance = sums.y * per_col;
+    if (variance == INFINITY) variance = squares_of(kDown) * per_col * kUp * kUp;
+    if (variance == INFINITY) return {fabsf(rest) < INFINITY ? rest : 0.0f, 0.0f};  // (of infinite differences: the sum may be NaN)
+    variance = __builtin_fmaf(-rest, rest, variance);
+    return {rest, 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + eps)};
+}
+
 // P pieces of a row to each of THREADS threads.  `off`, the differences from the mean as it came out of fp32 sums, are summed too: what is left of the mean's rounding is taken off
 // again, so that an offset of the whole row costs nothing but the rounding of x.  Bound by memory: 8192 x 4096 bf16 24.6 us, 5.5 TB/s read and written; one row of 4096 2.8 us, latency.
 template <class T, int THREADS, int P>
@@ -31,14 +61,18 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_forward_kernel(c
     const T* from = x + row * x_stride;
     const auto at = [&](int p) __attribute__((always_inline)) { return piece_at<T, THREADS, P>(p, thread, cols); };
     float v[P][kPiece<T>];
-    float total = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) values_of<T>(load_whole(from + at(p).col), v[p]);
+    const float m = mean_of(
+        [&](float factor) __attribute__((always_inline)) {
+            float total = 0.0f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) total += at(p).counts(i) ? v[p][i] : 0.0f;
-    const float m = sums(total, 0.0f).x * per_col;
+                for (int i = 0; i < kPiece<T>; ++i) total += at(p).counts(i) ? v[p][i] * factor : 0.0f;
+            return sums(total, 0.0f).x;
+        },
+        per_col);
     float off = 0.0f, squares = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -49,10 +83,25 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_forward_kernel(c
             off += d;
             squares = __builtin_fmaf(d, d, squares);
         }
-    const float2 s = sums(off, squares);
-    const float rest = s.x * per_col;
-    const float r = 1.0f / sqrtf(fmaxf(s.y * per_col - rest * rest, 0.0f) + eps);
+    const Spread s = spread_of(sums(off, squares), per_col, eps, [&](float factor) __attribute__((always_inline)) {
+        float squares = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < kPiece<T>; ++i) {
+                const float d = at(p).counts(i) ? v[p][i] * factor : 0.0f;
+                squares = __builtin_fmaf(d, d, squares);
+            }
+        return sums(squares, 0.0f).x;
+    });
+    const float rest = s.rest, r = s.rstd;
     if (thread == 0 && mean != nullptr) mean[row] = m + rest, rstd[row] = r;
+    if (r == 0.0f) {  // (differences may be infinite)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < kPiece<T>; ++i) v[p][i] = rest;
+    }
     T* to = y + row * y_stride;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -76,31 +125,39 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* 
     const uint64_t row = this_block();
     if (row >= rows) return;
     const T* from = x + row * x_stride;
-    float v[kPiece<T>], total = 0.0f;
-    for (uint32_t col = threadIdx.x * kPiece<T>; col < cols; col += 1024 * kPiece<T>) {
-        load_piece<false>(from + col, valid_of<T>(col, cols), v);
-        float t = 0.0f;
+    float v[kPiece<T>];
+    const float m = mean_of(
+        [&](float factor) __attribute__((always_inline)) {
+            float total = 0.0f;
+            for (uint32_t col = threadIdx.x * kPiece<T>; col < cols; col += 1024 * kPiece<T>) {
+                load_piece<false>(from + col, valid_of<T>(col, cols), v);
+                float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) t += v[i];
-        total += t;
-    }
-    const float m = sums(total, 0.0f).x * per_col;
-    float off = 0.0f, squares = 0.0f;
-    for (uint32_t col = threadIdx.x * kPiece<T>; col < cols; col += 1024 * kPiece<T>) {
-        const int valid = valid_of<T>(col, cols);
-        load_piece<false>(from + col, valid, v);
-        float o = 0.0f, q = 0.0f;
+                for (int i = 0; i < kPiece<T>; ++i) t += v[i] * factor;
+                total += t;
+            }
+            return sums(total, 0.0f).x;
+        },
+        per_col);
+    // the sums of the differences and of their squares, these of `factor` times them
+    const auto differences = [&](float factor) __attribute__((always_inline)) {
+        float off = 0.0f, squares = 0.0f;
+        for (uint32_t col = threadIdx.x * kPiece<T>; col < cols; col += 1024 * kPiece<T>) {
+            const int valid = valid_of<T>(col, cols);
+            load_piece<false>(from + col, valid, v);
+            float o = 0.0f, q = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) {
-            const float d = i < valid ? v[i] - m : 0.0f;
-            o += d;
-            q = __builtin_fmaf(d, d, q);
+            for (int i = 0; i < kPiece<T>; ++i) {
+                const float d = i < valid ? v[i] - m : 0.0f;
+                o += d;
+                q = __builtin_fmaf(d * factor, d * factor, q);
+            }
+            off += o, squares += q;
         }
-        off += o, squares += q;
-    }
-    const float2 s = sums(off, squares);
-    const float rest = s.x * per_col;
-    const float r = 1.0f / sqrtf(fmaxf(s.y * per_col - rest * rest, 0.0f) + eps);
+        return sums(off, squares);
+    };
+    const Spread s = spread_of(differences(1.0f), per_col, eps, [&](float factor) { return differences(factor).y; });
+    const float rest = s.rest, r = s.rstd;
     if (threadIdx.x == 0 && mean != nullptr) mean[row] = m + rest, rstd[row] = r;
     T* to = y + row * y_stride;
     for (uint32_t col = threadIdx.x * kPiece<T>; col < cols; col += 1024 * kPiece<T>) {
@@ -110,10 +167,13 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* 
         load_vector<T>(weight == nullptr ? nullptr : weight + col, valid, 1.0f, w);
         load_vector<T>(bias == nullptr ? nullptr : bias + col, valid, 0.0f, b);
 #pragma unroll
-        for (int i = 0; i < kPiece<T>; ++i) v[i] = __builtin_fmaf((v[i] - m - rest) * r, w[i], b[i]);
+        for (int i = 0; i < kPiece<T>; ++i) v[i] = __builtin_fmaf((r == 0.0f ? 0.0f : v[i] - m - rest) * r, w[i], b[i]);  // (differences may be infinite)
         store_piece<false>(to + col, valid, v);
     }
 }
+
+// A row's mean for its backward pass: differences from it, which may be infinite where the variance is beyond fp32, count for nothing there.
+__device__ __forceinline__ float mean_for(float mean, float rstd) { return rstd == 0.0f ? 0.0f : mean; }
 
 // What the kernels that add over the rows have in common: rows first ... last of workgroup n are n * part ..., its sums go to parts[n][2][pitch] (weight, then bias).
 struct RowParts {
@@ -169,7 +229,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
     for (uint32_t row = first + mine; row < last; row += kTurn) {
         if (!kAhead) fetch(row);
         float u[P][N], g[P][N];
-        const float m = next_mean, r = next_rstd;
+        const float r = next_rstd, m = mean_for(next_mean, r);
         float along = 0.0f, plain = 0.0f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -248,7 +308,7 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
     BlockSums<16> sums{space};
     const uint64_t row = this_block();
     if (row >= rows) return;
-    const float m = mean[row], r = rstd[row];
+    const float r = rstd[row], m = mean_for(mean[row], r);
     float u[N], g[N], w[N];
     const auto piece = [&](uint32_t col, int valid) __attribute__((always_inline)) {
         load_piece<false>(x + row * x_stride + col, valid, u);
@@ -310,7 +370,7 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
                 const uint64_t row = min(at + 4 * n, last - 1);
                 g_raw[n] = load_raw(dy + row * dy_stride + col, valid);
                 if constexpr (WHAT != Columns::kSums) x_raw[n] = load_raw(x + row * x_stride + col, valid);
-                if constexpr (WHAT == Columns::kNorm) m[n] = mean[row], r[n] = rstd[row];
+                if constexpr (WHAT == Columns::kNorm) r[n] = rstd[row], m[n] = mean_for(mean[row], r[n]);
             }
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) {

@@ -1,0 +1,79 @@
+"""libogq_layers on the GPU with values from the ends of their types' ranges and far from zero, against the formulas in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2002_11082_amd as ogq
+from tests import layers_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+# a row of one piece and less, of one wavefront's registers, of a workgroup's, and longer ones
+WIDTHS = [3, 8, 100, 3000, 8192, 40000]
+
+
+def randn(*shape, seed):
+    return torch.randn(*shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+
+
+# ---------------------------------------------------------------------------------------------------------------- norm
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_layer_norm_of_variances_beyond_fp32(cols, dtype):
+    """rstd is 0, y the bias and dx 0 where the variance is beyond fp32; other rows are as they are alone."""
+    print("[layers] norm, large variances", cols, dtype, flush=True)
+    x = randn(8, cols, seed=1)
+    x[1] *= 1e28
+    x[2] = (x[2].sign() * 1e28)
+    x[3] *= 1e36
+    x[4] = 3e38
+    x[4, ::4] = -3e38  # (the sum is beyond fp32, and so are differences from the mean)
+    x[5] *= 3e37
+    x = x.to(dtype)
+    large, other = [1, 2, 3, 4, 5], [0, 6, 7]
+    weight, bias, dy = 1.0 + 0.1 * randn(cols, seed=2), randn(cols, seed=3), randn(8, cols, seed=4).to(dtype)
+    y, mean, rstd = ogq.ogq_layer_norm_forward(x, weight, bias)
+    assert (rstd[large] == 0).all() and (y[large] == bias.to(dtype)).all()
+    exact = x.double().mean(1)
+    # a chain of at most 74 roundings, of sums that are at most the values' mean size
+    assert bool(((mean.double() - exact).abs() <= 80 * ref.U * x.double().abs().mean(1)).all())
+    want = ogq.ogq_layer_norm_forward(x[other].contiguous(), weight, bias)
+    for a, b in zip((y, mean, rstd), want):
+        assert torch.equal(a[other], b)
+    dx, dweight, dbias = ogq.ogq_layer_norm_backward(dy, x, mean, rstd, weight)
+    assert (dx[large] == 0).all()
+    alone = ogq.ogq_layer_norm_backward(dy[other].contiguous(), x[other].contiguous(), want[1], want[2], weight)
+    assert torch.equal(dx[other], alone[0])
+    # (the large rows have no part in it; eight numbers are added in another order)
+    assert bool(((dweight - alone[1]).abs() <= 8 * ref.U * (dy[other].double() * (x[other].double() - exact[other, None]) * want[2].double()[:, None]).abs().sum(0)).all())
+    assert torch.isfinite(dbias).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_layer_norm_of_sums_beyond_fp32(cols, dtype):
+    """The variance is within fp32 and the sum of squares is not; the mean is and the sum is not."""
+    x = (randn(5, cols, seed=1) * 2.0 ** 61).to(dtype)
+    x[3] = 3e38
+    x[4] = torch.finfo(dtype).max
+    bias = randn(cols, seed=2)
+    y, mean, rstd = ogq.ogq_layer_norm_forward(x, None, bias)
+    exact, m, r, bound = ref.norm_forward(x[:3], None, bias, 1e-5)
+    ref.close(y[:3], exact, ref.rounded(bound, exact, dtype), "y")
+    ref.close(rstd[:3], r, 50 * ref.U * r, "rstd")
+    ref.close(mean[:3], m, 4 * ref.U * m.abs() + 100 * ref.U / r, "mean")
+    # rows of one value: the mean may be off by a few steps of it, which is what every difference is then, and nothing is left of them but the mean's second rounding
+    assert torch.isfinite(mean).all() and bool(((mean[3:].double() / x[3:, 0].double()) - 1).abs().max() <= 4 * ref.U)
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_layer_norm_of_nan(cols):
+    for bad in (math.nan, math.inf, -math.inf):
+        x = randn(6, cols, seed=1)
+        x[2, cols // 2] = bad
+        y, mean, rstd = ogq.ogq_layer_norm_forward(x)
+        for t in (y, mean, rstd):
+            assert torch.isfinite(t[[0, 1, 3, 4, 5]]).all()
+        assert torch.isnan(y[2]).all() and torch.isnan(rstd[2]) and not torch.isfinite(mean[2])
