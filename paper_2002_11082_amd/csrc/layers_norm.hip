@@ -30,7 +30,7 @@ __device__ __forceinline__ float mean_of(F sum_of, float per_col)
 }
 
 // What is left of the mean's rounding, and 1 / deviation, from the sums of the differences from the mean and of their squares; squares_of(factor) is the sum of squares of the differences times a factor, for
-// sums that are beyond fp32 where the variance is not.  rstd is 0 where the variance is beyond fp32, NaN where a value is NaN or infinite.
+// sums that are beyond fp32 where the variance is not, and for squares that are too small for it.  rstd is 0 where the variance is beyond fp32, NaN where a value is NaN or infinite.
 struct Spread {
     float rest, rstd;
 };
@@ -43,7 +43,13 @@ __device__ __forceinline__ Spread spread_of(float2 sums, float per_col, float ep
     if (variance == INFINITY) variance = squares_of(kDown) * per_col * kUp * kUp;
     if (variance == INFINITY) return {fabsf(rest) < INFINITY ? rest : 0.0f, 0.0f};  // (of infinite differences: the sum may be NaN)
     variance = __builtin_fmaf(-rest, rest, variance);
-    return {rest, 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + eps)};
+    variance = variance < 0.0f ? 0.0f : variance;
+    if (variance + eps < 0x1p-96f) {  // (squares are lost below the least number)
+        constexpr float kFactor = 0x1p80f;
+        const float scaled = __builtin_fmaf(-rest * kFactor, rest * kFactor, squares_of(kFactor) * per_col);
+        return {rest, kFactor / sqrtf((scaled < 0.0f ? 0.0f : scaled) + eps * kFactor * kFactor)};
+    }
+    return {rest, 1.0f / sqrtf(variance + eps)};
 }
 
 // P pieces of a row to each of THREADS threads.  `off`, the differences from the mean as it came out of fp32 sums, are summed too: what is left of the mean's rounding is taken off

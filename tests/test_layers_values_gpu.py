@@ -77,3 +77,24 @@ def test_layer_norm_of_nan(cols):
         for t in (y, mean, rstd):
             assert torch.isfinite(t[[0, 1, 3, 4, 5]]).all()
         assert torch.isnan(y[2]).all() and torch.isnan(rstd[2]) and not torch.isfinite(mean[2])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -133])
+def test_layer_norm_of_variances_below_fp32(eps, cols, dtype):
+    """Values whose squares are below fp32's least number, with an eps that does not hide it."""
+    x = randn(6, cols, seed=1)
+    x[1] *= 2.0 ** -50
+    x[2] *= 2.0 ** -60
+    x[3] *= 2.0 ** -66
+    x[4] *= 2.0 ** -90
+    x[5] *= 2.0 ** -105
+    x = x.to(dtype)
+    y, mean, rstd = ogq.ogq_layer_norm_forward(x, eps=eps)
+    exact, m, r, bound = ref.norm_forward(x, None, None, eps)
+    ref.close(y, exact, ref.rounded(bound, exact, dtype), "y")
+    ref.close(rstd, r, 50 * ref.U * r, "rstd")
+    dy = randn(6, cols, seed=2).to(dtype)
+    (dx, b), _, _ = ref.norm_backward(dy, x, m.float(), r.float(), None)
+    ref.close(ogq.ogq_layer_norm_backward(dy, x, m.float(), r.float()), dx, ref.rounded(b, dx, dtype), "dx")
