@@ -181,6 +181,14 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T* 
 // A row's mean for its backward pass: differences from it, which may be infinite where the variance is beyond fp32, count for nothing there.
 __device__ __forceinline__ float mean_for(float mean, float rstd) { return rstd == 0.0f ? 0.0f : mean; }
 
+// Rows that lie far from zero, measured by their deviation: what the rounding of their mean has left in u is taken off it again, the mean of u.  (Of other rows it is at most 2^-20.)
+__device__ __forceinline__ bool is_far(float mean, float rstd) { return fabsf(mean * rstd) > 16.0f; }
+
+// What a row's gradient takes from the whole row: the mean of u, where the row is far from zero, and with what is left of u the means of g and g * u.
+struct RowMeans {
+    float off, plain, along;
+};
+
 // What the kernels that add over the rows have in common: rows first ... last of workgroup n are n * part ..., its sums go to parts[n][2][pitch] (weight, then bias).
 struct RowParts {
     uint32_t rows, cols, part, pitch;
@@ -236,14 +244,30 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
         if (!kAhead) fetch(row);
         float u[P][N], g[P][N];
         const float r = next_rstd, m = mean_for(next_mean, r);
-        float along = 0.0f, plain = 0.0f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             values_of<T>(next_x[p], u[p]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[p][i] = (u[p][i] - m) * r;
+        }
+        if (is_far(m, r)) {
+            float off = 0.0f;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < N; ++i) off += at(p).counts(i) ? u[p][i] : 0.0f;
+            off = sums(off, 0.0f).x * s.per_col;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < N; ++i) u[p][i] -= off;
+        }
+        float along = 0.0f, plain = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
             values_of<T>(next_dy[p], g[p]);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                u[p][i] = (u[p][i] - m) * r;
                 dw[p][i] = __builtin_fmaf(g[p][i], u[p][i], dw[p][i]);
                 db[p][i] += g[p][i];
                 g[p][i] *= w[p][i];
@@ -304,10 +328,10 @@ __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(
     }
 }
 
-// Rows of any length: the gradient of x by a workgroup for each row, which reads it twice.
+// Rows of any length: the gradient of x by a workgroup for each row, which reads it twice; or, where there are sums over the rows too, only what the gradient takes from the whole row.
 template <class T>
 __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, uint32_t rows, uint32_t cols, float per_col,
-                                                                      const float* weight, const float* mean, const float* rstd, T* dx, uint64_t dx_stride)
+                                                                      const float* weight, const float* mean, const float* rstd, T* dx, uint64_t dx_stride, RowMeans* means)
 {
     constexpr int N = kPiece<T>;
     __shared__ float2 space[2][16];
@@ -315,6 +339,19 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
     const uint64_t row = this_block();
     if (row >= rows) return;
     const float r = rstd[row], m = mean_for(mean[row], r);
+    RowMeans t{};
+    if (is_far(m, r)) {
+        float off = 0.0f, v[N];
+        for (uint32_t col = threadIdx.x * N; col < cols; col += 1024 * N) {
+            const int valid = valid_of<T>(col, cols);
+            load_piece<false>(x + row * x_stride + col, valid, v);
+            float c = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) c += i < valid ? (v[i] - m) * r : 0.0f;
+            off += c;
+        }
+        t.off = sums(off, 0.0f).x * per_col;
+    }
     float u[N], g[N], w[N];
     const auto piece = [&](uint32_t col, int valid) __attribute__((always_inline)) {
         load_piece<false>(x + row * x_stride + col, valid, u);
@@ -322,7 +359,7 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
         load_vector<T>(weight == nullptr ? nullptr : weight + col, valid, 1.0f, w);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            u[i] = i < valid ? (u[i] - m) * r : 0.0f;
+            u[i] = i < valid ? (u[i] - m) * r - t.off : 0.0f;
             g[i] *= w[i];
         }
     };
@@ -334,13 +371,17 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
         for (int i = 0; i < N; ++i) a += g[i], b = __builtin_fmaf(g[i], u[i], b);
         plain += a, along += b;
     }
-    const float2 t = sums(plain, along);
-    const float a = t.x * per_col, b = t.y * per_col;
+    const float2 all = sums(plain, along);
+    t.plain = all.x * per_col, t.along = all.y * per_col;
+    if (means != nullptr) {
+        if (threadIdx.x == 0) means[row] = t;
+        return;
+    }
     for (uint32_t col = threadIdx.x * N; col < cols; col += 1024 * N) {
         const int valid = valid_of<T>(col, cols);
         piece(col, valid);
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = r * (g[i] - __builtin_fmaf(u[i], b, a));
+        for (int i = 0; i < N; ++i) g[i] = r * (g[i] - __builtin_fmaf(u[i], t.along, t.plain));
         store_piece<false>(dx + row * dx_stride + col, valid, g);
     }
 }
@@ -348,13 +389,13 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T*
 enum class Columns { kNorm, kActivation, kSums };
 
 // Sums down the columns: a workgroup has 64 pieces of its columns and `part` rows, which its four wavefronts take in turn, and whose sums they add in LDS.
-//   kNorm        dy * u and dy, of rows that no workgroup holds whole
+//   kNorm        the gradient of x, stored in dz, and the sums of dy * u and dy, of rows that no workgroup holds whole, from the rows' means
 //   kActivation  dz = dy * act'(z), stored, and the sums of dz (s.parts may be null)
 //   kSums        the sums of dy
 // Bound by memory: kActivation (gelu by tanh) of 4096 x 4096 bf16 27 us with what the caches hold, 3.7 TB/s.
 template <class T, Columns WHAT>
-__global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, uint32_t blocks, const float* mean,
-                                                       const float* rstd, uint32_t act, T* dz, uint64_t dz_stride)
+__global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, uint32_t blocks, const float* weight,
+                                                       const float* mean, const float* rstd, const RowMeans* means, uint32_t act, T* dz, uint64_t dz_stride)
 {
     constexpr int N = kPiece<T>, kVectors = WHAT == Columns::kNorm ? 2 : 1, kAhead = 4;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -368,15 +409,18 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[k][i] = 0.0f;
     if (valid != 0) {
+        float w[N];
+        if constexpr (WHAT == Columns::kNorm) load_vector<T>(weight == nullptr ? nullptr : weight + col, valid, 1.0f, w);
         for (uint64_t at = first + wave; at < last; at += 4 * kAhead) {
             uint4 g_raw[kAhead], x_raw[kAhead];
             float m[kAhead], r[kAhead];
+            RowMeans t[kAhead];
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) {
                 const uint64_t row = min(at + 4 * n, last - 1);
                 g_raw[n] = load_raw(dy + row * dy_stride + col, valid);
                 if constexpr (WHAT != Columns::kSums) x_raw[n] = load_raw(x + row * x_stride + col, valid);
-                if constexpr (WHAT == Columns::kNorm) r[n] = rstd[row], m[n] = mean_for(mean[row], r[n]);
+                if constexpr (WHAT == Columns::kNorm) r[n] = rstd[row], m[n] = mean_for(mean[row], r[n]), t[n] = means[row];
             }
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) {
@@ -385,19 +429,23 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
                 float g[N], v[N];
                 values_of<T>(g_raw[n], g);
                 if constexpr (WHAT != Columns::kSums) values_of<T>(x_raw[n], v);
+                if constexpr (WHAT == Columns::kNorm) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const float u = i < valid ? (v[i] - m[n]) * r[n] - t[n].off : 0.0f;
+                        v[i] = r[n] * (g[i] * w[i] - __builtin_fmaf(u, t[n].along, t[n].plain));
+                        sum[0][i] = __builtin_fmaf(g[i], u, sum[0][i]);
+                        sum[1][i] += g[i];
+                    }
+                    store_piece<false>(dz + row * dz_stride + col, valid, v);
+                    continue;
+                }
                 if constexpr (WHAT == Columns::kActivation) {
                     each_of(act, v, [&](int i, float, float slope) { g[i] *= slope; });
                     store_piece<false>(dz + row * dz_stride + col, valid, g);
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    if constexpr (WHAT == Columns::kNorm) {
-                        sum[0][i] = __builtin_fmaf(g[i], i < valid ? (v[i] - m[n]) * r[n] : 0.0f, sum[0][i]);
-                        sum[1][i] += g[i];
-                    } else {
-                        sum[0][i] += g[i];
-                    }
-                }
+                for (int i = 0; i < N; ++i) sum[0][i] += g[i];
             }
         }
     }
@@ -502,11 +550,12 @@ Cut columns_cut(size_t rows, size_t cols, uint32_t dtype)
 }
 
 template <class T, Columns WHAT>
-void launch_columns(const Values& dy, const Values& x, const RowParts& s, const Cut& cut, const float* mean, const float* rstd, uint32_t act, const Result& dz, hipStream_t st)
+void launch_columns(const Values& dy, const Values& x, const RowParts& s, const Cut& cut, const float* weight, const float* mean, const float* rstd, const RowMeans* means, uint32_t act,
+                    const Result& dz, hipStream_t st)
 {
     const uint32_t blocks = (uint32_t)ceil_div(s.cols, 64 * kPiece<T>);
     launch_kernel(columns_kernel<T, WHAT>, grid_of((uint64_t)blocks * cut.parts), dim3(kBlock), st, static_cast<const T*>(dy.data), dy.stride,
-                  static_cast<const T*>(x.data), x.stride, s, blocks, mean, rstd, act, static_cast<T*>(dz.data), dz.stride);
+                  static_cast<const T*>(x.data), x.stride, s, blocks, weight, mean, rstd, means, act, static_cast<T*>(dz.data), dz.stride);
 }
 
 }  // namespace
@@ -542,11 +591,14 @@ void launch_layer_norm_forward(const Values& x, size_t rows, size_t cols, uint32
     });
 }
 
+// The workspace of a norm's sums: the parts' and, behind them, the means of rows that no workgroup holds whole.
+size_t parts_bytes(const Cut& cut, size_t cols) { return cut.parts > 1 ? (size_t)cut.parts * 2 * pitch_of(cols) * sizeof(float) : 0; }
+
 size_t layer_norm_backward_workspace(size_t rows, size_t cols, uint32_t dtype)
 {
     const RowShape shape = shape_of(cols, dtype, 2);
     const Cut cut = shape.threads != 0 ? backward_cut(rows, shape) : columns_cut(rows, cols, dtype);
-    return cut.parts > 1 ? (size_t)cut.parts * 2 * pitch_of(cols) * sizeof(float) : 0;
+    return parts_bytes(cut, cols) + (shape.threads != 0 ? 0 : rows * sizeof(RowMeans));
 }
 
 // The sums of a call's parts: to the workspace, and from there added up, or those of the only part straight to where they belong.
@@ -569,10 +621,10 @@ void launch_layer_norm_backward(const Values& dy, const Values& x, size_t rows, 
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
         if (shape.threads == 0) {
-            // (the sums first: dx may lie where dy is)
-            if (dweight != nullptr) launch_columns<T, Columns::kNorm>(dy, x, s, cut, mean, rstd, 0, {nullptr, 0}, st);
+            RowMeans* means = dweight != nullptr ? reinterpret_cast<RowMeans*>(static_cast<char*>(workspace) + parts_bytes(cut, cols)) : nullptr;
             launch_kernel(layer_norm_backward_long_kernel<T>, grid_of(rows), dim3(1024), st, static_cast<const T*>(dy.data), dy.stride, static_cast<const T*>(x.data),
-                          x.stride, (uint32_t)rows, (uint32_t)cols, per_col, weight, mean, rstd, static_cast<T*>(dx.data), dx.stride);
+                          x.stride, (uint32_t)rows, (uint32_t)cols, per_col, weight, mean, rstd, static_cast<T*>(dx.data), dx.stride, means);
+            if (means != nullptr) launch_columns<T, Columns::kNorm>(dy, x, s, cut, weight, mean, rstd, means, 0, dx, st);
             return;
         }
         const auto pick = [&](auto n) {
@@ -604,8 +656,8 @@ void launch_linear_backward(const Values& dy, size_t tokens, size_t outs, uint32
     const RowParts s = parts_of(tokens, outs, cut, 0.0f, workspace, dbias, nullptr, accumulate);
     with_type(dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (act == OGQ_IDENTITY) launch_columns<T, Columns::kSums>(dy, before, s, cut, nullptr, nullptr, act, dz, st);
-        else launch_columns<T, Columns::kActivation>(dy, before, s, cut, nullptr, nullptr, act, dz, st);
+        if (act == OGQ_IDENTITY) launch_columns<T, Columns::kSums>(dy, before, s, cut, nullptr, nullptr, nullptr, nullptr, act, dz, st);
+        else launch_columns<T, Columns::kActivation>(dy, before, s, cut, nullptr, nullptr, nullptr, nullptr, act, dz, st);
     });
     if (s.parts != nullptr) launch_add_vectors(s.parts, cut.parts, outs, s.pitch, dbias, nullptr, accumulate, st);
 }

@@ -98,3 +98,34 @@ def test_layer_norm_of_variances_below_fp32(eps, cols, dtype):
     dy = randn(6, cols, seed=2).to(dtype)
     (dx, b), _, _ = ref.norm_backward(dy, x, m.float(), r.float(), None)
     ref.close(ogq.ogq_layer_norm_backward(dy, x, m.float(), r.float()), dx, ref.rounded(b, dx, dtype), "dx")
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_layer_norm_backward_far_from_zero(kind, cols):
+    """Gradients are those of the exact mean, though the one that the forward pass leaves is rounded: a mean of 10^6 by up to 2^-5, a part of the deviation of 1."""
+    if kind == "fp32":
+        x = randn(40, cols, seed=1) + 1.0e6
+    else:  # rows of 1000, in which one value is the next one
+        x = torch.full((40, cols), 1000.0, device=DEV)
+        x[torch.arange(40, device=DEV), torch.arange(40, device=DEV) % cols] = 1008.0
+        x = x.bfloat16()
+    dy = randn(40, cols, seed=2).to(x.dtype)
+    _, mean, rstd = ogq.ogq_layer_norm_forward(x)
+    v, d, U = x.double(), dy.double(), ref.U
+    m = v.mean(1, keepdim=True)
+    r = ((v - m).square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    u = (v - m) * r
+    # u: rstd is off by 50 U, and the mean of u, whose terms are u and what the mean's rounding (half a step of it, and of its correction) makes of the deviation, has a chain of at most 74 roundings
+    off_u = U * (60 * u.abs() + 100 * (u.abs().mean(1, keepdim=True) + 2 * U * m.abs() * r))
+    for weight in (1.0 + 0.1 * randn(cols, seed=3), None):
+        got = ogq.ogq_layer_norm_backward(dy, x, mean, rstd, weight)
+        g = d if weight is None else d * weight.double()
+        a, b = g.mean(1, keepdim=True), (g * u).mean(1, keepdim=True)
+        dx = r * (g - a - u * b)
+        off_b = (g.abs() * off_u).mean(1, keepdim=True) + 80 * U * (g * u).abs().mean(1, keepdim=True)
+        bound = r * (6 * U * g.abs() + 80 * U * g.abs().mean(1, keepdim=True) + off_u * b.abs() + u.abs() * off_b) + 50 * U * dx.abs()
+        ref.close(got if weight is None else got[0], dx, ref.rounded(bound, dx, x.dtype), "dx")
+        if weight is not None:
+            dweight = (d * u).sum(0)
+            ref.close(got[1], dweight, ref.rounded((d.abs() * off_u).sum(0) + 130 * U * (d * u).abs().sum(0), dweight, torch.float32), "dweight")
