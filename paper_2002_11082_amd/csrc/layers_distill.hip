@@ -18,32 +18,27 @@ struct Distill {
     const float *values, *row_weight;
     float* loss;
     uint32_t slices;                // of a row, where several workgroups share it
-    float2* parts;                  // [rows][slices]: a slice's largest logit over the temperature and the sum of its exponentials
+    float2* parts;                  // [rows][slices]: a slice's largest logit, as Below has it, and the sum of its exponentials
     float* logits_there;            // [rows][top]: the logits at the teacher's places
 };
 
-// exp((x - most) / temperature), most being over the temperature already: in fp32 to a few roundings of 32 bits, for 16-bit results to 2^-17 of it.
-template <class T>
-struct ExpBelow {
-    float factor, most;
-    __device__ __forceinline__ ExpBelow(float per_temperature, float most_)
-    {
-        factor = sizeof(T) == 4 ? per_temperature : per_temperature * kLog2e;
-        most = sizeof(T) == 4 ? most_ : most_ * kLog2e;
-    }
-    __device__ __forceinline__ float operator()(float x) const
-    {
-        if constexpr (sizeof(T) == 4) {
-            const float d = x * factor - most;
-            // (-infinity has no fraction, NaN none either: the instruction takes both)
-            return d < -200.0f ? 0.0f : exp_of(d, 0.0f);
-        } else {
-            return __builtin_amdgcn_exp2f(__builtin_fmaf(x, factor, -most));
-        }
-    }
-};
-
+// exp(d) for d that are at most 0 but for a rounding.
 __device__ __forceinline__ float exp_of_share(float d) { return d < -200.0f ? 0.0f : exp_of(d, 0.0f); }
+
+// (x - most) / temperature for the logits x of a row, most being the largest, times 1 (fp32) or log2(e) (16 bits), and exp of it: in fp32 to a few roundings of 32 bits, for 16-bit results to 2^-17 of it.  The largest logit
+// is held times the factor, `held`, rounded.  All differences, those of the loss too, are one rounding from that same number, so that its own rounding, which grows with an offset of the logits,
+// is in none of the results: it cancels between a logit and the sum of exponentials.
+template <class T>
+struct Below {
+    static constexpr bool kWide = sizeof(T) == 4;
+    float factor, held;
+    static __device__ __forceinline__ float factor_of(float per_temperature) { return kWide ? per_temperature : per_temperature * kLog2e; }
+    __device__ __forceinline__ float difference(float x) const { return __builtin_fmaf(x, factor, -held); }
+    // exp of a difference.  (-infinity has no fraction, NaN none either: the instruction takes both)
+    static __device__ __forceinline__ float power(float d) { return kWide ? exp_of_share(d) : __builtin_amdgcn_exp2f(d); }
+    __device__ __forceinline__ float exp(float x) const { return power(difference(x)); }
+    __device__ __forceinline__ float natural(float x) const { return kWide ? difference(x) : difference(x) * 0.693147180559945f; }
+};
 
 // Place n of a row, -1 where it stands for none.
 __device__ __forceinline__ int64_t place_at(const Distill& s, uint64_t n)
@@ -144,6 +139,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
     uint32_t place[kSlots];
     float value[kSlots], logit[kSlots];
     float most_value = -INFINITY, most = -INFINITY, total = 0.0f, teacher = 0.0f;
+    const float factor = Below<T>::factor_of(s.per_temperature);
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
         const uint32_t slot = k * THREADS + thread;
@@ -153,7 +149,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
             const int64_t c = place_at(s, n);
             if (c >= 0) {
                 place[k] = (uint32_t)c;
-                value[k] = s.values[n] * s.per_temperature;
+                value[k] = s.values[n];
                 logit[k] = PASS == Pass::kRest ? s.logits_there[n] : (float)from[c];
                 most_value = fmaxf(most_value, value[k]);
                 if (PASS == Pass::kPart) s.logits_there[n] = logit[k];
@@ -166,15 +162,15 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
         for (uint32_t n = thread; n < s.slices; n += THREADS) most = fmaxf(most, parts[n].x);
         const float2 t = sums.largest(most, most_value);
         most = t.x, most_value = t.y;
-        for (uint32_t n = thread; n < s.slices; n += THREADS) total += parts[n].y * exp_of_share(parts[n].x - most);
+        for (uint32_t n = thread; n < s.slices; n += THREADS) total += parts[n].y * Below<T>::power(parts[n].x - most);
     } else {
         each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < N; ++i) most = fmaxf(most, P != 0 || counts(i) ? v[i] : -INFINITY);  // (twice is no harm)
         });
-        const float2 t = sums.largest(most * s.per_temperature, most_value);
+        const float2 t = sums.largest(most * factor, most_value);
         most = t.x, most_value = t.y;
-        const ExpBelow<T> exp_below(s.per_temperature, most);
+        const Below<T> below{factor, most};
         if (PASS == Pass::kPart && most == -INFINITY) {  // nothing but -infinities, of which the row may have others, and NaN
             each_piece(kOnly, [&](const float(&v)[N], auto) __attribute__((always_inline)) {
 #pragma unroll
@@ -184,16 +180,17 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
             each_piece(kOnly, [&](const float(&v)[N], auto counts) __attribute__((always_inline)) {
                 float t = 0.0f;
 #pragma unroll
-                for (int i = 0; i < N; ++i) t += counts(i) ? exp_below(v[i]) : 0.0f;
+                for (int i = 0; i < N; ++i) t += counts(i) ? below.exp(v[i]) : 0.0f;
                 total += t;
             });
         }
     }
+    const Below<float> below_teacher{s.per_temperature, most_value * s.per_temperature};
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
         const bool there = place[k] != 0xFFFFFFFFu;
         // (the largest of values that are all -infinity or NaN is -infinity: of the first the row has none, the second are NaN)
-        value[k] = there && value[k] != -INFINITY ? value[k] - most_value : -INFINITY;
+        value[k] = there && value[k] != -INFINITY ? below_teacher.difference(value[k]) : -INFINITY;
         const float e = there ? exp_of_share(value[k]) : 0.0f;
         teacher += e;
         if constexpr (kGradient) {
@@ -213,24 +210,24 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
         finish_without();
         return;
     }
-    const ExpBelow<T> exp_below(s.per_temperature, most);
+    const Below<T> below{factor, most};
     const float per_teacher = 1.0f / teacher, log_teacher = logf(teacher), log_total = logf(total);
     float divergence = 0.0f;
 #pragma unroll
     for (int k = 0; k < kSlots; ++k) {
         const float p = place[k] != 0xFFFFFFFFu ? exp_of_share(value[k]) * per_teacher : 0.0f;
         // (not equal to 0: a NaN stays)
-        if (p != 0.0f) divergence += p * ((value[k] - log_teacher) - ((logit[k] * s.per_temperature - most) - log_total));
+        if (p != 0.0f) divergence += p * ((value[k] - log_teacher) - (below.natural(logit[k]) - log_total));
     }
     const float2 sum = sums(divergence, 0.0f);
     if (thread == 0 && slice == 0 && s.loss != nullptr) s.loss[row] = row_weight * s.temperature * s.temperature * sum.x;
     if constexpr (kGradient) {
         // (a NaN of the teacher's is in `teacher`, one of the student's in `total`)
         if (PASS == Pass::kRest && dlogits == nullptr) return;
-        const float factor = row_weight * s.temperature, per_total = 1.0f / total, scale = teacher != teacher ? teacher : factor * per_total;
+        const float out = row_weight * s.temperature, per_total = 1.0f / total, scale = teacher != teacher ? teacher : out * per_total;
         each_piece(kStore, [&](float(&v)[N], auto) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = exp_below(v[i]) * scale;
+            for (int i = 0; i < N; ++i) v[i] = below.exp(v[i]) * scale;
         });
         // Behind the row's other values: the places, each with the shares of all that are the same.
         __syncthreads();
@@ -244,7 +241,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T* logits, Disti
                 p += a.x == place[k] ? c.x : 0.0f, p += a.y == place[k] ? c.y : 0.0f, p += a.z == place[k] ? c.z : 0.0f, p += a.w == place[k] ? c.w : 0.0f;
                 p += b.x == place[k] ? d.x : 0.0f, p += b.y == place[k] ? d.y : 0.0f, p += b.z == place[k] ? d.z : 0.0f, p += b.w == place[k] ? d.w : 0.0f;
             }
-            to[place[k]] = (T)(factor * (exp_below(logit[k]) * per_total - p * per_teacher));
+            to[place[k]] = (T)(out * (below.exp(logit[k]) * per_total - p * per_teacher));
         }
     }
 }

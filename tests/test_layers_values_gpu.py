@@ -129,3 +129,32 @@ def test_layer_norm_backward_far_from_zero(kind, cols):
         if weight is not None:
             dweight = (d * u).sum(0)
             ref.close(got[1], dweight, ref.rounded((d.abs() * off_u).sum(0) + 130 * U * (d * u).abs().sum(0), dweight, torch.float32), "dweight")
+
+
+# ------------------------------------------------------------------------------------------------------------- distill
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("top", [1, 20])
+@pytest.mark.parametrize("rows,cols", [(300, 700), (200, 3000), (200, 30000), (60, 60000), (100, 150000)])
+def test_distill_loss_far_from_zero(rows, cols, top, dtype):
+    """An offset of all of a row's logits and of the teacher's values costs nothing: the loss is as exact as differences from the largest logit make it."""
+    for offset, temperature in ((0.0, 1.0), (100.0, 1.5), (-1000.0, 1.0), (1000.0, 1.5), (1003.0, 1.0), (30000.0, 1.0)):
+        logits = (2.0 * randn(rows, cols, seed=1) + offset).to(dtype)
+        values = 2.0 * randn(rows, top, seed=2) + offset / 4
+        places = torch.rand(rows, cols, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).topk(top, 1).indices
+        t, U = temperature, ref.U
+        z, v = logits.double() / t, values.double() / t
+        z, v = z - z.amax(1, keepdim=True), v - v.amax(1, keepdim=True)
+        total = z.exp().sum(1, keepdim=True)
+        p = torch.softmax(v, 1)
+        log_p, log_q = torch.log_softmax(v, 1), z.gather(1, places) - total.log()
+        exact = t * t * (p * (log_p - log_q)).sum(1)
+        # A difference is one rounding and those of the factor and of log 2, in all below 6 U of it, and its exponential is off by as much and 6 U; sums of a row's exponentials have chains of at most 60
+        # additions, logarithms are off by 2 U.  The teacher's sums have as many terms as places.
+        mean = ((z.exp() / total) * z.abs()).sum(1, keepdim=True)
+        off_total = U * (66 + 6 * mean + 2 * total.log().abs())
+        off_teacher = U * (4 + 4 * v.abs().amax(1, keepdim=True) + top)
+        off = p * (6 * U * (z.gather(1, places).abs() + v.abs()) + off_total + off_teacher + 4 * U * (log_p.abs() + log_q.abs()))
+        bound = t * t * (off.sum(1) + ((2 * off_teacher + min(top, 30) * U) * p * (log_p - log_q).abs()).sum(1))
+        bound = bound + 4 * U * exact.abs()
+        ref.close(ogq.ogq_distill_loss(logits, places, values, t), exact, bound, f"loss at {offset}")
+        ref.close(ogq.ogq_distill_gradient(logits, places, values, t)[0], exact, bound, f"loss and gradient at {offset}")
