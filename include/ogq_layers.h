@@ -18,7 +18,8 @@
  *   - d_workspace: as many bytes as the size helper beside the entry point says, 16-byte aligned, may be NULL where that is 0.  Its contents before the call do not matter.  Calls that may
  *     run at the same time, replays of captured graphs among them, need workspaces of their own.
  *   - A call may be several launches; where the runtime refuses one, those before it are enqueued all the same.
- *   - Sums are held in fp32 (or more) in an order that the sizes alone decide (and the tokens, where a text below says so): results are the same from call to call.  Values are rounded once, to the type of the output.
+ *   - Sums are held in fp32 (or more) in an order that the sizes alone decide (and the tokens, where a text below says so): results are the same from call to call.  Values are rounded once, to the type of the output; outputs in fp32 are as
+ *     exact for inputs in 16 bits as for those in fp32.
  */
 #ifndef OGQ_LAYERS_H
 #define OGQ_LAYERS_H

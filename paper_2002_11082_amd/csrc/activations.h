@@ -106,26 +106,32 @@ __device__ __forceinline__ void activation(float x, float& value, float& slope)
     }
 }
 
-template <uint32_t ACT, int N, class F>
+template <uint32_t ACT, bool EXACT, int N, class F>
 __device__ __forceinline__ void each(const float (&x)[N], F f)
 {
-    constexpr bool kExact = N == kPiece<float>;  // (a piece of 32-bit values)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float value, slope;
-        activation<ACT, kExact>(x[i], value, slope);
+        activation<ACT, EXACT>(x[i], value, slope);
         f(i, value, slope);
     }
 }
 
 // f(i, act(x[i]), act'(x[i])): the activation is the same in all lanes, a branch of the scalar unit.
+template <bool EXACT, int N, class F>
+__device__ __forceinline__ void each_as(uint32_t act, const float (&x)[N], F f)
+{
+    if (act == OGQ_RELU) each<OGQ_RELU, EXACT>(x, f);
+    else if (act == OGQ_GELU) each<OGQ_GELU, EXACT>(x, f);
+    else if (act == OGQ_GELU_TANH) each<OGQ_GELU_TANH, EXACT>(x, f);
+    else each<OGQ_SILU, EXACT>(x, f);
+}
+
+// As exact as the results need it: a piece of four values is one of 32 bits.
 template <int N, class F>
 __device__ __forceinline__ void each_of(uint32_t act, const float (&x)[N], F f)
 {
-    if (act == OGQ_RELU) each<OGQ_RELU>(x, f);
-    else if (act == OGQ_GELU) each<OGQ_GELU>(x, f);
-    else if (act == OGQ_GELU_TANH) each<OGQ_GELU_TANH>(x, f);
-    else each<OGQ_SILU>(x, f);
+    each_as<N == kPiece<float>>(act, x, f);
 }
 
 }  // namespace ogq

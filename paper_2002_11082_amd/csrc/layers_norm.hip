@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
                     continue;
                 }
                 if constexpr (WHAT == Columns::kActivation) {
-                    each_of(act, v, [&](int i, float, float slope) { g[i] *= slope; });
+                    each_as<true>(act, v, [&](int i, float, float slope) { g[i] *= slope; });  // (16-bit types too: the sums are of 32 bits)
                     store_piece<false>(dz + row * dz_stride + col, valid, g);
                 }
 #pragma unroll

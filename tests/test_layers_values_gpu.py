@@ -158,3 +158,21 @@ def test_distill_loss_far_from_zero(rows, cols, top, dtype):
         bound = bound + 4 * U * exact.abs()
         ref.close(ogq.ogq_distill_loss(logits, places, values, t), exact, bound, f"loss at {offset}")
         ref.close(ogq.ogq_distill_gradient(logits, places, values, t)[0], exact, bound, f"loss and gradient at {offset}")
+
+
+# -------------------------------------------------------------------------------------------------------------- linear
+# How far a slope may be off in 32 bits, in U.  silu, s (1 + x (1 - s)): 7 U and 6 U in the second term, which is at most 0.28, and two roundings.  gelu, p + x g / sqrt(2 pi): 2 U, and 5 U of at most 0.25,
+# and two roundings.  gelu by tanh, s + x s (1 - s) u'(x): s is off by 7 U and by what the argument's 5 U make of it, at most 0.23 of them; the second term, at most 0.3, by 10 U and |u| (at most 4 where the term is above 0.1,
+# and less than 1 / term elsewhere) times 5 U.
+SLOPES = {"relu": 0, "silu": 11, "gelu": 6, "gelu_tanh": 19}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", SLOPES)
+def test_bias_gradients_are_of_32_bits_in_all_types(act, dtype):
+    """Of one token whose dy is 1 the bias' gradient are the slopes, in fp32 whatever the tokens' type."""
+    z = torch.cat([torch.linspace(-12, 12, 20001, device=DEV), torch.linspace(3, 6, 5000, device=DEV)]).to(dtype)[None]
+    dz, dbias = ogq.ogq_linear_backward(torch.ones_like(z), {"relu": ogq.RELU, "silu": ogq.SILU, "gelu": ogq.GELU, "gelu_tanh": ogq.GELU_TANH}[act], z)
+    slope = ref.act(act, z[0].double())[1]
+    ref.close(dbias, slope, torch.full_like(slope, SLOPES[act] * ref.U), "dbias")
+    assert torch.equal(dz[0], dbias.to(dtype))
