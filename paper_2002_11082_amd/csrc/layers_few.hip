@@ -85,15 +85,15 @@ __global__ __launch_bounds__(kBlock) void few_tokens_kernel(const T* x, const T*
 
 // y[t][o] = sum over k of x[t][k] * W[k][o], in fp32: 64 pieces of a row of weights to a workgroup, and `part` rows, which its four wavefronts take in turn.  One token, 4096 x 16384: 41 us
 // (6.5 TB/s).
-template <class T, int TOKENS>
-__global__ __launch_bounds__(kBlock) void few_tokens_across_kernel(const T* x, const T* weight, LinearShape s, Epilogue<T> e)
+template <int TOKENS>
+__global__ __launch_bounds__(kBlock) void few_tokens_across_kernel(const float* x, const float* weight, LinearShape s, Epilogue<float> e)
 {
-    constexpr int N = kPiece<T>, kAhead = 8;
+    constexpr int N = kPiece<float>, kAhead = 8;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t block = this_block() % s.tiles_out, part = this_block() / s.tiles_out;
     if (part >= s.parts) return;
     const uint32_t out = (block * 64 + lane) * N;
-    const int valid = valid_of<T>(out, s.outs);
+    const int valid = valid_of<float>(out, s.outs);
     const uint32_t first = part * s.part, last = min(s.cols, first + s.part);
     float sum[TOKENS][N] = {};
     if (valid != 0) {
@@ -105,13 +105,13 @@ __global__ __launch_bounds__(kBlock) void few_tokens_across_kernel(const T* x, c
                 const uint32_t row = min(at + n, last - 1);
                 w[n] = load_raw(weight + (uint64_t)row * s.weight_stride + out, valid);
 #pragma unroll
-                for (int t = 0; t < TOKENS; ++t) v[t][n] = (float)x[t * s.x_stride + row];
+                for (int t = 0; t < TOKENS; ++t) v[t][n] = x[t * s.x_stride + row];
             }
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) {
                 if (at + n >= last) break;
                 float a[N];
-                values_of<T>(w[n], a);
+                values_of<float>(w[n], a);
 #pragma unroll
                 for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
@@ -149,46 +149,47 @@ __global__ __launch_bounds__(kBlock) void few_tokens_across_kernel(const T* x, c
 }  // namespace
 
 // Rows of weights: four to a wavefront or, where all of a workgroup's wavefronts find a piece of a row, to a workgroup; one where there are few.  bf16, one token, by wavefront and by workgroup:
-// 16384 x 4096 22.8 us and 19.5, 4096 x 16384 26.6 and 20.0, 50000 x 1024 15.7 and 15.5, 16384 x 1024 4.0 and 5.8, 16384 x 256 4.1 and 5.1; 4096 x 256 4.6 and 4.3.  Transposed: as many parts as
-// give enough workgroups, of 32 rows at least, since the parts' sums are written and read again.
-FewPlan few_plan(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed)
-{
-    FewPlan p{4, 1, (uint32_t)cols, 1};
-    if (!transposed) {
-        if (outs < 8192 || cols >= (dtype == OGQ_FP32 ? 1024u : 2048u)) p.split = 4;
-        if (outs < 2048) p.rows = 1;
-        return p;
-    }
-    const uint64_t blocks = ceil_div(outs, dtype == OGQ_FP32 ? 256 : 512);
-    const uint64_t wanted = blocks < 512 ? 512 / blocks : 1, most = cols < 64 ? 1 : cols / 32;
-    const uint64_t parts = wanted < most ? wanted : most;
-    p.part = cols == 0 ? 32 : (uint32_t)(ceil_div(ceil_div(cols, parts), 32) * 32);
-    p.parts = cols == 0 ? 1 : (uint32_t)ceil_div(cols, p.part);
-    return p;
-}
-
+// 16384 x 4096 22.8 us and 19.5, 4096 x 16384 26.6 and 20.0, 50000 x 1024 15.7 and 15.5, 16384 x 1024 4.0 and 5.8, 16384 x 256 4.1 and 5.1; 4096 x 256 4.6 and 4.3.
 template <class T>
-void launch_few(const FewPlan& plan, const T* x, const T* weight, bool transposed, const LinearShape& s, const Epilogue<T>& e, hipStream_t st)
+void launch_few(const T* x, const T* weight, const LinearShape& s, const Epilogue<T>& e, hipStream_t st)
 {
+    const bool split = s.outs < 8192 || s.cols >= (sizeof(T) == 4 ? 1024u : 2048u);
     const auto go = [&](auto number) {
         constexpr int kTokens = decltype(number)::value;
         if (s.tokens != kTokens) return;
-        if constexpr (sizeof(T) == 4)
-            if (transposed) {
-                launch_kernel(few_tokens_across_kernel<T, kTokens>, grid_of((uint64_t)s.tiles_out * s.parts), dim3(kBlock), st, x, weight, s, e);
-                return;
-            }
-        if (plan.rows == 1) launch_kernel(few_tokens_kernel<T, kTokens, 1, 4>, grid_of(s.outs), dim3(kBlock), st, x, weight, s, e);
-        else if (plan.split == 4) launch_kernel(few_tokens_kernel<T, kTokens, 4, 4>, grid_of(ceil_div(s.outs, 4)), dim3(kBlock), st, x, weight, s, e);
+        if (s.outs < 2048) launch_kernel(few_tokens_kernel<T, kTokens, 1, 4>, grid_of(s.outs), dim3(kBlock), st, x, weight, s, e);
+        else if (split) launch_kernel(few_tokens_kernel<T, kTokens, 4, 4>, grid_of(ceil_div(s.outs, 4)), dim3(kBlock), st, x, weight, s, e);
         else launch_kernel(few_tokens_kernel<T, kTokens, 4, 1>, grid_of(ceil_div(s.outs, 16)), dim3(kBlock), st, x, weight, s, e);
     };
     go(std::integral_constant<int, 1>{}), go(std::integral_constant<int, 2>{}), go(std::integral_constant<int, 3>{}), go(std::integral_constant<int, 4>{});
     go(std::integral_constant<int, 5>{}), go(std::integral_constant<int, 6>{}), go(std::integral_constant<int, 7>{}), go(std::integral_constant<int, 8>{});
-    if (transposed && s.sums != nullptr) launch_join_parts(s, e, st);
 }
 
-template void launch_few<float>(const FewPlan&, const float*, const float*, bool, const LinearShape&, const Epilogue<float>&, hipStream_t);
-template void launch_few<__bf16>(const FewPlan&, const __bf16*, const __bf16*, bool, const LinearShape&, const Epilogue<__bf16>&, hipStream_t);
-template void launch_few<_Float16>(const FewPlan&, const _Float16*, const _Float16*, bool, const LinearShape&, const Epilogue<_Float16>&, hipStream_t);
+// As many parts as give enough workgroups, of 32 rows at least, since the parts' sums are written and read again.
+FewParts few_parts(size_t outs, size_t cols)
+{
+    if (cols == 0) return {32, 1};
+    const uint64_t blocks = ceil_div(outs, 256), wanted = blocks < 512 ? 512 / blocks : 1, most = cols < 64 ? 1 : cols / 32, parts = wanted < most ? wanted : most;
+    const uint32_t part = (uint32_t)(ceil_div(ceil_div(cols, parts), 32) * 32);
+    return {part, (uint32_t)ceil_div(cols, part)};
+}
+
+void launch_few_across(const float* x, const float* weight, LinearShape s, const Epilogue<float>& e, float* workspace, hipStream_t st)
+{
+    const FewParts parts = few_parts(s.outs, s.cols);
+    s.tiles_out = (uint32_t)ceil_div(s.outs, 256), s.part = parts.part, s.parts = parts.parts;
+    s.sums = parts.parts > 1 ? workspace : nullptr;
+    const auto go = [&](auto number) {
+        constexpr int kTokens = decltype(number)::value;
+        if (s.tokens == kTokens) launch_kernel(few_tokens_across_kernel<kTokens>, grid_of((uint64_t)s.tiles_out * s.parts), dim3(kBlock), st, x, weight, s, e);
+    };
+    go(std::integral_constant<int, 1>{}), go(std::integral_constant<int, 2>{}), go(std::integral_constant<int, 3>{}), go(std::integral_constant<int, 4>{});
+    go(std::integral_constant<int, 5>{}), go(std::integral_constant<int, 6>{}), go(std::integral_constant<int, 7>{}), go(std::integral_constant<int, 8>{});
+    if (s.sums != nullptr) launch_join_parts(s, e, st);
+}
+
+template void launch_few(const float*, const float*, const LinearShape&, const Epilogue<float>&, hipStream_t);
+template void launch_few(const __bf16*, const __bf16*, const LinearShape&, const Epilogue<__bf16>&, hipStream_t);
+template void launch_few(const _Float16*, const _Float16*, const LinearShape&, const Epilogue<_Float16>&, hipStream_t);
 
 }  // namespace ogq

@@ -94,19 +94,21 @@ struct LinearShape {
 // On the vector unit and in tiles, bf16: 16384 x 4096 2 tokens 19.9 us and 23.8, 4 22.0 and 23.9, 6 26.2 and 24.0; 4096 x 4096 2 4.6 and 10.5, 8 11.0 and 11.1; 50000 x 1024 1 15.5 and 18.9, 2 21.6 and
 // 18.8; transposed (16384 x 4096) 1 34.0 and 24.3, 8 40.5 and 24.9.  fp32: 16384 x 4096 1 38.6 and 57.9, 8 49.7 and 59.6; 4096 x 4096 8 15.5 and 22.0; transposed 16384 x 4096 1 41.3 and
 // 61.6, 8 50.6 and 63.1.
+// Transposed in fp32 alone.
 inline bool few_tokens(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed)
 {
     if (tokens > 8 || dtype == OGQ_FP32) return tokens <= 8;
     if (transposed) return false;
     return tokens == 1 || outs * cols <= (size_t)1 << 24 || (tokens <= 4 && cols >= 2048);
 }
-struct FewPlan {
-    uint32_t rows, split;   // weights' rows of a wavefront and wavefronts to a row; or
-    uint32_t part, parts;   // transposed: rows of a part of the sum, and how many
-};
-FewPlan few_plan(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed);
 template <class T>
-void launch_few(const FewPlan& plan, const T* x, const T* weight, bool transposed, const LinearShape& s, const Epilogue<T>& e, hipStream_t st);
+void launch_few(const T* x, const T* weight, const LinearShape& s, const Epilogue<T>& e, hipStream_t st);
+// Transposed: rows of weights in a part of the sum, and how many parts.
+struct FewParts {
+    uint32_t part, parts;
+};
+FewParts few_parts(size_t outs, size_t cols);
+void launch_few_across(const float* x, const float* weight, LinearShape s, const Epilogue<float>& e, float* workspace, hipStream_t st);
 
 // layers_linear.hip: the parts' sums, added in their order, through the epilogue.
 template <class T>

@@ -778,7 +778,7 @@ template void launch_join_parts<_Float16>(const LinearShape&, const Epilogue<_Fl
 
 size_t linear_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, bool transposed)
 {
-    const uint32_t parts = few_tokens(tokens, outs, cols, dtype, transposed) ? few_plan(tokens, outs, cols, dtype, transposed).parts : plan_of(tokens, outs, cols, dtype, true).parts;
+    const uint32_t parts = !few_tokens(tokens, outs, cols, dtype, transposed) ? plan_of(tokens, outs, cols, dtype, true).parts : transposed ? few_parts(outs, cols).parts : 1;
     return parts > 1 ? (size_t)parts * tokens * pitch_of(outs) * sizeof(float) : 0;
 }
 
@@ -793,10 +793,12 @@ void launch_linear(const Values& x, const Values& weight, bool transposed, size_
                             before.stride, s.outs,                               act};
         const auto from = static_cast<const T*>(x.data), w = static_cast<const T*>(weight.data);
         if (few_tokens(tokens, outs, cols, dtype, transposed)) {
-            const FewPlan plan = few_plan(tokens, outs, cols, dtype, transposed);
-            s.tiles_out = (uint32_t)ceil_div(outs, 64 * kPiece<T>), s.part = plan.part, s.parts = plan.parts;
-            s.sums = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
-            launch_few(plan, from, w, transposed, s, e, st);
+            if constexpr (sizeof(T) == 4)
+                if (transposed) {
+                    launch_few_across(from, w, s, e, static_cast<float*>(workspace), st);
+                    return;
+                }
+            launch_few(from, w, s, e, st);
             return;
         }
         // (with rows that are not near, what takes large tiles elsewhere takes others in one part: the workspace is what the sizes say)
