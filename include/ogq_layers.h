@@ -61,8 +61,8 @@ int ogq_layer_norm_backward(const void* d_dy, size_t dy_stride, const void* d_x,
 /* A linear layer: z = x W^T + bias, y = act(z) + residual, x [tokens, cols], W [outs, cols], y [tokens, outs]; all of one type but the bias.
  * transposed != 0: W is [cols, outs], z = x W + bias: with a layer's own weights and the gradient of its outputs for x, the gradient of its inputs.
  * d_bias, d_residual: NULL for none.  d_before: z as well, for the backward pass, NULL for no need of it.
- * activation: one of ogq_activation_t or OGQ_IDENTITY.  Products of 16-bit types are exact; those of fp32 are made of pieces of bf16, off by 2^-22 of a product's size, and what a value
- * has below 2^-133 may be lost in them.  d_y may be d_residual with the same stride.  tokens * outs below 2^38 in whole tiles of 128 x 128. */
+ * activation: one of ogq_activation_t or OGQ_IDENTITY.  Products of 16-bit types are exact; those of fp32 are made of pieces of bf16, less than 2^-21 of a product's size nearer
+ * to zero, and what a value has below 2^-133 may be lost in them.  d_y may be d_residual with the same stride.  tokens * outs below 2^38 in whole tiles of 128 x 128. */
 size_t ogq_linear_workspace(size_t tokens, size_t outs, size_t cols, uint32_t dtype, int transposed);
 int ogq_linear(const void* d_x, size_t x_stride, const void* d_weight, size_t weight_stride, int transposed, size_t tokens, size_t outs, size_t cols, uint32_t dtype,
                const float* d_bias, uint32_t activation, const void* d_residual, size_t residual_stride, void* d_y, size_t y_stride, void* d_before, size_t before_stride,

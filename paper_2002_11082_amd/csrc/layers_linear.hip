@@ -324,7 +324,7 @@ __global__ __launch_bounds__(256 * TEAMS) void linear_kernel(const T* x, const T
         s16x8 w[NO], x[NT];
     };
     const auto read = [&](Operands& r, const char* at, int n) __attribute__((always_inline)) {
-        constexpr int kW[6] = {2, 0, 1, 1, 0, 0}, kX[6] = {0, 2, 1, 0, 1, 0};  // (all but those below 2^-24 of the largest, the smallest first)
+        constexpr int kW[6] = {2, 0, 1, 1, 0, 0}, kX[6] = {0, 2, 1, 0, 1, 0};  // (the smallest first.  The second piece is below 2^-7 of the first, the third below 2^-15: the three pairs left out are below 2^-21 of a product, with its sign)
         const int h = n / kPairs, p = kPairs == 1 ? 0 : kW[n % 6], q = kPairs == 1 ? 0 : kX[n % 6];
 #pragma unroll
         for (int i = 0; i < NO; ++i) r.w[i] = FeedW::read(at + p * FeedW::kPlane, out_wave + 32 * i, h, lane);

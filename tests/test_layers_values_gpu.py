@@ -6,6 +6,7 @@ import torch
 
 import paper_2002_11082_amd as ogq
 from tests import layers_reference as ref
+from tests.layers_layouts import LINEAR
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -176,3 +177,114 @@ def test_bias_gradients_are_of_32_bits_in_all_types(act, dtype):
     slope = ref.act(act, z[0].double())[1]
     ref.close(dbias, slope, torch.full_like(slope, SLOPES[act] * ref.U), "dbias")
     assert torch.equal(dz[0], dbias.to(dtype))
+
+
+# few tokens on the vector unit, and all that goes to the matrix cores
+LAYOUTS = [(1, 300, 90, 0), (7, 3000, 90, 0)] + LINEAR
+
+
+def laid_out(values, pad):
+    wide = torch.empty(values.shape[0], values.shape[1] + pad, dtype=values.dtype, device=DEV)
+    wide[:, :values.shape[1]] = values
+    return wide[:, :values.shape[1]]
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols,pad", LAYOUTS)
+def test_fp32_products_have_all_their_pieces(tokens, outs, cols, pad, transposed):
+    """Sums of which one product is not 0.  Factors are cut into three pieces, the last below 2^-15 of the first and the second below 2^-7: the three products that are left out are below 2^-21 in all, and the sum of the six
+    that are taken has at most four roundings of its size."""
+    print("[layers] one product", tokens, outs, cols, pad, transposed, flush=True)
+    x = torch.zeros(tokens, cols, device=DEV)
+    at = torch.randint(0, cols, (tokens,), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    value, w = randn(tokens, seed=2), randn(outs, cols, seed=3)
+    x[torch.arange(tokens, device=DEV), at] = value
+    exact = value.double()[:, None] * w.double().t()[at]
+    got = ogq.ogq_linear(laid_out(x, pad), laid_out(w.t().contiguous() if transposed else w, pad), transposed=transposed)
+    ref.close(got, exact, (2.0 ** -21 + 4 * ref.U) * exact.abs(), "y")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols,pad", LAYOUTS)
+def test_linear_of_subnormal_factors(tokens, outs, cols, pad, transposed, dtype):
+    """Subnormal values of x count in full: whole numbers of the type's least, times whole numbers of a large power of two, so that sums are exact.  (In fp32 of 2^-133, below which the pieces have nothing.)"""
+    print("[layers] subnormal", tokens, outs, cols, pad, transposed, dtype, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    least, factor = {torch.float16: (-24, 9), torch.bfloat16: (-133, 100), torch.float32: (-133, 100)}[dtype]
+    a = torch.randint(-100, 101, (tokens, cols), generator=gen, device=DEV).double()
+    b = torch.randint(-3, 4, (outs, cols), generator=gen, device=DEV).double()
+    x, w = (a * 2.0 ** least).to(dtype), (b * 2.0 ** factor).to(dtype)
+    assert bool((x != 0).eq(a != 0).all()) and float(x.double().abs().max()) < torch.finfo(dtype).smallest_normal
+    weight = laid_out(w.t().contiguous() if transposed else w, pad)
+    exact = torch.mm(a, b.t()) * 2.0 ** (least + factor)
+    assert torch.equal(ogq.ogq_linear(laid_out(x, pad), weight, transposed=transposed), exact.to(dtype))
+    # and those of the weights
+    x, w = (a * 2.0 ** factor).to(dtype), (b * 2.0 ** least).to(dtype)
+    weight = laid_out(w.t().contiguous() if transposed else w, pad)
+    assert torch.equal(ogq.ogq_linear(laid_out(x, pad), weight, transposed=transposed), exact.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols,pad", LAYOUTS)
+def test_linear_of_infinities_and_nan_in_all_layouts(tokens, outs, cols, pad, transposed, dtype):
+    """They are in the sums that they belong to, in the first rows and the last, and in no others."""
+    print("[layers] infinities", tokens, outs, cols, pad, transposed, dtype, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randint(1, 4, (tokens, cols), generator=gen, device=DEV).to(dtype)
+    w = torch.randint(1, 4, (outs, cols), generator=gen, device=DEV).to(dtype)
+    x[-1, 5], w[7, 5], w[-1, 5], w[9, cols - 1], x[0, cols - 1] = math.inf, -2.0, 0.0, math.nan, 2.0
+    w[outs - 2, 3] = -math.inf
+    exact = torch.mm(x.double(), w.double().t())
+    assert torch.isnan(exact[:, 9]).all() and torch.isnan(exact[-1, -1]) and exact[-1, 7] == -math.inf and (tokens == 1 or exact[0, outs - 2] == -math.inf)
+    got = ogq.ogq_linear(laid_out(x, pad), laid_out(w.t().contiguous() if transposed else w, pad), transposed=transposed)
+    assert torch.equal(torch.isnan(got), torch.isnan(exact))
+    assert torch.equal(got.nan_to_num(nan=0.0, posinf=math.inf, neginf=-math.inf), exact.to(dtype).nan_to_num(nan=0.0, posinf=math.inf, neginf=-math.inf))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols,pad", LAYOUTS)
+def test_linear_in_all_layouts(tokens, outs, cols, pad, transposed, dtype):
+    """Sums of whole numbers are exact; with everything that happens to them on their way out, into tensors with gaps, in place of the residual."""
+    print("[layers] layouts", tokens, outs, cols, pad, transposed, dtype, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x, w = (torch.randint(-3, 4, (n, cols), generator=gen, device=DEV).to(dtype) for n in (tokens, outs))
+    x, w = laid_out(x, pad), laid_out(w.t().contiguous() if transposed else w, pad)
+    exact = torch.mm(x.double(), w.double() if transposed else w.double().t())
+    assert torch.equal(ogq.ogq_linear(x, w, transposed=transposed), exact.to(dtype))
+    x = laid_out(randn(tokens, cols, seed=4).to(dtype), pad)
+    w = laid_out((randn(*w.shape, seed=5) / math.sqrt(cols)).to(dtype), pad)
+    bias, residual = randn(outs, seed=6), randn(tokens, outs, seed=7).to(dtype)
+    for act, b, r, keep in ((None, None, None, False), ("gelu", bias, None, True), ("silu", None, residual, False), ("gelu_tanh", bias, residual, True)):
+        (y, bound), (z, z_bound) = ref.linear(x, w, b, act, r, transposed)
+        wide = torch.full((2, tokens, outs + 3), 55.0, dtype=dtype, device=DEV)
+        out, before = wide[0, :, :outs], wide[1, :, :outs] if keep else None
+        if r is not None:
+            out.copy_(r)
+        ogq.ogq_linear(x, w, b, None if act is None else {"gelu": ogq.GELU, "silu": ogq.SILU, "gelu_tanh": ogq.GELU_TANH}[act], None if r is None else out, transposed, y=out, before=before)
+        ref.close(out, y, ref.rounded(bound, y, dtype), f"y {act}")
+        if keep:
+            ref.close(before, z, ref.rounded(z_bound, z, dtype), f"before {act}")
+        assert (wide[:, :, outs:] == 55).all() and (keep or (wide[1] == 55).all())
+        del y, bound, z, z_bound
+    assert torch.equal(ogq.ogq_linear(x, w, bias, ogq.GELU_TANH, residual, transposed), out)
+
+
+@pytest.mark.parametrize("cols", (1409, 1408))
+def test_more_tiles_of_256_x_256_than_a_row_of_workgroups(cols):
+    """More than 2^20 tiles, of rows that begin anywhere and of aligned ones: small whole numbers, so that sums are exact and each tile is a copy of the first ones."""
+    torch.cuda.empty_cache()
+    tokens, outs = (1 << 18) + 512, 1 << 18
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("less than 160 GiB of memory free")
+    print("[layers] many tiles", cols, flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    small, w = (torch.randint(-3, 4, (512, cols), generator=gen, device=DEV).bfloat16() for _ in range(2))
+    y = ogq.ogq_linear(small.repeat(tokens // 512, 1), w.repeat(outs // 512, 1))
+    want = (small.double() @ w.double().T).bfloat16().repeat(1, outs // 512)
+    for at in range(0, tokens, 512):
+        assert torch.equal(y[at:at + 512], want), at
+    del y
+    torch.cuda.empty_cache()
