@@ -180,7 +180,7 @@ def test_bias_gradients_are_of_32_bits_in_all_types(act, dtype):
 
 
 # few tokens on the vector unit, and all that goes to the matrix cores
-LAYOUTS = [(1, 300, 90, 0), (7, 3000, 90, 0)] + LINEAR
+LAYOUTS = [(tokens, 300, 90, 0) for tokens in range(1, 9)] + [(7, 3000, 90, 0)] + LINEAR
 
 
 def laid_out(values, pad):
