@@ -288,3 +288,25 @@ def test_more_tiles_of_256_x_256_than_a_row_of_workgroups(cols):
         assert torch.equal(y[at:at + 512], want), at
     del y
     torch.cuda.empty_cache()
+
+
+def fastest(call, times=5):
+    """us on the GPU of the fastest of several calls."""
+    call()
+    begin, end, least = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True), math.inf
+    for _ in range(times):
+        begin.record()
+        call()
+        end.record()
+        end.synchronize()
+        least = min(least, 1e3 * begin.elapsed_time(end))
+    return least
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_products_of_nan_take_a_few_times_as_long(transposed):
+    """A step of training that has gone wrong: NaN that come from NaN are not made again (which takes a hundred times as long)."""
+    x, w = randn(2048, 2048, seed=1), randn(2048, 2048, seed=2)
+    bad = torch.full_like(x, math.nan)
+    assert torch.isnan(ogq.ogq_linear(bad, w, transposed=transposed)).all()
+    assert fastest(lambda: ogq.ogq_linear(bad, w, transposed=transposed)) < 20 * fastest(lambda: ogq.ogq_linear(x, w, transposed=transposed))
