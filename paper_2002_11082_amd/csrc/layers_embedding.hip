@@ -50,29 +50,44 @@ __global__ __launch_bounds__(kBlock) void embedding_kernel(const void* tokens, b
     }
 }
 
-// Zeros for the table's gradient: rows of `length` values in units of kUnit, `units` of them to a row (one row where the table has no gaps).
+// Zeros for the table's gradient: rows of `length` values in units of kUnit, `units` of them to a row (one row where the table has no gaps), or `together` short rows to a unit (0: rows are not short).
+// 4096 tokens in a table of 200000 x 16 with gaps, all launches: 26 us, a row to a unit 446; without gaps 25.
 constexpr uint32_t kUnit = 16384;
 struct Fill {
     float* to;
-    uint64_t length, stride, units, first, last;  // units first ... last of all rows' are this launch's
+    uint64_t rows, length, stride, units, first, last;  // units first ... last of all rows' are this launch's
+    uint32_t together;
 };
+
+// Four zeros at `at` of a row of which `left` values are left.
+__device__ __forceinline__ void fill_piece(float* to, uint32_t at, uint64_t left)
+{
+    const f32x4 zero = {};
+    if (at + 4 <= left) {
+        memcpy(to + at, &zero, sizeof zero);
+    } else {
+        for (uint32_t i = at; i < at + 4; ++i)
+            if (i < left) to[i] = 0.0f;
+    }
+}
 
 __device__ __forceinline__ void fill_unit(const Fill& f, uint64_t unit)
 {
+    if (f.together != 0) {
+        const uint32_t pieces = (uint32_t)(f.length + 3) / 4;
+#pragma unroll
+        for (uint32_t n = 0; n < kUnit / 4 / kRun; ++n) {
+            const uint32_t at = n * kRun + threadIdx.x, in = at / pieces, begin = (at - in * pieces) * 4;
+            const uint64_t row = unit * f.together + in;
+            if (in < f.together && row < f.rows) fill_piece(f.to + row * f.stride, begin, f.length);
+        }
+        return;
+    }
     const uint64_t row = f.units == 1 ? unit : unit / f.units, begin = (unit - row * f.units) * kUnit;
     float* to = f.to + row * f.stride + begin;
     const uint64_t left = f.length - begin;
-    const f32x4 zero = {};
 #pragma unroll
-    for (uint32_t n = 0; n < kUnit / 4 / kRun; ++n) {
-        const uint32_t at = (n * kRun + threadIdx.x) * 4;
-        if (at + 4 <= left) {
-            memcpy(to + at, &zero, sizeof zero);
-        } else {
-            for (uint32_t i = at; i < at + 4; ++i)
-                if (i < left) to[i] = 0.0f;
-        }
-    }
+    for (uint32_t n = 0; n < kUnit / 4 / kRun; ++n) fill_piece(to, (n * kRun + threadIdx.x) * 4, left);
 }
 
 // The first `runs` workgroups sort 1024 keys each: every wavefront places its 64 by counting, then neighbouring runs become one, four times over: a key's place is its own and what the other run
@@ -416,9 +431,13 @@ Space space_of(size_t number, size_t cols)
 Fill fill_of(const Result& dtable, size_t vocab, size_t cols)
 {
     const bool gaps = dtable.stride != cols && vocab > 1;
-    Fill f{static_cast<float*>(dtable.data), gaps ? cols : vocab * cols, dtable.stride, 0, 0, 0};
+    Fill f{static_cast<float*>(dtable.data), gaps ? vocab : 1, gaps ? cols : vocab * cols, dtable.stride, 0, 0, 0, 0};
     f.units = ceil_div(f.length, kUnit);
-    f.last = f.units * (gaps ? vocab : 1);
+    f.last = f.units * f.rows;
+    if (gaps && cols <= kUnit / 2) {
+        f.together = (uint32_t)(kUnit / 4 / ceil_div(cols, 4));
+        f.last = ceil_div(vocab, f.together);
+    }
     return f;
 }
 

@@ -129,6 +129,26 @@ def test_a_table_gradient_with_gaps(vocab, cols, gap, number):
     assert (wide[:, 0] == 77).all() and (wide[:, 1 + cols:] == 77).all()
 
 
+def test_gaps_in_a_large_table_cost_little():
+    """Short rows are filled together: one at a time they take eighteen times as long as without gaps."""
+    vocab, cols = 200000, 16
+    tokens, dy = torch.arange(4096, device=DEV) * 17 % vocab, randn(4096, cols, seed=1)
+    wide, plain = torch.empty(vocab, cols + 4, device=DEV), torch.empty(vocab, cols, device=DEV)
+
+    def fastest(dtable):
+        begin, end, times = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True), []
+        for _ in range(6):
+            begin.record()
+            ogq.ogq_embedding_gradient(tokens, dy, vocab, dtable=dtable)
+            end.record()
+            end.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+
+    assert fastest(wide[:, :cols]) < 6 * fastest(plain)
+    assert torch.equal(wide[:, :cols], plain)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols", [(5, 7), (50, 1000), (30, 5000), (7, 33001), (5, 70003), (100, 140001)])
 def test_results_with_gaps(rows, cols, dtype):
