@@ -70,7 +70,8 @@ int ogq_linear(const void* d_x, size_t x_stride, const void* d_weight, size_t we
 
 /* What the backward pass of such a layer begins with: dz = dy * act'(z), z from d_before, and the bias' gradient, the sum of dz over the tokens (as it is before dz is rounded), in fp32
  * [outs], or added to what d_dbias holds.  The gradient of the residual is dy, that of x ogq_linear's with dz and the weights, that of the weights ogq_weight_gradient's.
- * OGQ_IDENTITY: dz is dy, d_before and d_dz are NULL.  d_dbias may be NULL otherwise.  d_dz may be d_dy or d_before with the same stride. */
+ * Where z was beyond fp16, and is infinite in d_before, act' is
+ * what it is far out: 0 or 1.  OGQ_IDENTITY: dz is dy, d_before and d_dz are NULL.  d_dbias may be NULL otherwise.  d_dz may be d_dy or d_before with the same stride. */
 size_t ogq_linear_backward_workspace(size_t tokens, size_t outs, uint32_t dtype);
 int ogq_linear_backward(const void* d_dy, size_t dy_stride, size_t tokens, size_t outs, uint32_t dtype, uint32_t activation, const void* d_before, size_t before_stride, void* d_dz,
                         size_t dz_stride, float* d_dbias, int accumulate, void* d_workspace, size_t workspace_bytes, void* hip_stream);

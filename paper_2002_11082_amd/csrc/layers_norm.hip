@@ -441,6 +441,11 @@ __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t d
                     continue;
                 }
                 if constexpr (WHAT == Columns::kActivation) {
+                    // (a z beyond fp16 was finite for the forward pass: its slope is the one far out, not infinity times 0)
+                    if constexpr (__is_same(T, _Float16)) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) v[i] = fabsf(v[i]) == INFINITY ? copysignf(0x1p100f, v[i]) : v[i];
+                    }
                     each_as<true>(act, v, [&](int i, float, float slope) { g[i] *= slope; });  // (16-bit types too: the sums are of 32 bits)
                     store_piece<false>(dz + row * dz_stride + col, valid, g);
                 }

@@ -179,6 +179,24 @@ def test_bias_gradients_are_of_32_bits_in_all_types(act, dtype):
     assert torch.equal(dz[0], dbias.to(dtype))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", SLOPES)
+def test_the_backward_pass_of_arguments_beyond_the_type(act, dtype):
+    """An argument below fp16's values leaves -infinity for the backward pass, and an output of 0: its slope is 0; that of one above them is 1."""
+    code = {"relu": ogq.RELU, "silu": ogq.SILU, "gelu": ogq.GELU, "gelu_tanh": ogq.GELU_TANH}[act]
+    x, w = torch.full((5, 40), 200.0, device=DEV).to(dtype), torch.full((30, 40), 10.0, device=DEV).to(dtype)
+    w[:7] = -10.0
+    y, before = ogq.ogq_linear(x, w, activation=code, keep=True)
+    assert (y[:, :7] == 0).all() and torch.isinf(before).all() == (dtype == torch.float16)
+    dy = randn(5, 30, seed=1).to(dtype)
+    dz, dbias = ogq.ogq_linear_backward(dy, code, before)
+    assert (dz[:, :7] == 0).all() and torch.equal(dz[:, 7:], dy[:, 7:])
+    assert (dbias[:7] == 0).all() and torch.equal(dbias, ogq.ogq_linear_backward(dz)[1])
+    z = torch.where(before < 0, math.nan, before)
+    dz, dbias = ogq.ogq_linear_backward(dy, code, z)
+    assert torch.isnan(dz[:, :7]).all() and torch.isnan(dbias[:7]).all() and torch.equal(dz[:, 7:], dy[:, 7:])
+
+
 # few tokens on the vector unit, and all that goes to the matrix cores
 LAYOUTS = [(tokens, 300, 90, 0) for tokens in range(1, 9)] + [(7, 3000, 90, 0)] + LINEAR
 
