@@ -43,7 +43,7 @@ enum { OGQ_IDENTITY = 4 };
 
 /* Layer norm of every row:
  *   y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
- * d_weight, d_bias: [cols], or NULL for 1 and 0.  d_mean, d_rstd: [rows], for the backward pass, both given or both NULL.  The variance is that of the differences from the mean, not
+ * d_weight, d_bias: [cols], or NULL for 1 and 0.  d_mean, d_rstd: [rows], for the backward pass, both given or both NULL (without columns neither is written).  The variance is that of the differences from the mean, not
  * one of squares; where it is beyond fp32 (differences of about 2^63 and more), rstd is 0 and y the bias. */
 int ogq_layer_norm_forward(const void* d_x, size_t x_stride, size_t rows, size_t cols, uint32_t dtype, const float* d_weight, const float* d_bias, float eps, void* d_y,
                            size_t y_stride, float* d_mean, float* d_rstd, void* hip_stream);

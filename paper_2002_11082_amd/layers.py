@@ -104,13 +104,14 @@ def _load_marshal():
 
 
 def ogq_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, rstd=None):
-    """(x - mean) * rstd * weight + bias for every row.  Returns (y, mean, rstd); the last two are for ogq_layer_norm_backward."""
+    """(x - mean) * rstd * weight + bias for every row.  Returns (y, mean, rstd); the last two are for ogq_layer_norm_backward (and not
+    written where there are no columns)."""
     return (_marshal or _load_marshal()).layer_norm_forward(x, weight, bias, eps, y, mean, rstd)
 
 
 def ogq_layer_norm_backward(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, accumulate: bool = False, workspace=None):
     """The gradient of ogq_layer_norm_forward's x from that of its y; with a weight (dx, dweight, dbias), with accumulate the last two added to those that are given.
-    dx may be dy."""
+    dx may be dy.  (The gradient of a bias without a weight is that of ogq_linear_backward(dy).)"""
     return (_marshal or _load_marshal()).layer_norm_backward(dy, x, mean, rstd, weight, dx, dweight, dbias, accumulate, workspace)
 
 
