@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2002_11082_amd as ogq
+from tests.layers_layouts import LINEAR
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -209,3 +210,89 @@ def test_results_that_the_c_entry_points_leave_out(rows, cols, dtype):
     want = ogq.ogq_distill_gradient(x, places, values)[1]
     assert lib.ogq_distill_gradient(pointer(x), cols, rows, cols, code, pointer(places), ogq.INT64, pointer(values), 2, 1.0, None, None, pointer(out), cols, pointer(space), space.numel(), stream()) == 0
     assert torch.equal(out, want)
+
+
+# ------------------------------------------------------------------------------------------------------------ workspaces
+class Space:
+    """A workspace of exactly the bytes that are asked for, between others that stay as they are; its contents are NaN at first."""
+
+    def __init__(self, size):
+        self.whole = torch.full((16 * 1024 + (size + 15) // 16 * 16 + 16 * 1024,), 0xFF, dtype=torch.uint8, device=DEV)
+        self.size, self.space = size, self.whole[16 * 1024:16 * 1024 + size]
+
+    def unharmed(self):
+        return bool((self.whole[:16 * 1024] == 0xFF).all()) and bool((self.whole[16 * 1024 + self.size:] == 0xFF).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_workspaces_of_just_the_right_size(dtype):
+    code = CODE[dtype]
+    for rows, cols in ((3, 2), (70, 7), (5, 300), (3000, 100), (2100, 515), (700, 4099), (520, 9001), (40, 33001), (3, 40001), (300, 17000)):
+        print("[layers] workspaces", rows, cols, dtype, flush=True)
+        x, dy, weight = randn(rows, cols, seed=1).to(dtype), randn(rows, cols, seed=2).to(dtype), randn(cols, seed=3)
+        _, mean, rstd = ogq.ogq_layer_norm_forward(x, weight)
+        space = Space(ogq.ogq_layer_norm_backward_workspace(rows, cols, code))
+        got, want = ogq.ogq_layer_norm_backward(dy, x, mean, rstd, weight, workspace=space.space), ogq.ogq_layer_norm_backward(dy, x, mean, rstd, weight)
+        assert space.unharmed() and all(torch.equal(a, b) for a, b in zip(got, want))
+        space = Space(ogq.ogq_linear_backward_workspace(rows, cols, code))
+        got, want = ogq.ogq_linear_backward(dy, ogq.GELU, x, workspace=space.space), ogq.ogq_linear_backward(dy, ogq.GELU, x)
+        assert space.unharmed() and all(torch.equal(a, b) for a, b in zip(got, want))
+        places, values = torch.arange(rows * 5, device=DEV).view(rows, 5) % cols, randn(rows, 5, seed=4)
+        space = Space(ogq.ogq_distill_workspace(rows, cols, code, 5))
+        got, want = ogq.ogq_distill_gradient(x, places, values, workspace=space.space), ogq.ogq_distill_gradient(x, places, values)
+        assert space.unharmed() and all(torch.equal(a, b) for a, b in zip(got, want))
+        tokens = torch.arange(rows, device=DEV) * 7919 % 50
+        space = Space(ogq.ogq_embedding_gradient_workspace(rows, 50, cols))
+        got, want = ogq.ogq_embedding_gradient(tokens, dy, 50, workspace=space.space), ogq.ogq_embedding_gradient(tokens, dy, 50)
+        assert space.unharmed() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+def test_workspaces_of_linear_layers(transposed, dtype):
+    for tokens, outs, cols, _ in LINEAR + [(3, 300, 5000, 0), (8, 1001, 2000, 0), (256, 4096, 2100, 0)]:
+        x, w = randn(tokens, cols, seed=1).to(dtype), randn(cols if transposed else outs, outs if transposed else cols, seed=2).to(dtype)
+        space = Space(ogq.ogq_linear_workspace(tokens, outs, cols, CODE[dtype], transposed))
+        got = ogq.ogq_linear(x, w, transposed=transposed, workspace=space.space)
+        assert space.unharmed() and torch.equal(got, ogq.ogq_linear(x, w, transposed=transposed)), (tokens, outs, cols)
+
+
+def test_calls_of_several_launches_in_graphs():
+    """Two graphs of calls that use a workspace, replayed in turn with other inputs and eager calls between them."""
+    shapes = {"x": (40, 33001), "dy": (40, 33001), "a": (70, 4100), "w": (3000, 4100), "e": (3000, 520), "z": (9, 70001)}
+
+    def inputs(seed):
+        t = {name: randn(*shape, seed=seed + n) for n, (name, shape) in enumerate(shapes.items())}
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        t["tokens"] = torch.randint(-1, 60, (3000,), generator=gen, device=DEV)
+        t["places"], t["values"] = torch.randint(-1, 70001, (9, 6), generator=gen, device=DEV), randn(9, 6, seed=seed + 20)
+        t["x"][::3] += 1.0e5  # (rows far from zero)
+        return t
+
+    def calls(t):
+        y, mean, rstd = ogq.ogq_layer_norm_forward(t["x"])
+        weight = t["dy"][0].abs() + 0.5
+        return [y, *ogq.ogq_layer_norm_backward(t["dy"], t["x"], mean, rstd, weight), ogq.ogq_linear(t["a"], t["w"], None, ogq.GELU), ogq.ogq_linear_backward(t["e"])[1],
+                ogq.ogq_embedding_gradient(t["tokens"], t["e"], 60), *ogq.ogq_distill_gradient(t["z"], t["places"], t["values"])]
+
+    static = inputs(1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls(static)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, results = [], []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(calls(static))
+        graphs.append(graph)
+    for n in range(6):
+        new = inputs(100 * n + 7)
+        for name, t in static.items():
+            t.copy_(new[name])
+        graphs[n % 2].replay()
+        eager = calls(static)
+        torch.cuda.synchronize()
+        for got, want in zip(results[n % 2], eager):
+            assert torch.equal(got, want), n

@@ -328,3 +328,12 @@ def test_products_of_nan_take_a_few_times_as_long(transposed):
     bad = torch.full_like(x, math.nan)
     assert torch.isnan(ogq.ogq_linear(bad, w, transposed=transposed)).all()
     assert fastest(lambda: ogq.ogq_linear(bad, w, transposed=transposed)) < 20 * fastest(lambda: ogq.ogq_linear(x, w, transposed=transposed))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("tokens,outs,cols", [(5, 300, 96), (70, 3000, 4096), (840, 2320, 2432), (4000, 4088, 1472), (5778, 4984, 1344)])
+def test_linear_is_the_same_wherever_rows_begin(tokens, outs, cols, transposed, dtype):
+    """The order of a sum is that of the sizes alone: aligned rows, which large tiles fetch another way, and rows that begin anywhere have the same sums."""
+    x, w = randn(tokens, cols, seed=1).to(dtype), randn(cols if transposed else outs, outs if transposed else cols, seed=2).to(dtype)
+    assert torch.equal(ogq.ogq_linear(laid_out(x, 1), laid_out(w, 3), transposed=transposed), ogq.ogq_linear(x, w, transposed=transposed))
