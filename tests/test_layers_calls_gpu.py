@@ -1,5 +1,6 @@
 """libogq_layers on the GPU: calls that its documentation allows and that look unlike a training step's: rows that are one and the same, vectors and integers that begin anywhere, results with gaps, results left out."""
 import ctypes
+import threading
 
 import pytest
 import torch
@@ -296,3 +297,35 @@ def test_calls_of_several_launches_in_graphs():
         torch.cuda.synchronize()
         for got, want in zip(results[n % 2], eager):
             assert torch.equal(got, want), n
+
+
+def test_calls_at_the_same_time():
+    """Two threads with a stream each: the calls have nothing in common."""
+    def inputs(seed):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        return (randn(60, 33001, seed=seed), randn(33001, seed=seed + 1), randn(70, 4100, seed=seed + 2).bfloat16(), randn(3000, 4100, seed=seed + 3).bfloat16(),
+                torch.randint(-1, 50, (3000,), generator=gen, device=DEV), randn(3000, 400, seed=seed + 4), torch.randint(-1, 33001, (60, 8), generator=gen, device=DEV), randn(60, 8, seed=seed + 5))
+
+    def calls(x, weight, a, w, tokens, e, places, values):
+        y, mean, rstd = ogq.ogq_layer_norm_forward(x, weight)
+        return [y, *ogq.ogq_layer_norm_backward(y, x, mean, rstd, weight), ogq.ogq_linear(a, w, None, ogq.SILU), ogq.ogq_linear(w, a),
+                ogq.ogq_embedding_gradient(tokens, e, 50), *ogq.ogq_distill_gradient(x, places, values)]
+
+    given = [inputs(1), inputs(50)]
+    want = [calls(*t) for t in given]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(n):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(10):
+                got = calls(*given[n])
+                torch.cuda.current_stream().synchronize()
+                wrong.extend(i for i, (a, b) in enumerate(zip(got, want[n])) if not torch.equal(a, b))
+
+    threads = [threading.Thread(target=run, args=(n,)) for n in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not any(t.is_alive() for t in threads) and wrong == []
