@@ -2,7 +2,7 @@
 //
 // One workgroup to a row, which it reads once: largest logit, sum of exponentials and the gradient come from registers.  Bound by memory, with the vector unit close behind (an exponential twice
 // for each logit: keeping the first one's results would take the registers that the logits are in): 4096 x 32768 bf16 with its gradient 107 us, 5.0 TB/s, vector instructions issued in nearly all cycles.
-// Rows too long for the registers are read again, from the caches.  61 x 131071 fp16, several workgroups to a row: 6.3 + 12 us, of which 6.6 are the bytes' and the rest two chains of latencies.
+// Rows too long for the registers are read again, from the caches.  61 x 131071 fp16, several workgroups to a row: 6.1 + 12.7 us, of which 6.6 are the bytes' and the rest two chains of latencies.
 #include "layers_common.h"
 
 namespace ogq {

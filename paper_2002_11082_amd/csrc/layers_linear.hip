@@ -619,7 +619,7 @@ __device__ __forceinline__ void finish_large(const f32x16 (&sum)[4][4], uint32_t
 // A step's four quarters, sixteen products each; behind a product an operand of the next quarter is read or a load to LDS sets off.  LDS holds five planes of 32 KB: the step's two, the next
 // one's, and one to which the next plane is on its way: x two steps ahead in the first two quarters, W in the last, when the step's own operands have been read by all: one barrier a step.  A workgroup
 // stays and takes tile after tile; the next one's first two steps come in while the last one's sums leave, through the plane that is free.
-// Bound by the matrix cores and the power that they draw: 8192 x 4096 to 16384 bf16 880 to 930 us plain (1.18 to 1.25 PFLOP/s, the library's product 786 to 907), 925 to 975 with gelu and what goes into it;
+// Bound by the matrix cores and the power that they draw: 8192 x 4096 to 16384 bf16 880 to 930 us plain (1.18 to 1.25 PFLOP/s, the library's product 786 to 907), 925 to 975 with gelu and what goes into it (the first twenty launches 1000 to 1270, until the card's power has settled);
 // 8192 x 8192 sums of 8192 products 770 to 806 (1.36 to 1.43, library 676 to 728); transposed, 4096 x 4096 to 16384, 462 to 467 (library 504).  Matrix cores are busy for 0.63 to 0.71 of the cycles; products
 // alone, of random values in registers, reach 1.7 PFLOP/s.  No gain: a second set of operands a step ahead, all operands read in the first two quarters.
 template <class T, bool TRANSPOSED>

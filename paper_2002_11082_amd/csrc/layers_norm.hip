@@ -53,7 +53,7 @@ __device__ __forceinline__ Spread spread_of(float2 sums, float per_col, float ep
 }
 
 // P pieces of a row to each of THREADS threads.  `off`, the differences from the mean as it came out of fp32 sums, are summed too: what is left of the mean's rounding is taken off
-// again, so that an offset of the whole row costs nothing but the rounding of x.  Bound by memory: 8192 x 4096 bf16 24.6 us, 5.5 TB/s read and written; one row of 4096 2.8 us, latency.
+// again, so that an offset of the whole row costs nothing but the rounding of x.  Bound by memory: 8192 x 4096 bf16 24.7 us, 5.4 TB/s read and written; one row of 4096 2.9 us, latency.
 template <class T, int THREADS, int P>
 __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_forward_kernel(const T* x, uint64_t x_stride, uint32_t rows, uint32_t cols, const float* weight, const float* bias,
                                                                              float eps, float per_col, T* y, uint64_t y_stride, float* mean, float* rstd)
@@ -208,7 +208,7 @@ __device__ __forceinline__ void store_only(float* to, bool accumulate, const flo
 }
 
 // The backward pass of rows that THREADS threads hold, P pieces each.  A row's values set off while the one before is worked on.  64 threads to a row: the four wavefronts of a workgroup
-// take its rows in turn, and add their sums over the rows in LDS in the end.  Bound by memory: 8192 x 4096 bf16 41 us, 5.3 TB/s with the parts' sums; 1237 x 1001 fp32 5.6 us, latency.
+// take its rows in turn, and add their sums over the rows in LDS in the end.  Bound by memory: 8192 x 4096 bf16 45 us, 4.9 TB/s with the parts' sums (36 with what the caches hold); 1237 x 1001 fp32 5.8 us, latency.
 template <class T, int THREADS, int P>
 __global__ __launch_bounds__(block_of(THREADS)) void layer_norm_backward_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, const float* weight,
                                                                               const float* mean, const float* rstd, T* dx, uint64_t dx_stride)
@@ -392,7 +392,8 @@ enum class Columns { kNorm, kActivation, kSums };
 //   kNorm        the gradient of x, stored in dz, and the sums of dy * u and dy, of rows that no workgroup holds whole, from the rows' means
 //   kActivation  dz = dy * act'(z), stored, and the sums of dz (s.parts may be null)
 //   kSums        the sums of dy
-// Bound by memory: kActivation (gelu by tanh) of 4096 x 4096 bf16 27 us with what the caches hold, 3.7 TB/s.
+// Bound by memory, and by the latency of four rows under way in a wavefront: kActivation (gelu by tanh) of 4096 x 4096 bf16 30 us with what the caches hold, 3.4 TB/s; of slopes that only a 16-bit dz needs 28,
+// so that the vector unit's work is not all hidden.  kNorm of 2000 x 20000 fp32, with the rows' means before it, 162 us, 4.9 TB/s of x and dy read twice and dx written.
 template <class T, Columns WHAT>
 __global__ __launch_bounds__(kBlock) void columns_kernel(const T* dy, uint64_t dy_stride, const T* x, uint64_t x_stride, RowParts s, uint32_t blocks, const float* weight,
                                                        const float* mean, const float* rstd, const RowMeans* means, uint32_t act, T* dz, uint64_t dz_stride)
