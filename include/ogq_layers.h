@@ -51,7 +51,7 @@ int ogq_layer_norm_forward(const void* d_x, size_t x_stride, size_t rows, size_t
 /* Its backward pass.  With u = (x - mean) * rstd and g = dy * weight:
  *   dx = rstd * (g - mean of g - u * mean of (g * u)),   dweight = sum over the rows of dy * u,   dbias = sum over the rows of dy,
  * the last two in fp32 [cols], or added to what they hold (accumulate != 0).  In rows that lie more than 16 deviations from zero what the mean's rounding to fp32 leaves in u, whose mean over
- * a row is 0, is taken off it again, so that an offset costs no more than in the forward pass.  d_dweight and d_dbias are both given or both NULL, and without them there is no workspace.  d_dx may be
+ * a row is 0, is taken off it again, so that an offset costs no more than in the forward pass.  Rows whose rstd is 0 have dx 0 and no part in dweight.  d_dweight and d_dbias are both given or both NULL, and without them there is no workspace.  d_dx may be
  * d_dy with the same stride. */
 size_t ogq_layer_norm_backward_workspace(size_t rows, size_t cols, uint32_t dtype);
 int ogq_layer_norm_backward(const void* d_dy, size_t dy_stride, const void* d_x, size_t x_stride, size_t rows, size_t cols, uint32_t dtype, const float* d_weight,
